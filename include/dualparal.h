@@ -316,6 +316,102 @@ int dp_head_forward_static(const dp_ends_config* cfg, const dp_ends_weights* wei
 int dp_euler_step(float* x, const float* v, int64_t n, float sigma, float sigma_next, void* hip_stream);
 void dp_ends_free(dp_ends_t* ends);
 
+/*
+ * Paged key/value cache, and the operators around it.  A stage keeps ONE block's features of ONE video next to the block being
+ * processed (dp_cache_update).  These operators serve what lies beyond that: several videos on one device, histories of many
+ * blocks, features held in 8 bits.  A cache is a pool of pages, `page_tokens` consecutive tokens of one sequence each; which pages
+ * a sequence owns, in which order, is the caller's table.  They share the stage's readings of RMSNorm, of the 3D rotation and of
+ * softmax(q k^T) v, with norms per head instead of over the full width, and key heads that several query heads may share.
+ *
+ * Rows: element (t, h, c) of an array of [tokens, heads, head_dim] rows lies at data + t * token_stride + h * head_stride + c, in
+ * elements; a view of a fused q | k | v product is such an array.  data and both strides are multiples of 16 bytes (a stride
+ * that is never used, of one token or one head, may be anything); strides are not negative.  Rows that are written do not overlap one
+ * another.
+ */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride; /* in elements                                                */
+} dp_rows;
+
+/* What the pages hold.  DP_KV_PLAIN: the rows as they are (dtype).  DP_KV_FP8: each token's head as head_dim codes of 8 bits
+ * (OCP e4m3: 4 exponent and 3 fraction bits, largest value 448) times one power of two, the least 2^e with e >= -100 by which no
+ * finite value of the row exceeds 448, held as the byte e + 127.  A power of two loses no bit of a floating-point code's precision, and the value
+ * it stands for is exact in bfloat16 and float.  Rounding is to nearest, ties to even; a value that is not finite reads back as NaN. */
+enum { DP_KV_PLAIN = 0, DP_KV_FP8 = 1 };
+typedef struct {
+  int32_t kv_heads;           /* 1 .. 1024                                                         */
+  int32_t head_dim;           /* 64 or 128                                                         */
+  int32_t page_tokens;        /* a power of two, 16 .. 65536                                       */
+  int32_t n_pages;            /* n_pages * page_tokens <= 2^31 - 1                                 */
+  int32_t dtype;              /* DP_F32 or DP_BF16: rows handed over and read back                 */
+  int32_t format;             /* DP_KV_*                                                           */
+  void* data;                 /* device [n_pages, 2 (keys, values), kv_heads, page_tokens, head_dim] of dtype or of codes, 16-byte aligned */
+  uint8_t* scales;            /* device [n_pages, 2, kv_heads, page_tokens], DP_KV_FP8 only        */
+} dp_kv_cache;
+
+/* RMSNorm of every head of q and k over its own head_dim values, times the gain, then the stage's 3D rotation of channel pairs
+ * (2i, 2i+1), in one pass: y = R(pos) (x * rsqrt(mean(x^2) + eps) * g).  Statistics, angles (in 64 bits, any position) and products
+ * are fp32; one rounding at the end.
+ *   gq, gk : device [head_dim], of dtype, shared by the heads;  pos : device int32 [n_tokens, 3], (frame, row, column) */
+typedef struct {
+  int32_t q_heads, kv_heads;  /* 1 .. 1024 each                                                    */
+  int32_t head_dim;           /* 64 or 128                                                         */
+  int32_t dtype;              /* DP_F32 or DP_BF16                                                 */
+  float rope_theta, eps;
+  const void *gq, *gk;
+  const int32_t* pos;
+} dp_norm_rope;
+
+/* q_out and k_out may be q and k themselves (same data and strides); any other overlap with an input is not allowed.  n_tokens == 0 is a
+ * no-op.  Asynchronous on hip_stream, like every call below; none allocates, and all may be recorded into a HIP graph.
+ * Errors: DP_EINVAL (null pointer, sizes outside the limits, more than 2^24 tokens, alignment or strides as above), DP_EHIP. */
+int dp_qk_norm_rope(const dp_norm_rope* cfg, const dp_rows* q, const dp_rows* k, int64_t n_tokens, const dp_rows* q_out,
+                    const dp_rows* k_out, void* hip_stream);
+
+/* Writes the keys and values of n_tokens tokens into the pages: token t goes to place slot[t] % page_tokens of page
+ * slot[t] / page_tokens (int32, device).  A slot outside the pool writes nothing (rows of padding: -1).  The slots of one call are
+ * distinct; of two tokens with the same slot an unspecified mixture is left.  Errors: as above. */
+int dp_kv_write(const dp_kv_cache* cache, const dp_rows* k, const dp_rows* v, const int32_t* slot, int64_t n_tokens, void* hip_stream);
+
+/* dp_qk_norm_rope and dp_kv_write in one pass: q_out as there, the keys written from their fp32 values (one rounding), the values as
+ * they come.  cfg's kv_heads, head_dim and dtype are the cache's.  A token whose slot is outside the pool still gets its q_out. */
+int dp_kv_write_qkv(const dp_kv_cache* cache, const dp_norm_rope* cfg, const dp_rows* q, const dp_rows* k, const dp_rows* v,
+                    const int32_t* slot, int64_t n_tokens, const dp_rows* q_out, void* hip_stream);
+
+/* The keys and values that the pages hold at the given slots, as rows of dtype; a slot outside the pool reads zeros. */
+int dp_kv_read(const dp_kv_cache* cache, const int32_t* slot, int64_t n_tokens, const dp_rows* k_out, const dp_rows* v_out, void* hip_stream);
+
+/* Attention of a chunk of new tokens of each sequence over the keys and values of that sequence in the pages (those of the new tokens
+ * among them, written before): out = softmax(scale * q k^T) v, query head h with key head h / (q_heads / kv_heads).
+ *   q, out     : [n_tokens, q_heads, head_dim] of the cache's dtype, the new tokens of all sequences one behind the other; out may be q
+ *                itself.  Rows of no sequence are left as they are.
+ *   q_start    : device int32 [n_seqs + 1]: sequence b's new tokens are rows q_start[b] .. q_start[b + 1] - 1
+ *   kv_len     : device int32 [n_seqs]: its keys.  The new tokens are the last of them.
+ *   page_table : device int32 [n_seqs, table_width]: the pages of its keys, in order.  Keys of a page outside the pool, or beyond
+ *                table_width pages, do not exist.
+ * causal_group 0: every query sees every key.  g >= 1: keys come in groups of g (1: tokens, tok_h * tok_w: frames), and a query sees the
+ * groups up to its own: with p = kv_len - n + i for the i-th of n new tokens, the keys below (p / g + 1) * g (p >= 0; a query before the
+ * first key sees none).  A query that sees no key, or whose scores are all -inf, gets zeros.  What a query does not see does not touch its result, NaN and
+ * infinities included.
+ * max_q and max_kv size the launch: rows beyond a sequence's first max_q are left as they are, keys beyond max_kv not read.
+ * Scores, softmax and sums are fp32; with DP_BF16 the weights are rounded to bf16 before they meet the values.
+ *   workspace  : device, 256-byte aligned, dp_attn_paged_workspace_bytes(cache, cfg) bytes (0 for most calls: then it may be NULL),
+ *                used by one call at a time; nothing has to be kept in it between calls.
+ * Errors: DP_EINVAL (null pointer, sizes, alignment or strides outside the limits), DP_ENOMEM (workspace too small), DP_EHIP. */
+typedef struct {
+  int32_t q_heads;            /* a multiple of kv_heads, <= 1024                                   */
+  int32_t n_seqs;             /* 0 .. 65535                                                        */
+  int32_t max_q;              /* 0 .. 2^24                                                         */
+  int32_t max_kv;             /* 0 .. 2^31 - 1 - 65536                                             */
+  int32_t table_width;        /* >= 0                                                              */
+  int32_t causal_group;       /* >= 0                                                              */
+  float scale;                /* > 0 and finite, e.g. 1 / sqrt(head_dim)                           */
+} dp_attn_config;
+size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* cache, const dp_attn_config* cfg);   /* 0 also if a config is invalid: dp_attn_paged says why */
+int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_rows* q, int64_t n_tokens, const int32_t* q_start,
+                  const int32_t* kv_len, const int32_t* page_table, const dp_rows* out, void* workspace, size_t workspace_bytes,
+                  void* hip_stream);
+
 /* Test hook: copies an internal result to `dst` as float32, token-major [rows, dim].
  *   what : DP_PEEK_*; layer is used by the K / V / cache / modulation peeks, the others refer to the
  *          last layer the last forward ran (they need cfg.debug_taps for X_SELF / X_CROSS).

@@ -122,6 +122,38 @@ _lib.dp_probe_mfma_bf16.restype = C.c_int
 _lib.dp_probe_mfma_bf16.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(C.c_double)]
 _lib.dp_probe_stream_f32_bf16.restype = C.c_int
 _lib.dp_probe_stream_f32_bf16.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.POINTER(C.c_double)]
+class KvRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class KvCacheDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("kv_heads", "head_dim", "page_tokens", "n_pages", "dtype", "format")] + \
+               [("data", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class NormRope(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("q_heads", "kv_heads", "head_dim", "dtype")] + \
+               [("rope_theta", C.c_float), ("eps", C.c_float), ("gq", C.c_void_p), ("gk", C.c_void_p), ("pos", C.c_void_p)]
+
+
+class AttnConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("q_heads", "n_seqs", "max_q", "max_kv", "table_width", "causal_group")] + [("scale", C.c_float)]
+
+
+_ROWS, _CACHE = C.POINTER(KvRows), C.POINTER(KvCacheDesc)
+_lib.dp_qk_norm_rope.restype = C.c_int
+_lib.dp_qk_norm_rope.argtypes = [C.POINTER(NormRope), _ROWS, _ROWS, C.c_int64, _ROWS, _ROWS, C.c_void_p]
+_lib.dp_kv_write.restype = C.c_int
+_lib.dp_kv_write.argtypes = [_CACHE, _ROWS, _ROWS, C.c_void_p, C.c_int64, C.c_void_p]
+_lib.dp_kv_write_qkv.restype = C.c_int
+_lib.dp_kv_write_qkv.argtypes = [_CACHE, C.POINTER(NormRope), _ROWS, _ROWS, _ROWS, C.c_void_p, C.c_int64, _ROWS, C.c_void_p]
+_lib.dp_kv_read.restype = C.c_int
+_lib.dp_kv_read.argtypes = [_CACHE, C.c_void_p, C.c_int64, _ROWS, _ROWS, C.c_void_p]
+_lib.dp_attn_paged_workspace_bytes.restype = C.c_size_t
+_lib.dp_attn_paged_workspace_bytes.argtypes = [_CACHE, C.POINTER(AttnConfig)]
+_lib.dp_attn_paged.restype = C.c_int
+_lib.dp_attn_paged.argtypes = [_CACHE, C.POINTER(AttnConfig), _ROWS, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, _ROWS, C.c_void_p,
+                               C.c_size_t, C.c_void_p]
 _lib.dp_stage_free.argtypes = [C.c_void_p]
 _lib.dp_last_error.restype = C.c_char_p
 _lib.dp_last_error.argtypes = []
@@ -373,6 +405,143 @@ def euler_step(x, v, sigma, sigma_next, stream=None):
     _check(_lib.dp_euler_step(x.data_ptr(), v.data_ptr(), x.numel(), float(sigma), float(sigma_next), _stream_handle(stream)),
            "dp_euler_step")
     return x
+
+
+_KV_DTYPE = {torch.float32: DP_F32, torch.bfloat16: DP_BF16}
+
+
+def _rows(t, heads, n, like):
+    """t as [n, heads, head_dim] rows of the type and device of `like` = (head_dim, dtype, device)."""
+    assert t.shape == (n, heads, like[0]) and t.dtype == like[1] and t.device == like[2] and (t.stride(2) == 1 or t.numel() == 0), \
+        (tuple(t.shape), t.dtype, t.device, t.stride(), n, heads, like)
+    return KvRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _stream_on(device, stream):
+    """The stream handle of a call on `device`, which has to be the current one: the library launches there."""
+    assert device.type == "cuda" and device.index == torch.cuda.current_device(), f"tensors on {device}, current device {torch.cuda.current_device()}"
+    return _stream_handle(stream)
+
+
+def _used_on(stream, *tensors):
+    """Tensors allocated here and used on a stream that is not the current one: their memory waits for that stream when they go."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _norm_rope(q, k, gq, gk, pos, rope_theta, eps):
+    n, hq, d = q.shape
+    hk, dev, td = k.shape[1], q.device, q.dtype
+    assert td in _KV_DTYPE and gq.shape == gk.shape == (d,) and gq.dtype == gk.dtype == td and gq.is_contiguous() and gk.is_contiguous()
+    assert gq.device == gk.device == pos.device == dev and pos.shape == (n, 3) and pos.dtype == torch.int32 and pos.is_contiguous()
+    return NormRope(hq, hk, d, _KV_DTYPE[td], rope_theta, eps, gq.data_ptr(), gk.data_ptr(), pos.data_ptr())
+
+
+def qk_norm_rope(q, k, gq, gk, pos, rope_theta=1e4, eps=1e-6, q_out=None, k_out=None, stream=None):
+    """RMSNorm of each head of q [n, q_heads, head_dim] and k [n, kv_heads, head_dim] with gains gq, gk [head_dim], then the 3D rotation
+    at pos (int32 [n, 3]: frame, row, column), in one pass.  q and k may be views (of a fused product's output); q_out / k_out may be q / k themselves.
+    Returns (q_out, k_out)."""
+    cfg = _norm_rope(q, k, gq, gk, pos, rope_theta, eps)
+    n, like, st = q.shape[0], (q.shape[2], q.dtype, q.device), _stream_on(q.device, stream)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _used_on(stream, q_out)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        _used_on(stream, k_out)
+    _check(_lib.dp_qk_norm_rope(cfg, _rows(q, cfg.q_heads, n, like), _rows(k, cfg.kv_heads, n, like), n, _rows(q_out, cfg.q_heads, n, like),
+                                _rows(k_out, cfg.kv_heads, n, like), st), "dp_qk_norm_rope")
+    return q_out, k_out
+
+
+class KVCache:
+    """Pages of keys and values of many sequences.  data: [n_pages, 2, kv_heads, page_tokens, head_dim], keys at [:, 0] and values at [:, 1], of
+    the rows' type, or float8_e4m3fn with scales, uint8 [n_pages, 2, kv_heads, page_tokens]: byte b stands for the factor 2^(b - 127).
+    The tensors are the caller's and may be looked at; dtype ("f32", "bf16") is that of the rows, given only with 8-bit data.  Which pages a sequence owns is
+    the caller's page table; a slot is page * page_tokens + place in the page."""
+
+    def __init__(self, data, scales=None, dtype=None):
+        td = {"f32": torch.float32, "bf16": torch.bfloat16, None: data.dtype}[dtype]
+        fp8 = data.dtype == torch.float8_e4m3fn
+        assert td in _KV_DTYPE and (fp8 or td == data.dtype), (td, data.dtype)
+        assert data.is_cuda and data.dim() == 5 and data.shape[1] == 2 and data.is_contiguous(), tuple(data.shape)
+        assert (scales is not None) == fp8, "scales go with 8-bit data"
+        if fp8:
+            assert scales.dtype == torch.uint8 and scales.shape == data.shape[:4] and scales.is_contiguous() and scales.device == data.device
+        self.data, self.scales, self.torch_dtype = data, scales, td
+        self.n_pages, _, self.kv_heads, self.page_tokens, self.head_dim = data.shape
+        self._like = (self.head_dim, td, data.device)
+        self._desc = KvCacheDesc(self.kv_heads, self.head_dim, self.page_tokens, self.n_pages, _KV_DTYPE[td], int(fp8), data.data_ptr(),
+                                 scales.data_ptr() if fp8 else None)
+
+    @classmethod
+    def empty(cls, n_pages, kv_heads, page_tokens, head_dim, dtype="bf16", fp8=False, device=None):
+        """A cache of new, zeroed pages."""
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        shape = (n_pages, 2, kv_heads, page_tokens)
+        if fp8:
+            return cls(torch.zeros(shape + (head_dim,), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn),
+                       torch.full(shape, 127, dtype=torch.uint8, device=device), dtype)
+        return cls(torch.zeros(shape + (head_dim,), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device=device))
+
+    def _slots(self, slot):
+        assert slot.dim() == 1 and slot.dtype == torch.int32 and slot.device == self.data.device and slot.is_contiguous()
+        return slot.data_ptr()
+
+    def write(self, k, v, slot, stream=None):
+        """k, v: [n, kv_heads, head_dim] to slots (int32 [n], distinct; outside the pool: not written)."""
+        n, st = slot.shape[0], _stream_on(self.data.device, stream)
+        _check(_lib.dp_kv_write(self._desc, _rows(k, self.kv_heads, n, self._like), _rows(v, self.kv_heads, n, self._like), self._slots(slot), n, st),
+               "dp_kv_write")
+
+    def write_qkv(self, q, k, v, gq, gk, pos, slot, rope_theta=1e4, eps=1e-6, q_out=None, stream=None):
+        """qk_norm_rope of q and k and the write of k and v, in one pass.  Returns q_out (which may be q)."""
+        cfg = _norm_rope(q, k, gq, gk, pos, rope_theta, eps)
+        n, st = q.shape[0], _stream_on(self.data.device, stream)
+        assert slot.shape[0] == n
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            _used_on(stream, q_out)
+        _check(_lib.dp_kv_write_qkv(self._desc, cfg, _rows(q, cfg.q_heads, n, self._like), _rows(k, self.kv_heads, n, self._like),
+                                    _rows(v, self.kv_heads, n, self._like), self._slots(slot), n, _rows(q_out, cfg.q_heads, n, self._like), st),
+               "dp_kv_write_qkv")
+        return q_out
+
+    def read(self, slot, stream=None):
+        """The keys and values at the slots, [n, kv_heads, head_dim] each, zeros where a slot is outside the pool."""
+        n, st = slot.shape[0], _stream_on(self.data.device, stream)
+        k = torch.empty((n, self.kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.data.device)
+        v = torch.empty_like(k)
+        _used_on(stream, k, v)
+        _check(_lib.dp_kv_read(self._desc, self._slots(slot), n, _rows(k, self.kv_heads, n, self._like), _rows(v, self.kv_heads, n, self._like), st),
+               "dp_kv_read")
+        return k, v
+
+    def attend(self, q, q_start, kv_len, page_table, max_q, max_kv, causal_group=0, scale=None, out=None, stream=None):
+        """Attention of new tokens over their sequences' pages.  q: [n, q_heads, head_dim], the new tokens of all sequences one behind the
+        other; q_start int32 [n_seqs + 1], kv_len int32 [n_seqs], page_table int32 [n_seqs, width] on the device; max_q, max_kv: bounds of the
+        new tokens and of the keys of a sequence.  causal_group 0: every query sees every key; g >= 1: groups of g keys up to its own.
+        scale: 1 / sqrt(head_dim) if not given.  Rows of no sequence are left as they are (as they come, in a new `out`)."""
+        dev = self.data.device
+        n, hq, b = q.shape[0], q.shape[1], kv_len.shape[0]
+        assert q_start.shape == (b + 1,) and kv_len.dim() == 1 and page_table.dim() == 2 and page_table.shape[0] == b
+        for t in (q_start, kv_len, page_table):
+            assert t.dtype == torch.int32 and t.device == dev and t.is_contiguous()
+        st = _stream_on(dev, stream)
+        if out is None:
+            out = torch.empty((n, hq, self.head_dim), dtype=self.torch_dtype, device=dev)
+            _used_on(stream, out)
+        cfg = AttnConfig(hq, b, max_q, max_kv, page_table.shape[1], causal_group, self.head_dim ** -0.5 if scale is None else scale)
+        nbytes = _lib.dp_attn_paged_workspace_bytes(self._desc, cfg)
+        work = None
+        if nbytes:
+            work = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            _used_on(stream, work)
+        _check(_lib.dp_attn_paged(self._desc, cfg, _rows(q, hq, n, self._like), n, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                                  _rows(out, hq, n, self._like), work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
+        return out
 
 
 def pipeline_simulate(n_devices, T, block_num, order="reverse"):
