@@ -395,9 +395,9 @@ int dp_kv_read(const dp_kv_cache* cache, const int32_t* slot, int64_t n_tokens, 
  * infinities included.
  * max_q and max_kv size the launch: rows beyond a sequence's first max_q are left as they are, keys beyond max_kv not read.
  * Scores, softmax and sums are fp32; with DP_BF16 the weights are rounded to bf16 before they meet the values.
- *   workspace  : device, 256-byte aligned, dp_attn_paged_workspace_bytes(cache, cfg) bytes (0 for most calls: then it may be NULL),
- *                used by one call at a time; nothing has to be kept in it between calls.
- * Errors: DP_EINVAL (null pointer, sizes, alignment or strides outside the limits), DP_ENOMEM (workspace too small), DP_EHIP. */
+ *   workspace  : device, 256-byte aligned, dp_attn_paged_workspace_bytes(cache, cfg, n_tokens) bytes (0 for many calls: then it may be
+ *                NULL), used by one call at a time; nothing has to be kept in it between calls.
+ * Errors: DP_EINVAL (null pointer, sizes, alignment or strides outside the limits, n_tokens * q_heads of 2^31 or more), DP_ENOMEM (workspace too small), DP_EHIP. */
 typedef struct {
   int32_t q_heads;            /* a multiple of kv_heads, <= 1024                                   */
   int32_t n_seqs;             /* 0 .. 65535                                                        */
@@ -407,7 +407,7 @@ typedef struct {
   int32_t causal_group;       /* >= 0                                                              */
   float scale;                /* > 0 and finite, e.g. 1 / sqrt(head_dim)                           */
 } dp_attn_config;
-size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* cache, const dp_attn_config* cfg);   /* 0 also if a config is invalid: dp_attn_paged says why */
+size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* cache, const dp_attn_config* cfg, int64_t n_tokens);   /* 0 also if an argument is invalid: dp_attn_paged says why */
 int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_rows* q, int64_t n_tokens, const int32_t* q_start,
                   const int32_t* kv_len, const int32_t* page_table, const dp_rows* out, void* workspace, size_t workspace_bytes,
                   void* hip_stream);

@@ -150,7 +150,7 @@ _lib.dp_kv_write_qkv.argtypes = [_CACHE, C.POINTER(NormRope), _ROWS, _ROWS, _ROW
 _lib.dp_kv_read.restype = C.c_int
 _lib.dp_kv_read.argtypes = [_CACHE, C.c_void_p, C.c_int64, _ROWS, _ROWS, C.c_void_p]
 _lib.dp_attn_paged_workspace_bytes.restype = C.c_size_t
-_lib.dp_attn_paged_workspace_bytes.argtypes = [_CACHE, C.POINTER(AttnConfig)]
+_lib.dp_attn_paged_workspace_bytes.argtypes = [_CACHE, C.POINTER(AttnConfig), C.c_int64]
 _lib.dp_attn_paged.restype = C.c_int
 _lib.dp_attn_paged.argtypes = [_CACHE, C.POINTER(AttnConfig), _ROWS, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, _ROWS, C.c_void_p,
                                C.c_size_t, C.c_void_p]
@@ -534,7 +534,7 @@ class KVCache:
             out = torch.empty((n, hq, self.head_dim), dtype=self.torch_dtype, device=dev)
             _used_on(stream, out)
         cfg = AttnConfig(hq, b, max_q, max_kv, page_table.shape[1], causal_group, self.head_dim ** -0.5 if scale is None else scale)
-        nbytes = _lib.dp_attn_paged_workspace_bytes(self._desc, cfg)
+        nbytes = _lib.dp_attn_paged_workspace_bytes(self._desc, cfg, n)
         work = None
         if nbytes:
             work = torch.empty(nbytes, dtype=torch.uint8, device=dev)

@@ -1,50 +1,12 @@
-// Attention of a chunk of new tokens over the pages of a key/value cache (dp_attn_paged).
+// Attention of a chunk of new tokens over the pages of a key/value cache: the C entry, and the fp32 kernel (bf16: attn_paged_bf16.hip).
 //
-// Simplest form: one wavefront per new token and query head, 64 keys at a time (a lane owns a key's score), online softmax in fp32, the weighted sum
-// over the values with a lane owning channels.
+// fp32: one wavefront per new token and query head, 64 keys at a time (a lane owns a key's score), online softmax, the weighted sum over the
+// values with a lane owning channels.
 #include <math.h>
 
-#include "paged.h"
+#include "attn_paged.h"
 
 namespace {
-
-struct PagedArgs {
-  const void* data;
-  const uint8_t* scales;
-  const void* q;
-  void* out;
-  int64_t q_ts, q_hs, o_ts, o_hs, n_tokens;
-  const int32_t *q_start, *kv_len, *table;
-  int32_t n_pages, page_shift, hk, shared, n_seqs, max_q, max_kv, table_width, group;
-  float scale;                            // of the scores, times log2(e): softmax in powers of two
-};
-// a sequence's new tokens and keys, whatever the arrays hold
-struct Seq { int64_t row0; int n, rows, keys; };
-__device__ __forceinline__ Seq sequence(const PagedArgs& a, int b) {
-  Seq s;
-  int64_t r0 = a.q_start[b], r1 = a.q_start[b + 1];
-  r0 = r0 < 0 ? 0 : r0 > a.n_tokens ? a.n_tokens : r0;
-  r1 = r1 < r0 ? r0 : r1 > a.n_tokens ? a.n_tokens : r1;
-  s.row0 = r0;
-  s.n = (int)(r1 - r0);
-  s.rows = s.n < a.max_q ? s.n : a.max_q;
-  s.keys = a.kv_len[b] < 0 ? 0 : a.kv_len[b];
-  return s;
-}
-// keys that exist in the table and within the bound
-__device__ __forceinline__ int held(const PagedArgs& a, int keys) {
-  const int64_t most = (int64_t)a.table_width << a.page_shift;
-  const int k = keys < a.max_kv ? keys : a.max_kv;
-  return k < most ? k : (int)most;
-}
-// keys that the i-th of n new tokens sees, of keys
-__device__ __forceinline__ int seen(const PagedArgs& a, int i, int n, int keys) {
-  if (a.group == 0) return keys;
-  const int64_t p = (int64_t)keys - n + i;
-  if (p < 0) return 0;
-  const int64_t end = (p / a.group + 1) * a.group;
-  return end < keys ? (int)end : keys;
-}
 
 template <typename T, int HD, bool CODES>
 __global__ __launch_bounds__(64) void k_attn_paged_plain(const PagedArgs a) {
@@ -52,10 +14,10 @@ __global__ __launch_bounds__(64) void k_attn_paged_plain(const PagedArgs a) {
   const int lane = threadIdx.x, b = blockIdx.z, head = blockIdx.y, i = blockIdx.x;
   const Seq s = sequence(a, b);
   if (i >= s.rows) return;
-  const int keys = held(a, s.keys), hk = head / a.shared;
-  int end = seen(a, i, s.n, s.keys);
+  const int keys = held_keys(a, s.keys), hk = head / a.shared;
+  int end = seen_keys(a, i, s.n, s.keys);
   end = end < keys ? end : keys;
-  const T* const q = (const T*)a.q + (s.row0 + i) * a.q_ts + head * a.q_hs;
+  const T* const q = (const T*)a.q + (int64_t)(s.row0 + i) * a.q_ts + head * a.q_hs;
   for (int c = lane; c < HD; c += 64) sq[c] = Elem<T>::ld(q + c);
   __syncthreads();
   auto value = [&](int64_t row, int c) __attribute__((always_inline)) {
@@ -90,7 +52,7 @@ __global__ __launch_bounds__(64) void k_attn_paged_plain(const PagedArgs a) {
       for (int c = 0; c < HD / 64; ++c) o[c] = fmaf(wj, value(rj + ((int64_t)a.hk << a.page_shift), c * 64 + lane), o[c]);
     }
   }
-  T* const out = (T*)a.out + (s.row0 + i) * a.o_ts + head * a.o_hs;
+  T* const out = (T*)a.out + (int64_t)(s.row0 + i) * a.o_ts + head * a.o_hs;
   for (int c = 0; c < HD / 64; ++c) Elem<T>::st(out + c * 64 + lane, l > 0.f || l != l ? o[c] / l : 0.f);
 }
 
@@ -111,9 +73,28 @@ const char* why_not_attn(const dp_kv_cache* c, const dp_attn_config* cfg) {
 
 #define REFUSE_IF(expr) do { if (const char* why = (expr)) return refuse(entry, why); } while (0)
 
-extern "C" size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* c, const dp_attn_config* cfg) {
-  if (const char* why = why_not_attn(c, cfg)) { refuse("dp_attn_paged_workspace_bytes", why); return 0; }
-  return 0;
+namespace {
+PagedArgs arguments(const dp_kv_cache* c, const dp_attn_config* cfg, int64_t n_tokens) {
+  PagedArgs a{};
+  a.data = c->data; a.scales = c->scales; a.n_tokens = n_tokens;
+  a.n_pages = c->n_pages; a.page_shift = __builtin_ctz((unsigned)c->page_tokens); a.hk = c->kv_heads; a.shared = cfg->q_heads / c->kv_heads;
+  a.n_seqs = cfg->n_seqs; a.max_q = cfg->max_q < n_tokens ? cfg->max_q : (int32_t)n_tokens; a.table_width = cfg->table_width; a.group = cfg->causal_group;
+  const int64_t most = (int64_t)cfg->table_width << a.page_shift;
+  a.max_kv = cfg->max_kv < most ? cfg->max_kv : (int32_t)most;
+  a.scale = cfg->scale * 1.4426950408889634f;
+  return a;
+}
+const char* why_not_tokens(int64_t n, const dp_attn_config* cfg) {
+  return n < 0 || n > (1 << 24) || n * cfg->q_heads > 0x7fffffff ? "n_tokens must be in [0, 2^24], n_tokens * q_heads below 2^31" : nullptr;
+}
+}  // namespace
+
+extern "C" size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* c, const dp_attn_config* cfg, int64_t n_tokens) {
+  const char* why = why_not_attn(c, cfg);
+  if (!why) why = why_not_tokens(n_tokens, cfg);
+  if (why) { refuse("dp_attn_paged_workspace_bytes", why); return 0; }
+  if (n_tokens == 0 || cfg->n_seqs == 0 || cfg->max_q == 0) return 0;
+  return c->dtype == DP_BF16 ? launch_attn_paged_bf16(arguments(c, cfg, n_tokens), c->head_dim, c->format == DP_KV_FP8, false, nullptr) : 0;
 }
 
 extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, const dp_rows* q, int64_t n_tokens, const int32_t* q_start,
@@ -121,27 +102,35 @@ extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, co
                              void* stream) {
   static const char entry[] = "dp_attn_paged";
   REFUSE_IF(why_not_attn(c, cfg));
-  REFUSE_IF(n_tokens < 0 || n_tokens > (1 << 24) ? "n_tokens must be in [0, 2^24]" : nullptr);
+  REFUSE_IF(why_not_tokens(n_tokens, cfg));
   if (n_tokens == 0 || cfg->n_seqs == 0 || cfg->max_q == 0) return DP_OK;
   REFUSE_IF(!q_start || !kv_len || (!page_table && cfg->table_width > 0) ? "null pointer" : nullptr);
   REFUSE_IF(((uintptr_t)q_start | (uintptr_t)kv_len | (uintptr_t)page_table) & 3 ? "index arrays must be 4-byte aligned" : nullptr);
   REFUSE_IF(why_not_rows(q, n_tokens, cfg->q_heads, c->head_dim, c->dtype, false));
   REFUSE_IF(why_not_rows(out, n_tokens, cfg->q_heads, c->head_dim, c->dtype, true));
-  PagedArgs a{};
-  a.data = c->data; a.scales = c->scales; a.q = q->data; a.out = out->data;
+  PagedArgs a = arguments(c, cfg, n_tokens);
+  a.q = q->data; a.out = out->data;
   a.q_ts = q->token_stride; a.q_hs = q->head_stride; a.o_ts = out->token_stride; a.o_hs = out->head_stride;
-  a.n_tokens = n_tokens; a.q_start = q_start; a.kv_len = kv_len; a.table = page_table;
-  a.n_pages = c->n_pages; a.page_shift = __builtin_ctz((unsigned)c->page_tokens); a.hk = c->kv_heads; a.shared = cfg->q_heads / c->kv_heads;
-  a.n_seqs = cfg->n_seqs; a.max_q = cfg->max_q; a.max_kv = cfg->max_kv; a.table_width = cfg->table_width; a.group = cfg->causal_group;
-  a.scale = cfg->scale * 1.4426950408889634f;
-  const dim3 grid((unsigned)(cfg->max_q < n_tokens ? cfg->max_q : n_tokens), (unsigned)cfg->q_heads, (unsigned)cfg->n_seqs);
+  a.q_start = q_start; a.kv_len = kv_len; a.table = page_table;
   const hipStream_t st = (hipStream_t)stream;
   const bool codes = c->format == DP_KV_FP8;
+  if (c->dtype == DP_BF16) {
+    const size_t need = launch_attn_paged_bf16(a, c->head_dim, codes, false, nullptr);
+    if (need > 0) {
+      REFUSE_IF((uintptr_t)workspace & 255 ? "the workspace must be 256-byte aligned" : nullptr);
+      if (!workspace || workspace_bytes < need) return dp_set_error(DP_ENOMEM, "dp_attn_paged: workspace too small");
+    }
+    a.partial = (float*)workspace;
+  }
   (void)hipGetLastError();
-#define PLAIN(T, HD) do { if (codes) k_attn_paged_plain<T, HD, true><<<grid, 64, 0, st>>>(a); else k_attn_paged_plain<T, HD, false><<<grid, 64, 0, st>>>(a); } while (0)
-  if (c->dtype == DP_BF16) { if (c->head_dim == 128) PLAIN(bf16_t, 128); else PLAIN(bf16_t, 64); }
-  else { if (c->head_dim == 128) PLAIN(float, 128); else PLAIN(float, 64); }
+  if (c->dtype == DP_BF16) {
+    launch_attn_paged_bf16(a, c->head_dim, codes, true, st);
+  } else {
+    const dim3 grid((unsigned)a.max_q, (unsigned)cfg->q_heads, (unsigned)cfg->n_seqs);
+#define PLAIN(HD) do { if (codes) k_attn_paged_plain<float, HD, true><<<grid, 64, 0, st>>>(a); else k_attn_paged_plain<float, HD, false><<<grid, 64, 0, st>>>(a); } while (0)
+    if (c->head_dim == 128) PLAIN(128); else PLAIN(64);
 #undef PLAIN
+  }
   if (hipGetLastError() != hipSuccess) return dp_set_error(DP_EHIP, "dp_attn_paged: the launch failed");
   return DP_OK;
 }

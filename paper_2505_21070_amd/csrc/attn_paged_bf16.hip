@@ -1,0 +1,718 @@
+// Attention of new tokens over the pages of a key/value cache, bf16 (dp_attn_paged).
+//
+// Scores are computed transposed, S^T = K Q^T (v_mfma_f32_16x16x32_bf16), so that a lane's accumulators belong to one row and, turned
+// into weights and rounded to bf16, are the B operand of O^T = V^T P^T as they stand.  The rows of a block are (new token, query head)
+// pairs that share a key head: the matrix instructions' columns are filled by shared heads as by tokens, and one read of the keys serves
+// all of them.  Keys and values go from their pages through registers into LDS (codes of 8 bits become bf16 on the way, exactly) in rows as they
+// lie in the page; the operand V^T comes out of LDS by transposing reads (ds_read_b64_tr_b16), whose four consecutive keys a lane are just
+// those of four accumulators.
+//
+// A tile of keys is either seen whole by every row of the block, or holds a border (the sequence's end, a causal border, a page that
+// does not exist).  Whole tiles come first; a tile with a border is masked key by key, and its values that are not finite are kept from
+// the rows that do not see them (weighted_sum_checked).
+#include <math.h>
+
+#include <atomic>
+
+#include "attn_paged.h"
+#include "kernels.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float add_pk(uint32_t pk, float acc) {          // acc + lo + hi of a packed bf16 pair
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), __builtin_bit_cast(bf16x2, 0x3f803f80u), acc, false);
+}
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// LDS by byte address: 16 bytes in and out, and the transposing read of 8
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+#else
+  return 0;
+#endif
+}
+// an address that the constants added to it stay apart from, in the instructions' offset fields
+__device__ __forceinline__ uint32_t lds_base(uint32_t at) {
+#ifdef __HIP_DEVICE_COMPILE__
+  asm("" : "+v"(at));
+#endif
+  return at;
+}
+__device__ __forceinline__ bf16x8 lds_get(uint32_t at) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_bit_cast(bf16x8, *(const __attribute__((address_space(3))) u32x4*)at);
+#else
+  return bf16x8{};
+#endif
+}
+template <typename V> __device__ __forceinline__ void lds_put(uint32_t at, V v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  *(__attribute__((address_space(3))) V*)at = v;
+#endif
+}
+__device__ __forceinline__ bf16x4 lds_get_transposed(uint32_t at) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
+#else
+  return bf16x4{};
+#endif
+}
+
+// LDS tiles: rows of HD bf16 values, their 16-byte chunks exchanged by the row so that what an instruction reads spreads over the 64
+// banks: 16 rows of one chunk column (keys, 16 bytes a lane) and 16 rows of two (values, the transposing read's 32 bytes of a row).
+template <int HD> __device__ __forceinline__ int k_swizzle(int row) { return HD == 128 ? row & 15 : (row >> 1) & 7; }
+template <int HD> __device__ __forceinline__ int v_swizzle(int row) { return HD == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
+
+// A tile of TK keys and values on its way from the pages into LDS, in the registers of W wavefronts, of which this is number w.
+template <int HD, int TK, int W, bool CODES> struct Carry {
+  static constexpr int ROW = CODES ? HD : HD * 2;                            // bytes of a row in the pages
+  static constexpr int LB = TK * ROW / (W * 64) < 16 ? TK * ROW / (W * 64) : 16;   // bytes a lane takes at once
+  static constexpr int N = TK * ROW / (W * 64 * LB), RW = 64 * LB / ROW;     // trips, rows of a trip of one wavefront
+  static_assert(N * W * RW == TK && RW <= 16 && (LB == 16 || LB == 8), "a trip's rows lie in one page");
+  typedef typename std::conditional<LB == 16, u32x4, u32x2>::type Raw;
+  Raw raw[N];
+  uint32_t byte[CODES ? N : 1];
+  // keys key0 .. of the block's sequence; keys_or_values: rows between a head's keys and its values
+  __device__ __forceinline__ void load(const PagedArgs& a, const Block& b, int key0, int64_t to_values, int w, int lane) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t row = page_row(a, b, key0 + (i * W + w) * RW) + to_values;
+      raw[i] = *(const Raw*)((const char*)a.data + row * ROW + lane * LB);
+      if constexpr (CODES) byte[i] = (a.scales + row)[lane / (ROW / LB)];
+    }
+  }
+  template <bool VALUES> __device__ __forceinline__ void store(uint32_t tile, int w, int lane) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int row = (i * W + w) * RW + lane / (ROW / LB), s = (VALUES ? v_swizzle<HD>(row) : k_swizzle<HD>(row)) * 16;
+      const uint32_t at = tile + row * HD * 2;
+      if constexpr (!CODES) {
+        lds_put(at + (lane % (ROW / LB) * LB ^ s), raw[i]);
+      } else {
+        const float f = __uint_as_float(byte[i] << 23);
+        const int c = lane % (ROW / LB) * LB * 2;
+#pragma unroll
+        for (int h = 0; h < LB / 8; ++h)
+          lds_put(at + ((c + h * 16) ^ s), __builtin_bit_cast(u32x4, fp8x8_to_bf16(make_uint2(raw[i][2 * h], raw[i][2 * h + 1]), f)));
+      }
+    }
+  }
+};
+
+// A lane's place in a tile's rows for either operand, before the exchange of chunks: what selects channels is exclusive-or'ed in.
+template <int HD> __device__ __forceinline__ uint32_t k_lane(int lane) { return (lane & 15) * HD * 2 + ((lane >> 4) ^ k_swizzle<HD>(lane & 15)) * 16; }
+template <int HD> __device__ __forceinline__ uint32_t v_lane(int lane) {
+  const int r = (lane >> 4) * 4 + ((lane >> 2) & 3);         // each group of 16 lanes hands the read four rows' 32 bytes and gets a channel a lane
+  return r * HD * 2 + (((lane >> 1) & 1) ^ v_swizzle<HD>(r)) * 16 + (lane & 1) * 8;
+}
+// keys kt * 16 .., channels ks * 32 .. of a tile: A operand of S^T
+template <int HD> __device__ __forceinline__ bf16x8 read_k(uint32_t tile, uint32_t klane, int kt, int ks) {
+  return lds_get(lds_base((klane ^ (ks * 64)) + tile) + kt * 16 * HD * 2);
+}
+// keys s * 32 .., channels d * 16 .. of a tile: A operand of O^T.  Element e of a lane is key s * 32 + (e >> 2) * 16 + (lane >> 4) * 4 + (e & 3), as in the
+// accumulators of two tiles of 16 keys.
+template <int HD> __device__ __forceinline__ bf16x8 read_v(uint32_t tile, uint32_t vlane, int s, int d) {
+  const uint32_t at = lds_base((vlane ^ (d * 32)) + tile) + s * 32 * HD * 2;
+  return __builtin_shufflevector(lds_get_transposed(at), lds_get_transposed(at + 16 * HD * 2), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The softmax of 16 rows (one a lane & 15; the four lanes of a row hold keys of their own): reference and sums so far.  m is in units of
+// log2, after the scale; -inf as long as there is no score above it.
+struct Soft { float m, l; };
+
+// Weights of KT tiles of 16 keys of a row, from scores in sc, packed for the second product; l grows by the rounded weights.  The reference is m
+// (finite, or 0 while there is none).
+template <int KT> __device__ __forceinline__ void weigh(const f32x4 (&sc)[KT], float scale, float ref, float& l, uint4 (&pf)[KT / 2]) {
+#pragma unroll
+  for (int s = 0; s < KT / 2; ++s) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4& v = sc[2 * s + (i >> 1)];
+      w[i] = pack_bf16x2(__builtin_amdgcn_exp2f(fmaf(v[2 * (i & 1)], scale, -ref)), __builtin_amdgcn_exp2f(fmaf(v[2 * (i & 1) + 1], scale, -ref)));
+      l = add_pk(w[i], l);
+    }
+    pf[s] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+template <int KT> __device__ __forceinline__ float maximum(const f32x4 (&sc)[KT], int kt1) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+    if (kt < kt1)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[kt][r]);
+  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+  return fmaxf(mx, __shfl_xor(mx, 32, 64));
+}
+// raises the reference to the tile's maximum: returns the factor of what was summed so far, and the reference to weigh with
+__device__ __forceinline__ float raise(Soft& z, float top, float& ref) {
+  const float m = fmaxf(z.m, top);
+  ref = m == -INFINITY ? 0.f : m;
+  const float alpha = __builtin_amdgcn_exp2f(z.m - ref);     // 0 while there was no reference
+  z.m = m;
+  z.l *= alpha;
+  return alpha;
+}
+// Of a lane's four keys in each tile of 16 from key0 on: bit kt where their page does not exist (pages hold whole groups of 16)
+template <int KT> __device__ __forceinline__ uint32_t missing(const PagedArgs& a, const Block& b, int key0, int lane) {
+  uint32_t gone = 0;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const int key = key0 + kt * 16 + (lane >> 4) * 4;
+    gone |= (page_exists(a, b, key < b.end ? key : b.end - 1) ? 0u : 1u) << kt;
+  }
+  return gone;
+}
+// -inf for the keys that a row does not see: key0 is the tile's first, end the row's border
+template <int KT> __device__ __forceinline__ void hide(f32x4 (&sc)[KT], int key0, int end, uint32_t gone, int lane) {
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sc[kt][r] = (key0 + kt * 16 + (lane >> 4) * 4 + r >= end) | ((gone >> kt) & 1) ? -INFINITY : sc[kt][r];
+}
+// bf16 pairs: where the exponent is all ones (infinity or NaN)
+__device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+// O^T += V^T P^T of 32 keys, NT tiles of 16 rows, where a value that is not finite must not meet the weight 0 of a row that does not see its key (0 *
+// infinity is NaN).  Values are multiplied with what is not finite set to 0; rows that do see +inf, -inf or NaN in a channel are found by
+// products of ones and get it added.  seen: B operand of ones where the row sees the key.
+template <int HD, int NT>
+__device__ __forceinline__ void weighted_sum_checked(uint32_t tile, uint32_t vlane, int s, const uint4 (&pf)[NT], const uint4 (&seen)[NT], f32x4 (&o)[HD / 16][NT]) {
+#pragma unroll
+  for (int d = 0; d < HD / 16; ++d) {
+    uint4 v = __builtin_bit_cast(uint4, read_v<HD>(tile, vlane, s, d));
+    const bool bad = not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+    if (!__any(bad)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[d][t] = mfma(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pf[t]), o[d][t]);
+      continue;
+    }
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t fin[4], pos[4], neg[4], nan[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      fin[i] = w[i]; pos[i] = neg[i] = nan[i] = 0;
+#pragma unroll
+      for (int h = 0; h < 32; h += 16) {
+        const uint32_t x = (w[i] >> h) & 0xffffu;
+        if ((x & 0x7f80u) == 0x7f80u) fin[i] &= ~(0xffffu << h);
+        pos[i] |= (x == 0x7f80u ? 0x3f80u : 0u) << h;
+        neg[i] |= (x == 0xff80u ? 0x3f80u : 0u) << h;
+        nan[i] |= ((x & 0x7fffu) > 0x7f80u ? 0x3f80u : 0u) << h;
+      }
+    }
+    auto vec = [](const uint32_t (&x)[4]) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3])); };
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+      const bf16x8 ones = __builtin_bit_cast(bf16x8, seen[t]);
+      const f32x4 np = mfma(vec(pos), ones, zero), nn = mfma(vec(neg), ones, zero), nx = mfma(vec(nan), ones, zero);
+      o[d][t] = mfma(vec(fin), __builtin_bit_cast(bf16x8, pf[t]), o[d][t]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = o[d][t][r] + (np[r] > 0.f ? INFINITY : 0.f) - (nn[r] > 0.f ? INFINITY : 0.f);
+        o[d][t][r] = nx[r] > 0.f ? __uint_as_float(0x7fc00000u) : x;
+      }
+    }
+  }
+}
+// ones where a score is above -inf
+__device__ __forceinline__ uint4 ones_of(const f32x4& x, const f32x4& y) {
+  auto pair = [](float p, float q) __attribute__((always_inline)) { return (p == -INFINITY ? 0u : 0x3f80u) | (q == -INFINITY ? 0u : 0x3f800000u); };
+  return make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(y[0], y[1]), pair(y[2], y[3]));
+}
+// One tile of KT * 16 keys in plain order: scores, what a row does not see, the classical online softmax, the weighted sum.
+template <int HD, int KT, int NT>
+__device__ __forceinline__ void step(const PagedArgs& a, const Block& b, uint32_t ktile, uint32_t vtile, const bf16x8 (&qf)[NT][HD / 32], int key0, bool border,
+                                     const int (&end)[NT], bool gaps, Soft (&z)[NT], f32x4 (&o)[HD / 16][NT], int lane) {
+  f32x4 sc[NT][KT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int ks = 0; ks < HD / 32; ++ks)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      const bf16x8 kf = read_k<HD>(ktile, k_lane<HD>(lane), kt, ks);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sc[t][kt] = mfma(kf, qf[t][ks], sc[t][kt]);
+    }
+  uint4 pf[NT][KT / 2];
+  const uint32_t gone = gaps ? missing<KT>(a, b, key0, lane) : 0;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (border) hide<KT>(sc[t], key0, end[t], gone, lane);
+    float ref;
+    const float alpha = raise(z[t], maximum<KT>(sc[t], KT) * a.scale, ref);
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) o[d][t] *= alpha;
+    weigh<KT>(sc[t], a.scale, ref, z[t].l, pf[t]);
+  }
+#pragma unroll
+  for (int s = 0; s < KT / 2; ++s) {
+    uint4 p[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) p[t] = pf[t][s];
+    if (border) {
+      uint4 seen[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) seen[t] = ones_of(sc[t][2 * s], sc[t][2 * s + 1]);
+      weighted_sum_checked<HD, NT>(vtile, v_lane<HD>(lane), s, p, seen, o);
+    } else {
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) {
+        const bf16x8 vf = read_v<HD>(vtile, v_lane<HD>(lane), s, d);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[d][t] = mfma(vf, __builtin_bit_cast(bf16x8, p[t]), o[d][t]);
+      }
+    }
+  }
+}
+// 1 / l, or 0 for a row without a weight; NaN stays
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float over_lanes(float v) { v += __shfl_xor(v, 16, 64); return v + __shfl_xor(v, 32, 64); }
+
+template <int HD, int NT>
+__device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b, int row0, bf16x8 (&qf)[NT][HD / 32], int (&end)[NT], int lane) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = row0 + t * 16 + (lane & 15);
+    const bf16_t* const q = (const bf16_t*)a.q + row_at(a, b, row < b.rows ? row : b.rows - 1, a.q_ts, a.q_hs) + (lane >> 4) * 8;
+#pragma unroll
+    for (int ks = 0; ks < HD / 32; ++ks) qf[t][ks] = __builtin_bit_cast(bf16x8, *(const uint4*)(q + ks * 32));
+    end[t] = row_end(a, b, row);
+  }
+}
+
+// Few rows: NT * 16 of them, four wavefronts that deal the block's keys out in tiles of 32 (wavefront w: tiles w, w + 4, ...), each through its own piece of
+// LDS, the next tile on its way in registers; nobody waits for anybody until the four results are joined in LDS, in wavefront order.  Two
+// blocks to a CU keep 128 KB (codes: 64 KB) under way.  What bounds it: memory.
+template <int HD, int NT, bool CODES>
+__global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
+  constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
+  __shared__ uint4 smem[4 * 2 * TILE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x % a.parts), id = blockIdx.x / a.parts;
+  Block b;
+  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b)) return;
+  const int k0 = part * a.part_keys, k1 = b.end < k0 + a.part_keys || a.parts == 1 ? b.end : k0 + a.part_keys;
+  if (k0 >= k1 && part > 0) return;
+  bf16x8 qf[NT][HD / 32];
+  int end[NT];
+  load_queries<HD, NT>(a, b, b.first, qf, end, lane);
+  const bool gaps = __builtin_amdgcn_readfirstlane(pages_missing(a, b, k0, k1));
+  const uint32_t kt = lds_address(smem) + wave * 2 * TILE * 16, vt = kt + TILE * 16;
+  const int64_t to_values = (int64_t)a.hk << a.page_shift;
+  Soft z[NT];
+  f32x4 o[HD / 16][NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    z[t] = Soft{-INFINITY, 0.f};
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  Carry<HD, 32, 1, CODES> ck, cv;
+  int key = k0 + wave * 32;
+  if (key < k1) { ck.load(a, b, key, 0, 0, lane); cv.load(a, b, key, to_values, 0, lane); }
+  for (; key < k1; key += 128) {
+    ck.template store<false>(kt, 0, lane);
+    cv.template store<true>(vt, 0, lane);
+    if (key + 128 < k1) { ck.load(a, b, key + 128, 0, 0, lane); cv.load(a, b, key + 128, to_values, 0, lane); }
+    step<HD, KT, NT>(a, b, kt, vt, qf, key, key + 32 > b.whole || gaps, end, gaps, z, o, lane);
+  }
+  // join, 16 rows at a time: every wavefront's m and l and its O^T by rows, added up at the common reference
+  constexpr int OS = HD + 4;
+  float* const ml = (float*)smem;                            // [4][16][2]
+  float* const os = ml + 4 * 16 * 2;                         // [4][16][OS]
+  static_assert((4 * 16 * 2 + 4 * 16 * OS) * 4 <= (int)sizeof(smem), "fits the tiles' place");
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (b.first + t * 16 >= b.rows) break;
+    __syncthreads();
+    const float lsum = over_lanes(z[t].l);
+    if (lane < 16) { ml[(wave * 16 + lane) * 2] = z[t].m; ml[(wave * 16 + lane) * 2 + 1] = lsum; }
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) *(f32x4*)(os + (wave * 16 + (lane & 15)) * OS + d * 16 + (lane >> 4) * 4) = o[d][t];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * (HD / 4); i += 256) {
+      const int r = i / (HD / 4), c = i % (HD / 4) * 4, row = t * 16 + r;
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      float l = 0.f;
+      f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - ref);
+        l += ml[(w * 16 + r) * 2 + 1] * f;
+        v += *(const f32x4*)(os + (w * 16 + r) * OS + c) * f;
+      }
+      if (b.first + row >= b.rows) continue;
+      if (a.parts == 1) {
+        const float inv = inverse(l);
+        *(uint2*)((bf16_t*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c) = make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
+      } else {
+        float* const ps = a.partial + (size_t)blockIdx.x * (QB * (2 + HD));
+        if (c == 0) { ps[row] = m; ps[QB + row] = l; }
+        *(f32x4*)(ps + 2 * QB + row * HD + c) = v;
+      }
+    }
+  }
+}
+
+// Joins the key ranges of a block's rows: a lane has four channels of a row.
+template <int HD, int QB>
+__global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
+  constexpr int LANES = HD / 4, ROWS = 256 / LANES;
+  const int id = blockIdx.x / (QB / ROWS), row = blockIdx.x % (QB / ROWS) * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+  Block b;
+  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b) || b.first + row >= b.rows) return;
+  int parts = (int)(((int64_t)b.end + a.part_keys - 1) / a.part_keys);
+  if (parts < 1) parts = 1;                                  // the first range is always there
+  const float* const ps = a.partial + (size_t)id * a.parts * (QB * (2 + HD));
+  float m = -INFINITY;
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, ps[(size_t)i * (QB * (2 + HD)) + row]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  f32x4 v{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < parts; ++i) {
+    const float* const p = ps + (size_t)i * (QB * (2 + HD));
+    const float f = __builtin_amdgcn_exp2f(p[row] - ref);
+    l += p[QB + row] * f;
+    v += *(const f32x4*)(p + 2 * QB + row * HD + c) * f;
+  }
+  const float inv = inverse(l);
+  *(uint2*)((bf16_t*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c) = make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
+}
+
+// Many rows: eight wavefronts of 32 rows (two columns of 16), key tiles of 64.  KG = 1: all share every tile, a block has 256 rows and its halves are the
+// wavefronts 0-3 and 4-7.  KG = 2: the halves have the same 128 rows and one part of the keys each, with tiles of their own, and meet in LDS at the end.
+// Whole tiles: the two wavefronts of a SIMD (one of each half) take turns, with a barrier at every change: one multiplies, the scores
+// of tile j + 1 and the weighted sum of tile j, and reads tile j's values from LDS between the products; the other turns its scores
+// of tile j + 1 into weights, reads tile j + 2's keys, and moves tiles to come: from registers into LDS (keys of j + 3, values of j + 2), the ones behind
+// them from the pages into registers.  The softmax's reference is fixed to a row's maximum over the first 32 keys: weights (bf16) and
+// fp32 sums have 8 exponent bits, so nothing is lost until a sum is beyond 2^100; such a block, or one that is not finite, is done again by the
+// classical online softmax (step), which also does the tiles that hold a border.
+// What bounds it: the matrix pipes.
+template <int HD, int KG, bool CODES>
+__global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
+  constexpr int KS = HD / 32, DT = HD / 16, TILE = 64 * HD * 2;   // bytes
+  constexpr int QG = 8 / KG, QB = QG * 32;   // wavefronts that share a tile; rows per block
+  constexpr int NS = KG == 1 ? 3 : 2;        // LDS stages of either
+  extern __shared__ uint4 smem[];            // per key group: NS key tiles, NS value tiles
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qt = wave % QG, kg = wave / QG;
+  // blocks are handed out to the eight XCDs in turn: each gets a run of tiles, whose neighbours share keys in its L2
+  const int total = a.tiles * a.hk * a.parts, per = (total + 7) >> 3;
+  const int pid = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || pid >= total) return;
+  const int part = __builtin_amdgcn_readfirstlane(pid % a.parts), id = pid / a.parts;
+  Block b;
+  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b)) return;
+  const int k0 = part * a.part_keys, k1 = b.end < k0 + a.part_keys || a.parts == 1 ? b.end : k0 + a.part_keys;
+  if (k0 >= k1 && part > 0) return;
+  bf16x8 qf[2][KS];
+  int end[2];
+  load_queries<HD, 2>(a, b, b.first + qt * 32, qf, end, lane);
+  const bool gaps = __builtin_amdgcn_readfirstlane(pages_missing(a, b, k0, k1));
+  // tiles of this range: whole ones from t0 on, then those with a border up to t1; of two key groups each has half of either
+  const int t0 = k0 / 64, t1 = (k1 + 63) / 64;
+  int whole = gaps ? 0 : (b.whole < k1 ? b.whole : k1) / 64 - t0;
+  if (whole < KG) whole = 0;
+  const int n_border = t1 - t0 - whole;
+  const int nw = KG == 2 ? (whole + 1) / 2 : whole, nb = KG == 2 ? (n_border + 1) / 2 : n_border;   // trip counts for everyone
+  const int cw = kg ? whole - nw : nw, cb = kg ? n_border - nb : nb;
+  const int w0 = t0 + (kg ? nw : 0), b0 = t0 + whole + (kg ? nb : 0);
+  const uint32_t kst = lds_address(smem) + kg * 2 * NS * TILE, vst = kst + NS * TILE;
+  uint32_t klane = k_lane<HD>(lane), vlane = v_lane<HD>(lane);
+  const int64_t to_values = (int64_t)a.hk << a.page_shift;
+  Carry<HD, 64, QG, CODES> ck, cv;
+
+  bf16x8 kf[2][4], vf[2][4];                 // operands two steps of the head dim, two groups of four values' tiles ahead
+  f32x4 o[DT][2], sc[2][4];
+  uint4 pf[2][2];
+  Soft z[2];
+  auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      z[t] = Soft{-INFINITY, 0.f};
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  // LDS traffic of this wavefront is done before the barrier, and none of what follows is moved ahead of it
+  auto turn = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // tiles past the range: its first one again, never used
+  auto key_of_tile = [&](int j) __attribute__((always_inline)) { return (w0 + (j < cw ? j : 0)) * 64; };
+  auto load_k = [&](int j) __attribute__((always_inline)) { ck.load(a, b, key_of_tile(j), 0, qt, lane); };
+  auto load_v = [&](int j) __attribute__((always_inline)) { cv.load(a, b, key_of_tile(j), to_values, qt, lane); };
+  auto store_k = [&](int j) __attribute__((always_inline)) { ck.template store<false>(kst + (j % NS) * TILE, qt, lane); };
+  auto store_v = [&](int j) __attribute__((always_inline)) { cv.template store<true>(vst + (j % NS) * TILE, qt, lane); };
+  // keys of tile j at channels ks * 32 ..; the g-th four of the values' tiles (32-key half f / DT, channels f % DT * 16 ..)
+  auto read_keys = [&](int j, auto ks_) __attribute__((always_inline)) {
+    constexpr int ks = decltype(ks_)::value;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) kf[ks & 1][kt] = read_k<HD>(kst + (j % NS) * TILE, klane, kt, ks);
+  };
+  auto read_values = [&](int j, auto g_) __attribute__((always_inline)) {
+    constexpr int g = decltype(g_)::value;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vf[g & 1][i] = read_v<HD>(vst + (j % NS) * TILE, vlane, (g * 4 + i) / DT, (g * 4 + i) % DT);
+  };
+  auto score_step = [&](auto ks_) __attribute__((always_inline)) {
+    constexpr int ks = decltype(ks_)::value;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) sc[t][kt] = mfma(kf[ks & 1][kt], qf[t][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[t][kt]);
+  };
+  auto sum_step = [&](auto g_) __attribute__((always_inline)) {
+    constexpr int g = decltype(g_)::value;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) o[(g * 4 + i) % DT][t] = mfma(vf[g & 1][i], __builtin_bit_cast(bf16x8, pf[t][(g * 4 + i) / DT]), o[(g * 4 + i) % DT][t]);
+  };
+  typedef std::integral_constant<int, 0> I0;
+  typedef std::integral_constant<int, 1> I1;
+  float ref[2];
+  auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) weigh<4>(sc[t], a.scale, ref[t], z[t].l, pf[t]);
+  };
+
+  clear();
+  int done = 0;                              // whole tiles that are in the sums
+  if (nw > 0) {
+    // tiles 0 and 1 of either, and keys of tile 2, one behind the other; then the first scores, their maximum, their weights
+    load_k(0); load_v(0);
+    store_k(0); store_v(0);
+    load_k(1); load_v(1);
+    store_k(1); store_v(1);
+    load_k(2); load_v(2);
+    turn();
+    static_for<KS>([&](auto k_) __attribute__((always_inline)) { read_keys(0, k_); score_step(k_); });
+#pragma unroll
+    for (int t = 0; t < 2; ++t) z[t].m = ref[t] = maximum<4>(sc[t], 2) * a.scale;
+    weights();
+    read_keys(1, I0{}); read_keys(1, I1{});
+    turn();
+    store_k(2);
+    load_k(3);
+    turn();
+    if (wave >= 4) turn();                   // the second half starts half a turn later
+    for (int j = 0; j < nw - 1; ++j) {
+      if (KG == 2 && j >= cw - 1) {          // this key group is a tile shorter: it only keeps step
+        turn();
+        turn();
+        continue;
+      }
+      asm volatile("" : "+v"(klane), "+v"(vlane));   // a dozen addresses made of them each time, not kept in registers that the loop has none of
+      __builtin_amdgcn_s_setprio(1);
+      static_for<KS>([&](auto k_) __attribute__((always_inline)) {
+        constexpr int ks = decltype(k_)::value;
+        score_step(k_);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (ks + 2 < KS) read_keys(j + 1, std::integral_constant<int, ks + 2>{});
+        else read_values(j, std::integral_constant<int, ks + 2 - KS>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      static_for<KS>([&](auto g_) __attribute__((always_inline)) {
+        constexpr int g = decltype(g_)::value;
+        sum_step(g_);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (g + 2 < KS) read_values(j, std::integral_constant<int, g + 2>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      __builtin_amdgcn_s_setprio(0);
+      turn();
+      // the other half multiplies
+      read_keys(j + 2, I0{}); read_keys(j + 2, I1{});
+      __builtin_amdgcn_sched_barrier(0);
+      store_k(j + 3);
+      store_v(j + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      load_k(j + 4);
+      load_v(j + 3);
+      __builtin_amdgcn_sched_barrier(0);
+      weights();
+      turn();
+    }
+    // the last tile's weighted sum
+    static_for<KS>([&](auto g_) __attribute__((always_inline)) { read_values(cw - 1, g_); sum_step(g_); });
+    if (wave < 4) turn();                    // the halves meet again
+    done = whole;
+    const float l0 = over_lanes(z[0].l), l1 = over_lanes(z[1].l);
+    if (__syncthreads_or(!(l0 <= 0x1p100f) || !(l1 <= 0x1p100f))) {
+      clear();
+      done = 0;
+    }
+  }
+  // tile by tile: what is left, or everything once more
+  const int again = done ? 0 : nw;
+  for (int j = 0; j < again + nb; ++j) {
+    const bool mine = j < again ? j < cw : j - again < cb;
+    const int tile = j < again ? w0 + j : b0 + j - again;
+    if (mine) {
+      ck.load(a, b, tile * 64, 0, qt, lane);
+      cv.load(a, b, tile * 64, to_values, qt, lane);
+    }
+    __syncthreads();
+    if (mine) { ck.template store<false>(kst, qt, lane); cv.template store<true>(vst, qt, lane); }
+    __syncthreads();
+    if (mine) step<HD, 4, 2>(a, b, kst, vst, qf, tile * 64, j >= again, end, gaps, z, o, lane);
+  }
+  float l[2] = {over_lanes(z[0].l), over_lanes(z[1].l)};
+  __syncthreads();
+  if constexpr (KG == 2) {
+    // the two key groups meet in LDS: group 1 publishes m, l, O^T, and group 0 goes on with both
+    float4* const xch = (float4*)smem + (size_t)qt * (2 * DT + 1) * 64 + lane;     // [qt][2 * DT + 1][64 lanes]
+    if (kg == 1) {
+      xch[0] = make_float4(z[0].m, z[1].m, l[0], l[1]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) xch[(1 + 2 * d + t) * 64] = make_float4(o[d][t][0], o[d][t][1], o[d][t][2], o[d][t][3]);
+    }
+    __syncthreads();
+    if (kg == 1) return;
+    const float4 ml = xch[0];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float m1 = t ? ml.y : ml.x, l1 = t ? ml.w : ml.z, m = fmaxf(z[t].m, m1), to = m == -INFINITY ? 0.f : m;
+      const float f0 = __builtin_amdgcn_exp2f(z[t].m - to), f1 = __builtin_amdgcn_exp2f(m1 - to);
+      z[t].m = m;
+      l[t] = l[t] * f0 + l1 * f1;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const float4 v = xch[(1 + 2 * d + t) * 64];
+        o[d][t] = o[d][t] * f0 + f32x4{v.x, v.y, v.z, v.w} * f1;
+      }
+    }
+  }
+  if (a.parts > 1) {
+    float* const ps = a.partial + (size_t)pid * (QB * (2 + HD));
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int row = qt * 32 + t * 16 + lr;
+      if (b.first + row >= b.rows) continue;
+      if (lg == 0) { ps[row] = z[t].m; ps[QB + row] = l[t]; }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) *(f32x4*)(ps + 2 * QB + row * HD + d * 16 + lg * 4) = o[d][t];
+    }
+  } else {
+    // a lane holds 4 consecutive channels of a row per accumulator tile.  The 32 x HD tile of this wavefront goes through LDS (a wavefront
+    // only touches its own rows, and LDS serves a wavefront's accesses in order) so that global memory sees whole rows, 16 bytes
+    // per lane.  8-byte units are exchanged by the row.
+    constexpr int UPR = HD / 4, CPR = HD / 8, RPI = 64 / CPR;      // units, 16-byte chunks per row; rows per read
+    constexpr int STG0 = KG == 2 ? QG * (2 * DT + 1) * 64 : 0;     // behind the exchange area
+    uint2* const stg = (uint2*)(smem + STG0) + qt * 32 * UPR;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float inv = inverse(l[t]);
+      const int row = t * 16 + lr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        stg[row * UPR + ((d * 4 + lg) ^ (row & (UPR - 1)))] = make_uint2(pack_bf16x2(o[d][t][0] * inv, o[d][t][1] * inv), pack_bf16x2(o[d][t][2] * inv, o[d][t][3] * inv));
+    }
+    const uint4* const stg16 = (const uint4*)stg;
+#pragma unroll
+    for (int it = 0; it < 32 / RPI; ++it) {
+      const int row = it * RPI + lane / CPR, p = lane % CPR;
+      uint4 dv = stg16[row * CPR + p];
+      // units 2p and 2p+1 of the exchanged row are the halves of chunk p ^ (exchange >> 1), the other way round for odd rows
+      if (row & 1) dv = make_uint4(dv.z, dv.w, dv.x, dv.y);
+      const int c = p ^ ((row & (UPR - 1)) >> 1), r = b.first + qt * 32 + row;
+      if (r < b.rows) *(uint4*)((bf16_t*)a.out + row_at(a, b, r, a.o_ts, a.o_hs) + c * 8) = dv;
+    }
+  }
+}
+
+// What a call takes: rows per block, and ranges that a block's keys are cut into
+struct Route { int qb, parts, part_keys; int64_t tiles, tiles_of_seq; };
+Route route(const PagedArgs& a) {
+  Route r{};
+  const int64_t rows = (int64_t)a.max_q * a.shared;          // of a sequence, at most
+  auto tiles = [&](int qb) {
+    const int64_t each = (rows + qb - 1) / qb, all = a.n_tokens * a.shared / qb + a.n_seqs;
+    return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
+  };
+  r.qb = rows <= 16 ? 16 : rows <= 32 ? 32 : tiles(256) * a.hk >= 128 ? 256 : 128;
+  r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
+  r.tiles = tiles(r.qb);
+  const int64_t blocks = r.tiles * a.hk, keys = a.max_kv;
+  if (r.qb <= 32) {
+    // one range for as many blocks as keep the chip full several times over; none shorter than a trip of the four wavefronts
+    int64_t parts = (2048 + blocks - 1) / blocks;
+    if (parts > (keys + 255) / 256) parts = (keys + 255) / 256;
+    if (parts > 256) parts = 256;
+    if (parts < 1) parts = 1;
+    r.part_keys = (int)(((keys + parts - 1) / parts + 127) / 128 * 128);
+  } else {
+    int64_t parts = 1;
+    const int64_t rest = blocks % 256;
+    if (blocks < 256 && rest > 0) parts = 256 / rest;
+    if (parts > 8) parts = 8;
+    if (parts > keys / 512) parts = keys / 512;
+    if (parts < 1) parts = 1;
+    r.part_keys = (int)(((keys + parts - 1) / parts + 63) / 64 * 64);
+  }
+  r.parts = r.part_keys > 0 ? (int)((keys + r.part_keys - 1) / r.part_keys) : 1;
+  if (r.parts < 1) r.parts = 1;
+  return r;
+}
+
+template <int HD, int NT> void few(const PagedArgs& a, bool codes, hipStream_t st) {
+  const unsigned g = (unsigned)((int64_t)a.tiles * a.hk * a.parts);
+  if (codes) k_paged_few<HD, NT, true><<<g, 256, 0, st>>>(a); else k_paged_few<HD, NT, false><<<g, 256, 0, st>>>(a);
+}
+template <int HD, int KG, bool CODES> void turns_of(const PagedArgs& a, hipStream_t st) {
+  constexpr int tile = 64 * HD * 2, lds = KG == 1 ? 6 * tile : 8 * tile;
+  static std::atomic<uint64_t> done;
+  allow_dynamic_lds((const void*)k_paged_turns<HD, KG, CODES>, lds, done);
+  const int64_t total = (int64_t)a.tiles * a.hk * a.parts;
+  k_paged_turns<HD, KG, CODES><<<(unsigned)((total + 7) / 8 * 8), 512, lds, st>>>(a);
+}
+template <int HD, int KG> void turns(const PagedArgs& a, bool codes, hipStream_t st) {
+  if (codes) turns_of<HD, KG, true>(a, st); else turns_of<HD, KG, false>(a, st);
+}
+template <int HD> void launch(const PagedArgs& a, int qb, bool codes, hipStream_t st) {
+  const unsigned joins = (unsigned)((int64_t)a.tiles * a.hk * qb * (HD / 4) / 256);
+  if (qb == 16) {
+    few<HD, 1>(a, codes, st);
+    if (a.parts > 1) k_paged_join<HD, 16><<<joins, 256, 0, st>>>(a);
+  } else if (qb == 32) {
+    few<HD, 2>(a, codes, st);
+    if (a.parts > 1) k_paged_join<HD, 32><<<joins, 256, 0, st>>>(a);
+  } else if (qb == 128) {
+    turns<HD, 2>(a, codes, st);
+    if (a.parts > 1) k_paged_join<HD, 128><<<joins, 256, 0, st>>>(a);
+  } else {
+    turns<HD, 1>(a, codes, st);
+    if (a.parts > 1) k_paged_join<HD, 256><<<joins, 256, 0, st>>>(a);
+  }
+}
+
+}  // namespace
+
+size_t launch_attn_paged_bf16(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st) {
+  const Route r = route(a);
+  a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys;
+  if (go) { if (head_dim == 128) launch<128>(a, r.qb, codes, st); else launch<64>(a, r.qb, codes, st); }
+  return r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts * ((size_t)r.qb * (2 + head_dim) * sizeof(float)) : 0;
+}

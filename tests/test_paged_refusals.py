@@ -70,7 +70,7 @@ def test_bad_caches(bad):
     refused(read(c=cache(**bad)), "dp_kv_read")
     refused(qkv(c=cache(**bad)), "dp_kv_write_qkv")
     refused(attend(c=cache(**bad)), "dp_attn_paged")
-    assert L.dp_attn_paged_workspace_bytes(cache(**bad), attn()) == 0
+    assert L.dp_attn_paged_workspace_bytes(cache(**bad), attn(), 7) == 0
 
 
 @pytest.mark.parametrize("bad", BAD_NORM, ids=str)
@@ -82,7 +82,7 @@ def test_bad_norms(bad):
 @pytest.mark.parametrize("bad", BAD_ATTN, ids=str)
 def test_bad_attention_configs(bad):
     refused(attend(a=attn(**bad)), "dp_attn_paged")
-    assert L.dp_attn_paged_workspace_bytes(cache(), attn(**bad)) == 0
+    assert L.dp_attn_paged_workspace_bytes(cache(), attn(**bad), 7) == 0
 
 
 @pytest.mark.parametrize("bad", BAD_ROWS, ids=str)
@@ -127,6 +127,16 @@ def test_null_pointers_and_counts():
         refused(qkv(slot=slot), "dp_kv_write_qkv")
     for kw in (dict(start=None), dict(lens=None), dict(table=None), dict(start=AT + 2), dict(lens=AT + 1), dict(table=AT + 3)):
         refused(attend(**kw), "dp_attn_paged")
+
+
+def test_workspaces():
+    big = attn(q_heads=4, n_seqs=1, max_q=1, max_kv=4000, table_width=250)
+    need = L.dp_attn_paged_workspace_bytes(cache(), big, 1)
+    assert need > 0 and L.dp_attn_paged_workspace_bytes(cache(), big, 0) == 0
+    for work, nbytes in ((None, need), (AT, need - 1), (AT, 0)):
+        assert attend(a=big, n=1, work=work, nbytes=nbytes) == B.DP_ENOMEM and "workspace" in B.last_error()
+    refused(attend(a=big, n=1, work=AT + 128, nbytes=need), "dp_attn_paged")
+    refused(attend(a=attn(q_heads=512), n=1 << 22, q=rows(512), out=rows(512)), "dp_attn_paged")
 
 
 def test_nothing_to_do():
