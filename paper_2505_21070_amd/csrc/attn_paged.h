@@ -137,5 +137,122 @@ __device__ __forceinline__ bool pages_missing(const PagedArgs& a, const Block& k
   return __syncthreads_or(bad);
 }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// The softmax of 16 rows (one a lane & 15; the four lanes of a row hold keys of their own): reference and sums so far.  m is in units of
+// log2, after the scale; -inf as long as there is no score above it.
+struct Soft { float m, l; };
+
+template <int KT> __device__ __forceinline__ float maximum(const f32x4 (&sc)[KT], int kt1) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+    if (kt < kt1)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[kt][r]);
+  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+  return fmaxf(mx, __shfl_xor(mx, 32, 64));
+}
+// raises the reference to the tile's maximum: returns the factor of what was summed so far, and the reference to weigh with
+__device__ __forceinline__ float raise(Soft& z, float top, float& ref) {
+  const float m = fmaxf(z.m, top);
+  ref = m == -INFINITY ? 0.f : m;
+  const float alpha = __builtin_amdgcn_exp2f(z.m - ref);     // 0 while there was no reference
+  z.m = m;
+  z.l *= alpha;
+  return alpha;
+}
+// Of a lane's four keys in each tile of 16 from key0 on: bit kt where their page does not exist (pages hold whole groups of 16)
+template <int KT> __device__ __forceinline__ uint32_t missing(const PagedArgs& a, const Block& b, int key0, int lane) {
+  uint32_t gone = 0;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const int key = key0 + kt * 16 + (lane >> 4) * 4;
+    gone |= (page_exists(a, b, key < b.end ? key : b.end - 1) ? 0u : 1u) << kt;
+  }
+  return gone;
+}
+// -inf for the keys that a row does not see: key0 is the tile's first, end the row's border
+template <int KT> __device__ __forceinline__ void hide(f32x4 (&sc)[KT], int key0, int end, uint32_t gone, int lane) {
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sc[kt][r] = (key0 + kt * 16 + (lane >> 4) * 4 + r >= end) | ((gone >> kt) & 1) ? -INFINITY : sc[kt][r];
+}
+// 1 / l, or 0 for a row without a weight; NaN stays
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float over_lanes(float v) { v += __shfl_xor(v, 16, 64); return v + __shfl_xor(v, 32, 64); }
+// four channels of an output row
+__device__ __forceinline__ void store_four(float* p, f32x4 v) { *(f32x4*)p = v; }
+__device__ __forceinline__ void store_four(bf16_t* p, f32x4 v) { *(uint2*)p = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
+
+// The end of a block whose four wavefronts have the same NT * 16 rows and keys of their own: joined 16 rows at a time, every wavefront's m and l and its
+// O^T by rows, added up in wavefront order at the common reference.  smem: 4 * 16 * (2 + HD + 4) floats, which every wavefront is done with.
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, float* smem, const Soft (&z)[NT], const f32x4 (&o)[HD / 16][NT], int wave, int lane) {
+  constexpr int OS = HD + 4, QB = NT * 16;
+  float* const ml = smem;                                    // [4][16][2]
+  float* const os = ml + 4 * 16 * 2;                         // [4][16][OS]
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (b.first + t * 16 >= b.rows) break;
+    __syncthreads();
+    const float lsum = over_lanes(z[t].l);
+    if (lane < 16) { ml[(wave * 16 + lane) * 2] = z[t].m; ml[(wave * 16 + lane) * 2 + 1] = lsum; }
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) *(f32x4*)(os + (wave * 16 + (lane & 15)) * OS + d * 16 + (lane >> 4) * 4) = o[d][t];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * (HD / 4); i += 256) {
+      const int r = i / (HD / 4), c = i % (HD / 4) * 4, row = t * 16 + r;
+      if (b.first + row >= b.rows) continue;
+      float m = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      float l = 0.f;
+      f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - ref);
+        l += ml[(w * 16 + r) * 2 + 1] * f;
+        v += *(const f32x4*)(os + (w * 16 + r) * OS + c) * f;
+      }
+      if (a.parts == 1) {
+        store_four((T*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c, v * inverse(l));
+      } else {
+        float* const ps = a.partial + (size_t)blockIdx.x * (QB * (2 + HD));
+        if (c == 0) { ps[row] = m; ps[QB + row] = l; }
+        *(f32x4*)(ps + 2 * QB + row * HD + c) = v;
+      }
+    }
+  }
+}
+
+// Joins the key ranges of a block's rows: a lane has four channels of a row.
+template <typename T, int HD, int QB>
+__global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
+  constexpr int LANES = HD / 4, ROWS = 256 / LANES;
+  const int id = blockIdx.x / (QB / ROWS), row = blockIdx.x % (QB / ROWS) * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+  Block b;
+  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b) || b.first + row >= b.rows) return;
+  int parts = (int)(((int64_t)b.end + a.part_keys - 1) / a.part_keys);
+  if (parts < 1) parts = 1;                                  // the first range is always there
+  const float* const ps = a.partial + (size_t)id * a.parts * (QB * (2 + HD));
+  float m = -INFINITY;
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, ps[(size_t)i * (QB * (2 + HD)) + row]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  f32x4 v{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < parts; ++i) {
+    const float* const p = ps + (size_t)i * (QB * (2 + HD));
+    const float f = __builtin_amdgcn_exp2f(p[row] - ref);
+    l += p[QB + row] * f;
+    v += *(const f32x4*)(p + 2 * QB + row * HD + c) * f;
+  }
+  const float inv = inverse(l);
+  store_four((T*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c, v * inv);
+}
+
 // ---- the launches; each fills in the launch fields of a and returns the bytes of partial results it needs (partial == null: only that)
 size_t launch_attn_paged_bf16(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st);
+size_t launch_attn_paged_f32(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st);

@@ -1,60 +1,10 @@
-// Attention of a chunk of new tokens over the pages of a key/value cache: the C entry, and the fp32 kernel (bf16: attn_paged_bf16.hip).
-//
-// fp32: one wavefront per new token and query head, 64 keys at a time (a lane owns a key's score), online softmax, the weighted sum over the
-// values with a lane owning channels.
+// Attention of a chunk of new tokens over the pages of a key/value cache: the C entry (kernels:
+// attn_paged_bf16.hip, attn_paged_f32.hip).
 #include <math.h>
 
 #include "attn_paged.h"
 
 namespace {
-
-template <typename T, int HD, bool CODES>
-__global__ __launch_bounds__(64) void k_attn_paged_plain(const PagedArgs a) {
-  __shared__ float sq[HD];
-  const int lane = threadIdx.x, b = blockIdx.z, head = blockIdx.y, i = blockIdx.x;
-  const Seq s = sequence(a, b);
-  if (i >= s.rows) return;
-  const int keys = held_keys(a, s.keys), hk = head / a.shared;
-  int end = seen_keys(a, i, s.n, s.keys);
-  end = end < keys ? end : keys;
-  const T* const q = (const T*)a.q + (int64_t)(s.row0 + i) * a.q_ts + head * a.q_hs;
-  for (int c = lane; c < HD; c += 64) sq[c] = Elem<T>::ld(q + c);
-  __syncthreads();
-  auto value = [&](int64_t row, int c) __attribute__((always_inline)) {
-    if constexpr (CODES) return fp8x4_to_f32(((const uint8_t*)a.data)[row * HD + c], __uint_as_float((uint32_t)a.scales[row] << 23)).x;
-    else return Elem<T>::ld((const T*)a.data + row * HD + c);
-  };
-  float m = -INFINITY, l = 0.f, o[HD / 64] = {};
-  for (int k0 = 0; k0 < end; k0 += 64) {
-    const int key = k0 + lane;
-    int64_t row = -1;
-    if (key < end) {
-      const int page = a.table[(int64_t)b * a.table_width + (key >> a.page_shift)];
-      if (page >= 0 && page < a.n_pages) row = ((((int64_t)page * 2 * a.hk) + hk) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
-    }
-    float score = -INFINITY;
-    if (row >= 0) {
-      score = 0.f;
-      for (int c = 0; c < HD; ++c) score = fmaf(sq[c], value(row, c), score);
-      score *= a.scale;
-    }
-    float top = score;
-    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-    const float now = fmaxf(m, top), ref = now == -INFINITY ? 0.f : now;
-    const float alpha = exp2f(m - ref), w = exp2f(score - ref);
-    m = now;
-    l = l * alpha + wave_sum(w);
-    for (int c = 0; c < HD / 64; ++c) o[c] *= alpha;
-    for (int j = 0; j < 64; ++j) {
-      const float wj = __shfl(w, j, 64);
-      const int64_t rj = __shfl((long long)row, j, 64);
-      if (rj < 0 || wj == 0.f) continue;
-      for (int c = 0; c < HD / 64; ++c) o[c] = fmaf(wj, value(rj + ((int64_t)a.hk << a.page_shift), c * 64 + lane), o[c]);
-    }
-  }
-  T* const out = (T*)a.out + (int64_t)(s.row0 + i) * a.o_ts + head * a.o_hs;
-  for (int c = 0; c < HD / 64; ++c) Elem<T>::st(out + c * 64 + lane, l > 0.f || l != l ? o[c] / l : 0.f);
-}
 
 const char* why_not_attn(const dp_kv_cache* c, const dp_attn_config* cfg) {
   if (const char* why = why_not_cache(c)) return why;
@@ -94,7 +44,7 @@ extern "C" size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* c, const dp_a
   if (!why) why = why_not_tokens(n_tokens, cfg);
   if (why) { refuse("dp_attn_paged_workspace_bytes", why); return 0; }
   if (n_tokens == 0 || cfg->n_seqs == 0 || cfg->max_q == 0) return 0;
-  return c->dtype == DP_BF16 ? launch_attn_paged_bf16(arguments(c, cfg, n_tokens), c->head_dim, c->format == DP_KV_FP8, false, nullptr) : 0;
+  return (c->dtype == DP_BF16 ? launch_attn_paged_bf16 : launch_attn_paged_f32)(arguments(c, cfg, n_tokens), c->head_dim, c->format == DP_KV_FP8, false, nullptr);
 }
 
 extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, const dp_rows* q, int64_t n_tokens, const int32_t* q_start,
@@ -114,23 +64,14 @@ extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, co
   a.q_start = q_start; a.kv_len = kv_len; a.table = page_table;
   const hipStream_t st = (hipStream_t)stream;
   const bool codes = c->format == DP_KV_FP8;
-  if (c->dtype == DP_BF16) {
-    const size_t need = launch_attn_paged_bf16(a, c->head_dim, codes, false, nullptr);
-    if (need > 0) {
-      REFUSE_IF((uintptr_t)workspace & 255 ? "the workspace must be 256-byte aligned" : nullptr);
-      if (!workspace || workspace_bytes < need) return dp_set_error(DP_ENOMEM, "dp_attn_paged: workspace too small");
-    }
+  auto* const launch = c->dtype == DP_BF16 ? launch_attn_paged_bf16 : launch_attn_paged_f32;
+  if (const size_t need = launch(a, c->head_dim, codes, false, nullptr)) {
+    REFUSE_IF((uintptr_t)workspace & 255 ? "the workspace must be 256-byte aligned" : nullptr);
+    if (!workspace || workspace_bytes < need) return dp_set_error(DP_ENOMEM, "dp_attn_paged: workspace too small");
     a.partial = (float*)workspace;
   }
   (void)hipGetLastError();
-  if (c->dtype == DP_BF16) {
-    launch_attn_paged_bf16(a, c->head_dim, codes, true, st);
-  } else {
-    const dim3 grid((unsigned)a.max_q, (unsigned)cfg->q_heads, (unsigned)cfg->n_seqs);
-#define PLAIN(HD) do { if (codes) k_attn_paged_plain<float, HD, true><<<grid, 64, 0, st>>>(a); else k_attn_paged_plain<float, HD, false><<<grid, 64, 0, st>>>(a); } while (0)
-    if (c->head_dim == 128) PLAIN(128); else PLAIN(64);
-#undef PLAIN
-  }
+  launch(a, c->head_dim, codes, true, st);
   if (hipGetLastError() != hipSuccess) return dp_set_error(DP_EHIP, "dp_attn_paged: the launch failed");
   return DP_OK;
 }

@@ -22,7 +22,6 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float add_pk(uint32_t pk, float acc) {          // acc + lo + hi of a packed bf16 pair
@@ -123,10 +122,6 @@ template <int HD> __device__ __forceinline__ bf16x8 read_v(uint32_t tile, uint32
   return __builtin_shufflevector(lds_get_transposed(at), lds_get_transposed(at + 16 * HD * 2), 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// The softmax of 16 rows (one a lane & 15; the four lanes of a row hold keys of their own): reference and sums so far.  m is in units of
-// log2, after the scale; -inf as long as there is no score above it.
-struct Soft { float m, l; };
-
 // Weights of KT tiles of 16 keys of a row, from scores in sc, packed for the second product; l grows by the rounded weights.  The reference is m
 // (finite, or 0 while there is none).
 template <int KT> __device__ __forceinline__ void weigh(const f32x4 (&sc)[KT], float scale, float ref, float& l, uint4 (&pf)[KT / 2]) {
@@ -141,42 +136,6 @@ template <int KT> __device__ __forceinline__ void weigh(const f32x4 (&sc)[KT], f
     }
     pf[s] = make_uint4(w[0], w[1], w[2], w[3]);
   }
-}
-template <int KT> __device__ __forceinline__ float maximum(const f32x4 (&sc)[KT], int kt1) {
-  float mx = -INFINITY;
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-    if (kt < kt1)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[kt][r]);
-  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-  return fmaxf(mx, __shfl_xor(mx, 32, 64));
-}
-// raises the reference to the tile's maximum: returns the factor of what was summed so far, and the reference to weigh with
-__device__ __forceinline__ float raise(Soft& z, float top, float& ref) {
-  const float m = fmaxf(z.m, top);
-  ref = m == -INFINITY ? 0.f : m;
-  const float alpha = __builtin_amdgcn_exp2f(z.m - ref);     // 0 while there was no reference
-  z.m = m;
-  z.l *= alpha;
-  return alpha;
-}
-// Of a lane's four keys in each tile of 16 from key0 on: bit kt where their page does not exist (pages hold whole groups of 16)
-template <int KT> __device__ __forceinline__ uint32_t missing(const PagedArgs& a, const Block& b, int key0, int lane) {
-  uint32_t gone = 0;
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt) {
-    const int key = key0 + kt * 16 + (lane >> 4) * 4;
-    gone |= (page_exists(a, b, key < b.end ? key : b.end - 1) ? 0u : 1u) << kt;
-  }
-  return gone;
-}
-// -inf for the keys that a row does not see: key0 is the tile's first, end the row's border
-template <int KT> __device__ __forceinline__ void hide(f32x4 (&sc)[KT], int key0, int end, uint32_t gone, int lane) {
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) sc[kt][r] = (key0 + kt * 16 + (lane >> 4) * 4 + r >= end) | ((gone >> kt) & 1) ? -INFINITY : sc[kt][r];
 }
 // bf16 pairs: where the exponent is all ones (infinity or NaN)
 __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
@@ -276,10 +235,6 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, uint32_
     }
   }
 }
-// 1 / l, or 0 for a row without a weight; NaN stays
-__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
-__device__ __forceinline__ float over_lanes(float v) { v += __shfl_xor(v, 16, 64); return v + __shfl_xor(v, 32, 64); }
-
 template <int HD, int NT>
 __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b, int row0, bf16x8 (&qf)[NT][HD / 32], int (&end)[NT], int lane) {
 #pragma unroll
@@ -299,6 +254,7 @@ template <int HD, int NT, bool CODES>
 __global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
   constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
   __shared__ uint4 smem[4 * 2 * TILE];
+  static_assert(sizeof(smem) >= sizeof(float) * 4 * 16 * (2 + HD + 4), "join_waves");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = __builtin_amdgcn_readfirstlane(blockIdx.x % a.parts), id = blockIdx.x / a.parts;
   Block b;
@@ -308,7 +264,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
   bf16x8 qf[NT][HD / 32];
   int end[NT];
   load_queries<HD, NT>(a, b, b.first, qf, end, lane);
-  const bool gaps = __builtin_amdgcn_readfirstlane(pages_missing(a, b, k0, k1));
+  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
   const uint32_t kt = lds_address(smem) + wave * 2 * TILE * 16, vt = kt + TILE * 16;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
   Soft z[NT];
@@ -328,70 +284,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
     if (key + 128 < k1) { ck.load(a, b, key + 128, 0, 0, lane); cv.load(a, b, key + 128, to_values, 0, lane); }
     step<HD, KT, NT>(a, b, kt, vt, qf, key, key + 32 > b.whole || gaps, end, gaps, z, o, lane);
   }
-  // join, 16 rows at a time: every wavefront's m and l and its O^T by rows, added up at the common reference
-  constexpr int OS = HD + 4;
-  float* const ml = (float*)smem;                            // [4][16][2]
-  float* const os = ml + 4 * 16 * 2;                         // [4][16][OS]
-  static_assert((4 * 16 * 2 + 4 * 16 * OS) * 4 <= (int)sizeof(smem), "fits the tiles' place");
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (b.first + t * 16 >= b.rows) break;
-    __syncthreads();
-    const float lsum = over_lanes(z[t].l);
-    if (lane < 16) { ml[(wave * 16 + lane) * 2] = z[t].m; ml[(wave * 16 + lane) * 2 + 1] = lsum; }
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) *(f32x4*)(os + (wave * 16 + (lane & 15)) * OS + d * 16 + (lane >> 4) * 4) = o[d][t];
-    __syncthreads();
-    for (int i = threadIdx.x; i < 16 * (HD / 4); i += 256) {
-      const int r = i / (HD / 4), c = i % (HD / 4) * 4, row = t * 16 + r;
-      float m = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
-      const float ref = m == -INFINITY ? 0.f : m;
-      float l = 0.f;
-      f32x4 v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - ref);
-        l += ml[(w * 16 + r) * 2 + 1] * f;
-        v += *(const f32x4*)(os + (w * 16 + r) * OS + c) * f;
-      }
-      if (b.first + row >= b.rows) continue;
-      if (a.parts == 1) {
-        const float inv = inverse(l);
-        *(uint2*)((bf16_t*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c) = make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
-      } else {
-        float* const ps = a.partial + (size_t)blockIdx.x * (QB * (2 + HD));
-        if (c == 0) { ps[row] = m; ps[QB + row] = l; }
-        *(f32x4*)(ps + 2 * QB + row * HD + c) = v;
-      }
-    }
-  }
-}
-
-// Joins the key ranges of a block's rows: a lane has four channels of a row.
-template <int HD, int QB>
-__global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
-  constexpr int LANES = HD / 4, ROWS = 256 / LANES;
-  const int id = blockIdx.x / (QB / ROWS), row = blockIdx.x % (QB / ROWS) * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
-  Block b;
-  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b) || b.first + row >= b.rows) return;
-  int parts = (int)(((int64_t)b.end + a.part_keys - 1) / a.part_keys);
-  if (parts < 1) parts = 1;                                  // the first range is always there
-  const float* const ps = a.partial + (size_t)id * a.parts * (QB * (2 + HD));
-  float m = -INFINITY;
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, ps[(size_t)i * (QB * (2 + HD)) + row]);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  f32x4 v{0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < parts; ++i) {
-    const float* const p = ps + (size_t)i * (QB * (2 + HD));
-    const float f = __builtin_amdgcn_exp2f(p[row] - ref);
-    l += p[QB + row] * f;
-    v += *(const f32x4*)(p + 2 * QB + row * HD + c) * f;
-  }
-  const float inv = inverse(l);
-  *(uint2*)((bf16_t*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c) = make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
+  join_waves<bf16_t, HD, NT>(a, b, (float*)smem, z, o, wave, lane);
 }
 
 // Many rows: eight wavefronts of 32 rows (two columns of 16), key tiles of 64.  KG = 1: all share every tile, a block has 256 rows and its halves are the
@@ -423,7 +316,7 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
   bf16x8 qf[2][KS];
   int end[2];
   load_queries<HD, 2>(a, b, b.first + qt * 32, qf, end, lane);
-  const bool gaps = __builtin_amdgcn_readfirstlane(pages_missing(a, b, k0, k1));
+  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
   // tiles of this range: whole ones from t0 on, then those with a border up to t1; of two key groups each has half of either
   const int t0 = k0 / 64, t1 = (k1 + 63) / 64;
   int whole = gaps ? 0 : (b.whole < k1 ? b.whole : k1) / 64 - t0;
@@ -652,26 +545,31 @@ Route route(const PagedArgs& a) {
     const int64_t each = (rows + qb - 1) / qb, all = a.n_tokens * a.shared / qb + a.n_seqs;
     return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
   };
-  r.qb = rows <= 16 ? 16 : rows <= 32 ? 32 : tiles(256) * a.hk >= 128 ? 256 : 128;
-  r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
-  r.tiles = tiles(r.qb);
-  const int64_t blocks = r.tiles * a.hk, keys = a.max_kv;
-  if (r.qb <= 32) {
-    // one range for as many blocks as keep the chip full several times over; none shorter than a trip of the four wavefronts
+  const int64_t keys = a.max_kv;
+  if (rows <= 32) {
+    r.qb = rows <= 16 ? 16 : 32;
+    r.tiles = tiles(r.qb);
+    const int64_t blocks = r.tiles * a.hk;
+    // one range for as many blocks as keep the chip full several times over; none shorter than two trips of the four wavefronts
     int64_t parts = (2048 + blocks - 1) / blocks;
     if (parts > (keys + 255) / 256) parts = (keys + 255) / 256;
     if (parts > 256) parts = 256;
     if (parts < 1) parts = 1;
     r.part_keys = (int)(((keys + parts - 1) / parts + 127) / 128 * 128);
   } else {
-    int64_t parts = 1;
-    const int64_t rest = blocks % 256;
-    if (blocks < 256 && rest > 0) parts = 256 / rest;
-    if (parts > 8) parts = 8;
-    if (parts > keys / 512) parts = keys / 512;
-    if (parts < 1) parts = 1;
-    r.part_keys = (int)(((keys + parts - 1) / parts + 63) / 64 * 64);
+    // Blocks of either shape, one to a CU, run in rounds of 256; a step of 64 keys x 256 rows, or 2 x 64 keys x 128 rows, is 1.7 us at heads of 128, and what a
+    // block does around its steps about 5 of them.  Ranges fill the last round, and cost a launch and the traffic of partial results (7 MB a step).
+    int64_t best = INT64_MAX;
+    const int64_t key_tiles = (keys + 63) / 64;
+    for (int qb = 256; qb >= 128; qb -= 128)
+      for (int64_t parts = 1; parts <= 8; ++parts) {
+        const int64_t n = tiles(qb), blocks = n * a.hk * parts, of_part = (key_tiles + parts - 1) / parts;
+        if (parts > 1 && of_part < 8) break;
+        const int64_t cost = ((blocks + 255) / 256) * ((qb == 256 ? of_part : (of_part + 1) / 2) + 5) + (parts > 1 ? 4 + blocks * qb * 520 / 7000000 : 0);
+        if (cost < best) { best = cost; r.qb = qb; r.tiles = n; r.part_keys = (int)(of_part * 64); }
+      }
   }
+  r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
   r.parts = r.part_keys > 0 ? (int)((keys + r.part_keys - 1) / r.part_keys) : 1;
   if (r.parts < 1) r.parts = 1;
   return r;
@@ -695,16 +593,16 @@ template <int HD> void launch(const PagedArgs& a, int qb, bool codes, hipStream_
   const unsigned joins = (unsigned)((int64_t)a.tiles * a.hk * qb * (HD / 4) / 256);
   if (qb == 16) {
     few<HD, 1>(a, codes, st);
-    if (a.parts > 1) k_paged_join<HD, 16><<<joins, 256, 0, st>>>(a);
+    if (a.parts > 1) k_paged_join<bf16_t, HD, 16><<<joins, 256, 0, st>>>(a);
   } else if (qb == 32) {
     few<HD, 2>(a, codes, st);
-    if (a.parts > 1) k_paged_join<HD, 32><<<joins, 256, 0, st>>>(a);
+    if (a.parts > 1) k_paged_join<bf16_t, HD, 32><<<joins, 256, 0, st>>>(a);
   } else if (qb == 128) {
     turns<HD, 2>(a, codes, st);
-    if (a.parts > 1) k_paged_join<HD, 128><<<joins, 256, 0, st>>>(a);
+    if (a.parts > 1) k_paged_join<bf16_t, HD, 128><<<joins, 256, 0, st>>>(a);
   } else {
     turns<HD, 1>(a, codes, st);
-    if (a.parts > 1) k_paged_join<HD, 256><<<joins, 256, 0, st>>>(a);
+    if (a.parts > 1) k_paged_join<bf16_t, HD, 256><<<joins, 256, 0, st>>>(a);
   }
 }
 
