@@ -6,6 +6,7 @@ There is no fallback: if the library has not been built, importing fails.
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -140,20 +141,20 @@ class AttnConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("q_heads", "n_seqs", "max_q", "max_kv", "table_width", "causal_group")] + [("scale", C.c_float)]
 
 
-_ROWS, _CACHE = C.POINTER(KvRows), C.POINTER(KvCacheDesc)
+# structs of these calls are passed as bytes packed anew for each call: a third of the time that filling in ctypes' own takes
+_PACK_ROWS, _PACK_NORM, _PACK_ATTN = struct.Struct("Pqq").pack, struct.Struct("4i2f3P").pack, struct.Struct("6if").pack
 _lib.dp_qk_norm_rope.restype = C.c_int
-_lib.dp_qk_norm_rope.argtypes = [C.POINTER(NormRope), _ROWS, _ROWS, C.c_int64, _ROWS, _ROWS, C.c_void_p]
+_lib.dp_qk_norm_rope.argtypes = [C.c_void_p] * 3 + [C.c_int64] + [C.c_void_p] * 3
 _lib.dp_kv_write.restype = C.c_int
-_lib.dp_kv_write.argtypes = [_CACHE, _ROWS, _ROWS, C.c_void_p, C.c_int64, C.c_void_p]
+_lib.dp_kv_write.argtypes = [C.c_void_p] * 4 + [C.c_int64, C.c_void_p]
 _lib.dp_kv_write_qkv.restype = C.c_int
-_lib.dp_kv_write_qkv.argtypes = [_CACHE, C.POINTER(NormRope), _ROWS, _ROWS, _ROWS, C.c_void_p, C.c_int64, _ROWS, C.c_void_p]
+_lib.dp_kv_write_qkv.argtypes = [C.c_void_p] * 6 + [C.c_int64] + [C.c_void_p] * 2
 _lib.dp_kv_read.restype = C.c_int
-_lib.dp_kv_read.argtypes = [_CACHE, C.c_void_p, C.c_int64, _ROWS, _ROWS, C.c_void_p]
+_lib.dp_kv_read.argtypes = [C.c_void_p] * 2 + [C.c_int64] + [C.c_void_p] * 3
 _lib.dp_attn_paged_workspace_bytes.restype = C.c_size_t
-_lib.dp_attn_paged_workspace_bytes.argtypes = [_CACHE, C.POINTER(AttnConfig), C.c_int64]
+_lib.dp_attn_paged_workspace_bytes.argtypes = [C.c_void_p] * 2 + [C.c_int64]
 _lib.dp_attn_paged.restype = C.c_int
-_lib.dp_attn_paged.argtypes = [_CACHE, C.POINTER(AttnConfig), _ROWS, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, _ROWS, C.c_void_p,
-                               C.c_size_t, C.c_void_p]
+_lib.dp_attn_paged.argtypes = [C.c_void_p] * 3 + [C.c_int64] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
 _lib.dp_stage_free.argtypes = [C.c_void_p]
 _lib.dp_last_error.restype = C.c_char_p
 _lib.dp_last_error.argtypes = []
@@ -410,49 +411,54 @@ def euler_step(x, v, sigma, sigma_next, stream=None):
 _KV_DTYPE = {torch.float32: DP_F32, torch.bfloat16: DP_BF16}
 
 
-def _rows(t, heads, n, like):
-    """t as [n, heads, head_dim] rows of the type and device of `like` = (head_dim, dtype, device)."""
-    assert t.shape == (n, heads, like[0]) and t.dtype == like[1] and t.device == like[2] and (t.stride(2) == 1 or t.numel() == 0), \
-        (tuple(t.shape), t.dtype, t.device, t.stride(), n, heads, like)
-    return KvRows(t.data_ptr(), t.stride(0), t.stride(1))
+def _rows(t, heads, n, d, td, device):
+    """t as [n, heads, d] rows of a type on a device."""
+    assert t.shape == (n, heads, d) and t.dtype == td and t.device == device, (tuple(t.shape), t.dtype, t.device, (n, heads, d), td, device)
+    ts, hs, cs = t.stride()
+    assert cs == 1 or n == 0, t.stride()
+    return _PACK_ROWS(t.data_ptr(), ts, hs)
+
+
+def _current_device():
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
 def _stream_on(device, stream):
     """The stream handle of a call on `device`, which has to be the current one: the library launches there."""
-    assert device.type == "cuda" and device.index == torch.cuda.current_device(), f"tensors on {device}, current device {torch.cuda.current_device()}"
+    assert device.type == "cuda" and device.index == _current_device(), f"tensors on {device}, not on the current device"
     return _stream_handle(stream)
 
 
-def _used_on(stream, *tensors):
-    """Tensors allocated here and used on a stream that is not the current one: their memory waits for that stream when they go."""
+def _new(shape, like, stream, dtype=None):
+    """Memory for a result.  On a stream that is not the current one its memory waits for that stream when it goes."""
+    t = like.new_empty(shape, dtype=dtype)
     if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+        t.record_stream(stream)
+    return t
 
 
-def _norm_rope(q, k, gq, gk, pos, rope_theta, eps):
-    n, hq, d = q.shape
-    hk, dev, td = k.shape[1], q.device, q.dtype
+def _norm_rope(q, hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps):
     assert td in _KV_DTYPE and gq.shape == gk.shape == (d,) and gq.dtype == gk.dtype == td and gq.is_contiguous() and gk.is_contiguous()
     assert gq.device == gk.device == pos.device == dev and pos.shape == (n, 3) and pos.dtype == torch.int32 and pos.is_contiguous()
-    return NormRope(hq, hk, d, _KV_DTYPE[td], rope_theta, eps, gq.data_ptr(), gk.data_ptr(), pos.data_ptr())
+    return _PACK_NORM(hq, hk, d, _KV_DTYPE[td], rope_theta, eps, gq.data_ptr(), gk.data_ptr(), pos.data_ptr())
 
 
 def qk_norm_rope(q, k, gq, gk, pos, rope_theta=1e4, eps=1e-6, q_out=None, k_out=None, stream=None):
     """RMSNorm of each head of q [n, q_heads, head_dim] and k [n, kv_heads, head_dim] with gains gq, gk [head_dim], then the 3D rotation
     at pos (int32 [n, 3]: frame, row, column), in one pass.  q and k may be views (of a fused product's output); q_out / k_out may be q / k themselves.
     Returns (q_out, k_out)."""
-    cfg = _norm_rope(q, k, gq, gk, pos, rope_theta, eps)
-    n, like, st = q.shape[0], (q.shape[2], q.dtype, q.device), _stream_on(q.device, stream)
+    (n, hq, d), hk, td, dev = q.shape, k.shape[1], q.dtype, q.device
+    st = _stream_on(dev, stream)
+    cfg = _norm_rope(q, hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps)
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _used_on(stream, q_out)
+        q_out = _new((n, hq, d), q, stream)
     if k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        _used_on(stream, k_out)
-    _check(_lib.dp_qk_norm_rope(cfg, _rows(q, cfg.q_heads, n, like), _rows(k, cfg.kv_heads, n, like), n, _rows(q_out, cfg.q_heads, n, like),
-                                _rows(k_out, cfg.kv_heads, n, like), st), "dp_qk_norm_rope")
+        k_out = _new((n, hk, d), q, stream)
+    _check(_lib.dp_qk_norm_rope(cfg, _rows(q, hq, n, d, td, dev), _rows(k, hk, n, d, td, dev), n, _rows(q_out, hq, n, d, td, dev),
+                                _rows(k_out, hk, n, d, td, dev), st), "dp_qk_norm_rope")
     return q_out, k_out
 
 
@@ -473,8 +479,8 @@ class KVCache:
         self.data, self.scales, self.torch_dtype = data, scales, td
         self.n_pages, _, self.kv_heads, self.page_tokens, self.head_dim = data.shape
         self._like = (self.head_dim, td, data.device)
-        self._desc = KvCacheDesc(self.kv_heads, self.head_dim, self.page_tokens, self.n_pages, _KV_DTYPE[td], int(fp8), data.data_ptr(),
-                                 scales.data_ptr() if fp8 else None)
+        self._desc = bytes(KvCacheDesc(self.kv_heads, self.head_dim, self.page_tokens, self.n_pages, _KV_DTYPE[td], int(fp8), data.data_ptr(),
+                                       scales.data_ptr() if fp8 else None))
 
     @classmethod
     def empty(cls, n_pages, kv_heads, page_tokens, head_dim, dtype="bf16", fp8=False, device=None):
@@ -493,30 +499,27 @@ class KVCache:
     def write(self, k, v, slot, stream=None):
         """k, v: [n, kv_heads, head_dim] to slots (int32 [n], distinct; outside the pool: not written)."""
         n, st = slot.shape[0], _stream_on(self.data.device, stream)
-        _check(_lib.dp_kv_write(self._desc, _rows(k, self.kv_heads, n, self._like), _rows(v, self.kv_heads, n, self._like), self._slots(slot), n, st),
+        _check(_lib.dp_kv_write(self._desc, _rows(k, self.kv_heads, n, *self._like), _rows(v, self.kv_heads, n, *self._like), self._slots(slot), n, st),
                "dp_kv_write")
 
     def write_qkv(self, q, k, v, gq, gk, pos, slot, rope_theta=1e4, eps=1e-6, q_out=None, stream=None):
         """qk_norm_rope of q and k and the write of k and v, in one pass.  Returns q_out (which may be q)."""
-        cfg = _norm_rope(q, k, gq, gk, pos, rope_theta, eps)
-        n, st = q.shape[0], _stream_on(self.data.device, stream)
+        (n, hq, _), (d, td, dev) = q.shape, self._like
+        st = _stream_on(dev, stream)
+        cfg = _norm_rope(q, hq, self.kv_heads, n, d, td, dev, gq, gk, pos, rope_theta, eps)
         assert slot.shape[0] == n
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            _used_on(stream, q_out)
-        _check(_lib.dp_kv_write_qkv(self._desc, cfg, _rows(q, cfg.q_heads, n, self._like), _rows(k, self.kv_heads, n, self._like),
-                                    _rows(v, self.kv_heads, n, self._like), self._slots(slot), n, _rows(q_out, cfg.q_heads, n, self._like), st),
-               "dp_kv_write_qkv")
+            q_out = _new((n, hq, d), q, stream)
+        _check(_lib.dp_kv_write_qkv(self._desc, cfg, _rows(q, hq, n, d, td, dev), _rows(k, self.kv_heads, n, d, td, dev),
+                                    _rows(v, self.kv_heads, n, d, td, dev), self._slots(slot), n, _rows(q_out, hq, n, d, td, dev), st), "dp_kv_write_qkv")
         return q_out
 
     def read(self, slot, stream=None):
         """The keys and values at the slots, [n, kv_heads, head_dim] each, zeros where a slot is outside the pool."""
-        n, st = slot.shape[0], _stream_on(self.data.device, stream)
-        k = torch.empty((n, self.kv_heads, self.head_dim), dtype=self.torch_dtype, device=self.data.device)
-        v = torch.empty_like(k)
-        _used_on(stream, k, v)
-        _check(_lib.dp_kv_read(self._desc, self._slots(slot), n, _rows(k, self.kv_heads, n, self._like), _rows(v, self.kv_heads, n, self._like), st),
-               "dp_kv_read")
+        n, (d, td, dev), hk = slot.shape[0], self._like, self.kv_heads
+        st = _stream_on(dev, stream)
+        k, v = _new((n, hk, d), self.data, stream, td), _new((n, hk, d), self.data, stream, td)
+        _check(_lib.dp_kv_read(self._desc, self._slots(slot), n, _PACK_ROWS(k.data_ptr(), hk * d, d), _PACK_ROWS(v.data_ptr(), hk * d, d), st), "dp_kv_read")
         return k, v
 
     def attend(self, q, q_start, kv_len, page_table, max_q, max_kv, causal_group=0, scale=None, out=None, stream=None):
@@ -524,23 +527,18 @@ class KVCache:
         other; q_start int32 [n_seqs + 1], kv_len int32 [n_seqs], page_table int32 [n_seqs, width] on the device; max_q, max_kv: bounds of the
         new tokens and of the keys of a sequence.  causal_group 0: every query sees every key; g >= 1: groups of g keys up to its own.
         scale: 1 / sqrt(head_dim) if not given.  Rows of no sequence are left as they are (as they come, in a new `out`)."""
-        dev = self.data.device
-        n, hq, b = q.shape[0], q.shape[1], kv_len.shape[0]
-        assert q_start.shape == (b + 1,) and kv_len.dim() == 1 and page_table.dim() == 2 and page_table.shape[0] == b
+        (n, hq, _), (d, td, dev), b, width = q.shape, self._like, kv_len.shape[0], page_table.shape[1]
+        st = _stream_on(dev, stream)
+        assert q_start.shape == (b + 1,) and kv_len.dim() == 1 and page_table.shape == (b, width)
         for t in (q_start, kv_len, page_table):
             assert t.dtype == torch.int32 and t.device == dev and t.is_contiguous()
-        st = _stream_on(dev, stream)
         if out is None:
-            out = torch.empty((n, hq, self.head_dim), dtype=self.torch_dtype, device=dev)
-            _used_on(stream, out)
-        cfg = AttnConfig(hq, b, max_q, max_kv, page_table.shape[1], causal_group, self.head_dim ** -0.5 if scale is None else scale)
+            out = _new((n, hq, d), q, stream)
+        cfg = _PACK_ATTN(hq, b, max_q, max_kv, width, causal_group, d ** -0.5 if scale is None else scale)
         nbytes = _lib.dp_attn_paged_workspace_bytes(self._desc, cfg, n)
-        work = None
-        if nbytes:
-            work = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-            _used_on(stream, work)
-        _check(_lib.dp_attn_paged(self._desc, cfg, _rows(q, hq, n, self._like), n, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
-                                  _rows(out, hq, n, self._like), work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
+        work = _new(nbytes, self.data, stream, torch.uint8) if nbytes else None
+        _check(_lib.dp_attn_paged(self._desc, cfg, _rows(q, hq, n, d, td, dev), n, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                                  _rows(out, hq, n, d, td, dev), work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
         return out
 
 

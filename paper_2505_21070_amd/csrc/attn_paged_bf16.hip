@@ -264,7 +264,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
   bf16x8 qf[NT][HD / 32];
   int end[NT];
   load_queries<HD, NT>(a, b, b.first, qf, end, lane);
-  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
   const uint32_t kt = lds_address(smem) + wave * 2 * TILE * 16, vt = kt + TILE * 16;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
   Soft z[NT];
@@ -278,6 +277,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
   Carry<HD, 32, 1, CODES> ck, cv;
   int key = k0 + wave * 32;
   if (key < k1) { ck.load(a, b, key, 0, 0, lane); cv.load(a, b, key, to_values, 0, lane); }
+  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
   for (; key < k1; key += 128) {
     ck.template store<false>(kt, 0, lane);
     cv.template store<true>(vt, 0, lane);
@@ -456,19 +456,19 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
       done = 0;
     }
   }
-  // tile by tile: what is left, or everything once more
+  // tile by tile: what is left, or everything once more; the next one on its way, in stages 0 and 1 in turn
   const int again = done ? 0 : nw;
+  auto tile_at = [&](int j) __attribute__((always_inline)) { return j < again ? (j < cw ? w0 + j : -1) : j - again < cb ? b0 + j - again : -1; };
+  int tile = tile_at(0);
+  auto load_both = [&](int at) __attribute__((always_inline)) { ck.load(a, b, at * 64, 0, qt, lane); cv.load(a, b, at * 64, to_values, qt, lane); };
+  if (tile >= 0) load_both(tile);
   for (int j = 0; j < again + nb; ++j) {
-    const bool mine = j < again ? j < cw : j - again < cb;
-    const int tile = j < again ? w0 + j : b0 + j - again;
-    if (mine) {
-      ck.load(a, b, tile * 64, 0, qt, lane);
-      cv.load(a, b, tile * 64, to_values, qt, lane);
-    }
+    const int next = tile_at(j + 1);
+    if (tile >= 0) { store_k(j & 1); store_v(j & 1); }
+    if (j + 1 < again + nb && next >= 0) load_both(next);
     __syncthreads();
-    if (mine) { ck.template store<false>(kst, qt, lane); cv.template store<true>(vst, qt, lane); }
-    __syncthreads();
-    if (mine) step<HD, 4, 2>(a, b, kst, vst, qf, tile * 64, j >= again, end, gaps, z, o, lane);
+    if (tile >= 0) step<HD, 4, 2>(a, b, kst + (j & 1) * TILE, vst + (j & 1) * TILE, qf, tile * 64, j >= again, end, gaps, z, o, lane);
+    tile = next;
   }
   float l[2] = {over_lanes(z[0].l), over_lanes(z[1].l)};
   __syncthreads();
@@ -551,21 +551,24 @@ Route route(const PagedArgs& a) {
     r.tiles = tiles(r.qb);
     const int64_t blocks = r.tiles * a.hk;
     // one range for as many blocks as keep the chip full several times over; none shorter than two trips of the four wavefronts
-    int64_t parts = (2048 + blocks - 1) / blocks;
+    int64_t parts = ((a.n_seqs > 1 ? 8192 : 2048) + blocks - 1) / blocks;
     if (parts > (keys + 255) / 256) parts = (keys + 255) / 256;
     if (parts > 256) parts = 256;
     if (parts < 1) parts = 1;
     r.part_keys = (int)(((keys + parts - 1) / parts + 127) / 128 * 128);
   } else {
-    // Blocks of either shape, one to a CU, run in rounds of 256; a step of 64 keys x 256 rows, or 2 x 64 keys x 128 rows, is 1.7 us at heads of 128, and what a
-    // block does around its steps about 5 of them.  Ranges fill the last round, and cost a launch and the traffic of partial results (7 MB a step).
+    // Blocks of either shape, one to a CU; a step of 64 keys x 256 rows, or 2 x 64 keys x 128 rows, is 1.7 us at heads of 128, and what a
+    // block does around its steps about 5 of them.  One sequence, seen whole: rounds of 256 blocks.  Sequences of several lengths and causal borders: all the work, with
+    // ranges of half the bound on average, and one block's at the end.  Ranges cost a launch and the traffic of partial results (7 MB a step).
+    const bool even = a.n_seqs == 1 && a.group == 0;
     int64_t best = INT64_MAX;
     const int64_t key_tiles = (keys + 63) / 64;
     for (int qb = 256; qb >= 128; qb -= 128)
-      for (int64_t parts = 1; parts <= 8; ++parts) {
-        const int64_t n = tiles(qb), blocks = n * a.hk * parts, of_part = (key_tiles + parts - 1) / parts;
+      for (int64_t parts = 1; parts <= 16; ++parts) {
+        const int64_t n = tiles(qb), blocks = n * a.hk * parts, of_part = (key_tiles + parts - 1) / parts, steps = qb == 256 ? of_part : (of_part + 1) / 2;
         if (parts > 1 && of_part < 8) break;
-        const int64_t cost = ((blocks + 255) / 256) * ((qb == 256 ? of_part : (of_part + 1) / 2) + 5) + (parts > 1 ? 4 + blocks * qb * 520 / 7000000 : 0);
+        const int64_t work = even ? (blocks + 255) / 256 * (steps + 5) : blocks * (steps / 2 + 5) / 256 + steps + 5;
+        const int64_t cost = work + (parts > 1 ? 4 + blocks * qb * 520 / 7000000 : 0);
         if (cost < best) { best = cost; r.qb = qb; r.tiles = n; r.part_keys = (int)(of_part * 64); }
       }
   }

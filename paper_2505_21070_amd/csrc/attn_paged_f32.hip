@@ -45,21 +45,33 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
                                      bool border, const int (&end)[NT], bool gaps, Soft (&z)[NT], f32x4 (&o)[HD / 16][NT], int lane) {
   constexpr int RS = HD + 4;
   const int lr = lane & 15, lg = lane >> 4;
-  f32x4 sc[NT][KT];
+  // two chains of sums for each tile of scores, so that no product waits for the one before it
+  f32x4 sc[NT][KT], odd[NT][KT];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int kt = 0; kt < KT; ++kt) sc[t][kt] = odd[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int c = 0; c < HD / 16; ++c)
+  for (int c = 0; c < HD / 16; c += 2) {
+    f32x4 k[2][KT];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const f32x4 k = *(const f32x4*)(ktile + (kt * 16 + lr) * RS + c * 16 + lg * 4);
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int kt = 0; kt < KT; ++kt) k[h][kt] = *(const f32x4*)(ktile + (kt * 16 + lr) * RS + (c + h) * 16 + lg * 4);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sc[t][kt] = mfma(k[j], qf[t][c][j], sc[t][kt]);
-    }
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          sc[t][kt] = mfma(k[0][kt][j], qf[t][c][j], sc[t][kt]);
+          odd[t][kt] = mfma(k[1][kt][j], qf[t][c + 1][j], odd[t][kt]);
+        }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) sc[t][kt] += odd[t][kt];
   const uint32_t gone = gaps ? missing<KT>(a, b, key0, lane) : 0;
   f32x4 p[NT][KT];
 #pragma unroll
@@ -77,6 +89,21 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
         z[t].l += p[t][kt][r];
       }
   }
+  if (!border) {
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) {
+          const float v = vtile[(kt * 16 + lg * 4 + r) * RS + d * 16 + lr];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) o[d][t] = mfma(v, p[t][kt][r], o[d][t]);
+        }
+    return;
+  }
+  // A value that is not finite must not meet the weight 0 of a row that does not see its key (0 * infinity is NaN): it is multiplied as 0, and rows that do
+  // see +inf, -inf or NaN are found by products of ones and get it added.
 #pragma unroll
   for (int d = 0; d < HD / 16; ++d) {
     float v[KT][4];
@@ -88,35 +115,29 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
         v[kt][r] = vtile[(kt * 16 + lg * 4 + r) * RS + d * 16 + lr];
         bad |= !(fabsf(v[kt][r]) < INFINITY);
       }
-    // a value that is not finite must not meet the weight 0 of a row that does not see its key: it is multiplied as 0, and rows that do
-    // see +inf, -inf or NaN are found by products of ones and get it added
-    const bool check = border && __any(bad);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float x = check && !(fabsf(v[kt][r]) < INFINITY) ? 0.f : v[kt][r];
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) o[d][t] = mfma(x, p[t][kt][r], o[d][t]);
-      }
-    if (check) {
+        for (int t = 0; t < NT; ++t) o[d][t] = mfma(fabsf(v[kt][r]) < INFINITY ? v[kt][r] : 0.f, p[t][kt][r], o[d][t]);
+    if (!__any(bad)) continue;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        f32x4 np{0.f, 0.f, 0.f, 0.f}, nn = np, nx = np;
+    for (int t = 0; t < NT; ++t) {
+      f32x4 np{0.f, 0.f, 0.f, 0.f}, nn = np, nx = np;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float x = v[kt][r], one = sc[t][kt][r] == -INFINITY ? 0.f : 1.f;
-            np = mfma(x == INFINITY ? 1.f : 0.f, one, np);
-            nn = mfma(x == -INFINITY ? 1.f : 0.f, one, nn);
-            nx = mfma(x != x ? 1.f : 0.f, one, nx);
-          }
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float x = o[d][t][r] + (np[r] > 0.f ? INFINITY : 0.f) - (nn[r] > 0.f ? INFINITY : 0.f);
-          o[d][t][r] = nx[r] > 0.f ? __uint_as_float(0x7fc00000u) : x;
+          const float x = v[kt][r], one = sc[t][kt][r] == -INFINITY ? 0.f : 1.f;
+          np = mfma(x == INFINITY ? 1.f : 0.f, one, np);
+          nn = mfma(x == -INFINITY ? 1.f : 0.f, one, nn);
+          nx = mfma(x != x ? 1.f : 0.f, one, nx);
         }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = o[d][t][r] + (np[r] > 0.f ? INFINITY : 0.f) - (nn[r] > 0.f ? INFINITY : 0.f);
+        o[d][t][r] = nx[r] > 0.f ? __uint_as_float(0x7fc00000u) : x;
       }
     }
   }
@@ -149,13 +170,13 @@ __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
   float* const kt = smem + kg * 2 * TILE;
   float* const vt = kt + TILE;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
   Carry<HD, TK, QG, CODES> ck, cv;
   int key = k0 + kg * TK;
   if (key < k1) { ck.load(a, b, key, 0, qt, lane); cv.load(a, b, key, to_values, qt, lane); }
+  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
   for (; key < k1; key += KG * TK) {
     if constexpr (QG > 1) __syncthreads();
     ck.store(kt, qt, lane);

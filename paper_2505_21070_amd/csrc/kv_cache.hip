@@ -4,8 +4,8 @@
 //
 // All are bound by memory: a value is read once and written once, 4 bytes a value in bf16, 3 into codes.  A head's row is 8 to 32 lanes of 16
 // bytes, so its sum of squares and its largest value stay within the lanes that hold it, and a channel pair (2i, 2i+1) within one lane.  A wavefront
-// takes a run of one token's heads: the token's angles are the same for all of them and are computed once, in 64 bits up to the turn's
-// fraction.
+// takes a run of one token's heads, all queries, all keys or all values: the token's angles are the same for all of them and are computed once, a
+// pair a lane, in 64 bits up to the turn's fraction.
 #include <math.h>
 
 #include "paged.h"
@@ -23,8 +23,9 @@ struct RowArgs {
   const int32_t *pos, *slot;
   const void *gq, *gk;
   int64_t n_tokens;
-  int32_t hq, hk, n_rows;                 // rows of a token: hq + hk (+ hk)
-  int32_t runs, per_run;                  // runs of heads a token is cut into, rows of a run
+  int32_t hq, hk;
+  int32_t runs_q, runs_k, runs;           // runs that a token's queries, its keys (and as well its values), and all of it are cut into
+  int32_t per_q, per_k;                   // rows of a run
   int32_t page_shift, n_slots;
   float eps;
   // pair i of an axis with c pairs turns by theta^(-i/c) a step: powers theta^(-2^j/c) of the frame axis (0) and of the other two (1)
@@ -67,103 +68,107 @@ template <> struct Vec<float> {
   }
 };
 
-// cos and sin of the token's angles for this lane's pairs c0/2 .. of a head
+// cos and sin of the token's angles, one pair a lane (a head of 64: lanes 32 .. as lanes 0 ..), handed to the lanes that hold the pairs from pair0 on
 template <int HD, int NP>
-__device__ __forceinline__ void angles(const RowArgs& a, int64_t t, int pair0, float (&cs)[NP], float (&sn)[NP]) {
+__device__ __forceinline__ void angles(const RowArgs& a, int64_t t, int lane, int pair0, float (&cs)[NP], float (&sn)[NP]) {
   constexpr int CS = HD / 6, CF = HD / 2 - 2 * CS;          // pairs of the row and column axes, and of the frame axis
   const int32_t pf = a.pos[3 * t], py = a.pos[3 * t + 1], px = a.pos[3 * t + 2];
+  const int p = lane & (HD / 2 - 1);
+  const bool frame = p < CF;
+  const int e = frame ? p : p < CF + CS ? p - CF : p - CF - CS;
+  const int32_t at = frame ? pf : p < CF + CS ? py : px;
+  double f = 0.15915494309189533577;                         // 1 / (2 pi): angles in turns
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int p = pair0 + i;
-    const bool frame = p < CF;
-    const int e = frame ? p : p < CF + CS ? p - CF : p - CF - CS;
-    const int32_t at = frame ? pf : p < CF + CS ? py : px;
-    double f = 0.15915494309189533577;                       // 1 / (2 pi): angles in turns
+  for (int j = 0; j < 6; ++j) f *= (e >> j) & 1 ? (frame ? a.power[0][j] : a.power[1][j]) : 1.0;
+  const double turns = (double)at * f;
+  float c, s;
+  sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
 #pragma unroll
-    for (int j = 0; j < 6; ++j) f *= (e >> j) & 1 ? (frame ? a.power[0][j] : a.power[1][j]) : 1.0;
-    const double turns = (double)at * f;
-    sincospif(2.f * (float)(turns - rint(turns)), &sn[i], &cs[i]);
-  }
+  for (int i = 0; i < NP; ++i) { cs[i] = __shfl(c, pair0 + i, 64); sn[i] = __shfl(s, pair0 + i, 64); }
 }
 
-// One wavefront: rows run * per_run .. of token t, 64 / LANES at a time, U of those trips to memory under way at once.
+// One wavefront: the rows of a run, 64 / LANES at a time, U of those trips to memory under way at once.
 template <typename T, int HD, bool NORM, int TO>
 __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
   constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = 4;
   const int lane = threadIdx.x & 63, in_row = lane % LANES, c0 = in_row * N;
-  const uint32_t task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^24 + 2^14, see cut()
+  const uint32_t task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^26, see cut()
   const int64_t t = task / (uint32_t)a.runs;
   if (t >= a.n_tokens) return;
-  const int first = (int)(task % (uint32_t)a.runs) * a.per_run, last = first + a.per_run < a.n_rows ? first + a.per_run : a.n_rows;
+  int run = (int)(task % (uint32_t)a.runs);
+  // which rows these are; all the same
+  const bool is_q = NORM && run < a.runs_q;
+  run -= is_q ? 0 : a.runs_q;
+  const bool is_v = !is_q && run >= a.runs_k;
+  run -= is_v ? a.runs_k : 0;
+  const int per = is_q ? a.per_q : a.per_k, of = is_q ? a.hq : a.hk;
+  const int first = run * per, last = first + per < of ? first + per : of;
   int32_t slot = 0;
-  if constexpr (TO != TO_ROWS) slot = a.slot[t];
-  const bool kept = TO == TO_ROWS || (slot >= 0 && slot < a.n_slots);
-  const T* const q = (const T*)a.q + t * a.q_ts + c0;
-  const T* const k = (const T*)a.k + t * a.k_ts + c0;
-  const T* const v = (const T*)a.v + t * a.v_ts + c0;
-  auto load = [&](int r) __attribute__((always_inline)) {
-    const T* const p = NORM && r < a.hq ? q + r * a.q_hs : r < a.hq + a.hk ? k + (r - a.hq) * a.k_hs : v + (r - a.hq - a.hk) * a.v_hs;
-    return *(const uint4*)p;
-  };
+  if constexpr (TO != TO_ROWS) {
+    slot = a.slot[t];
+    if (!is_q && !(slot >= 0 && slot < a.n_slots)) return;   // a row of padding
+  }
+  const int64_t hs = is_q ? a.q_hs : is_v ? a.v_hs : a.k_hs;
+  const T* const src = (is_q ? (const T*)a.q + t * a.q_ts : is_v ? (const T*)a.v + t * a.v_ts : (const T*)a.k + t * a.k_ts) + c0;
   uint4 raw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int r = first + u * ROWS + lane / LANES;
-    raw[u] = r < last ? load(r) : uint4{};
+    raw[u] = r < last ? *(const uint4*)(src + r * hs) : uint4{};
   }
-  float gq[N], gk[N], cs[N / 2], sn[N / 2];
-  if constexpr (NORM) {
-    Vec<T>::unpack(*(const uint4*)((const T*)a.gq + c0), gq);
-    Vec<T>::unpack(*(const uint4*)((const T*)a.gk + c0), gk);
-    angles<HD, N / 2>(a, t, c0 / 2, cs, sn);
+  // y0 = (x0 g0 cos - x1 g1 sin) / rms and y1 = (x0 g0 sin + x1 g1 cos) / rms: the gains are folded into the turn
+  float g0c[N / 2], g1s[N / 2], g0s[N / 2], g1c[N / 2];
+  if (NORM && !is_v) {
+    float g[N], cs[N / 2], sn[N / 2];
+    Vec<T>::unpack(*(const uint4*)((const T*)(is_q ? a.gq : a.gk) + c0), g);
+    angles<HD, N / 2>(a, t, lane, c0 / 2, cs, sn);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      g0c[i] = g[2 * i] * cs[i]; g0s[i] = g[2 * i] * sn[i];
+      g1c[i] = g[2 * i + 1] * cs[i]; g1s[i] = g[2 * i + 1] * sn[i];
+    }
   }
-  const int64_t page = slot >> a.page_shift, in_page = slot & ((1 << a.page_shift) - 1);
+  const bool to_rows = TO == TO_ROWS || is_q;
+  const int64_t out_hs = is_q ? a.qo_hs : a.ko_hs;
+  T* const dst = (is_q ? (T*)a.qo + t * a.qo_ts : (T*)a.ko + t * a.ko_ts) + c0;
+  // row 0 of the token's heads in the pages: [page][keys | values][head][token]
+  const int64_t row0 = ((((int64_t)(slot >> a.page_shift) * 2 + is_v) * a.hk) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
   for (int r0 = first; r0 < last; r0 += U * ROWS) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * ROWS + lane / LANES;
-      const uint4 now = raw[u];
-      const int next = r + U * ROWS;
-      if (r0 + (U + u) * ROWS < last) raw[u] = next < last ? load(next) : uint4{};
-      if (r0 + u * ROWS >= last) continue;
+      if (r0 + u * ROWS >= last) break;
+      const int r = r0 + u * ROWS + lane / LANES, next = r + U * ROWS;
       float x[N];
-      Vec<T>::unpack(now, x);
-      const bool is_v = r >= a.hq + a.hk, is_q = NORM && r < a.hq;
-      if constexpr (NORM) {
+      Vec<T>::unpack(raw[u], x);
+      raw[u] = next < last ? *(const uint4*)(src + next * hs) : uint4{};
+      if (NORM && !is_v) {
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) sum = fmaf(x[i], x[i], sum);
         const float inv = rsqrtf(over_row<LANES>(sum, [](float m, float n) { return m + n; }) * (1.f / HD) + a.eps);
-        if (!is_v) {
 #pragma unroll
-          for (int i = 0; i < N; i += 2) {
-            const float m = x[i] * inv * (is_q ? gq[i] : gk[i]), n = x[i + 1] * inv * (is_q ? gq[i + 1] : gk[i + 1]);
-            x[i] = m * cs[i / 2] - n * sn[i / 2];
-            x[i + 1] = m * sn[i / 2] + n * cs[i / 2];
-          }
+        for (int i = 0; i < N; i += 2) {
+          const float m = x[i] * inv, n = x[i + 1] * inv;
+          x[i] = m * g0c[i / 2] - n * g1s[i / 2];
+          x[i + 1] = m * g0s[i / 2] + n * g1c[i / 2];
         }
       }
-      if constexpr (TO == TO_ROWS) {
-        if (r < last) *(uint4*)(is_q ? (T*)a.qo + t * a.qo_ts + r * a.qo_hs + c0 : (T*)a.ko + t * a.ko_ts + (r - a.hq) * a.ko_hs + c0) = Vec<T>::pack(x);
+      if (to_rows) {
+        if (r < last) *(uint4*)(dst + r * out_hs) = Vec<T>::pack(x);
       } else {
-        // row of the pages: [page][keys | values][head][token]
-        const int64_t row = (((page * 2 + is_v) * a.hk + (r - a.hq - (is_v ? a.hk : 0))) << a.page_shift) + in_page;
-        const bool to_page = r < last && !is_q && kept;
-        if constexpr (NORM) {
-          if (r < last && is_q) *(uint4*)((T*)a.qo + t * a.qo_ts + r * a.qo_hs + c0) = Vec<T>::pack(x);
-        }
+        const int64_t row = row0 + ((int64_t)r << a.page_shift);
         if constexpr (TO == TO_PAGES) {
-          if (to_page) *(uint4*)((T*)a.data + row * HD + c0) = Vec<T>::pack(x);
+          if (r < last) *(uint4*)((T*)a.data + row * HD + c0) = Vec<T>::pack(x);
         } else {
           float top = 0.f;
 #pragma unroll
           for (int i = 0; i < N; ++i) top = fabsf(x[i]) < INFINITY ? fmaxf(top, fabsf(x[i])) : top;
           const int e = fp8_exponent(over_row<LANES>(top, [](float m, float n) { return fmaxf(m, n); }));
           const float inv = pow2f(-e);
-          if (to_page) {
-            uint8_t* const dst = (uint8_t*)a.data + row * HD + c0;
-            if constexpr (N == 8) *(uint2*)dst = make_uint2(to_fp8x4(x[0], x[1], x[2], x[3], inv), to_fp8x4(x[4], x[5], x[6], x[7], inv));
-            else *(uint32_t*)dst = to_fp8x4(x[0], x[1], x[2], x[3], inv);
+          if (r < last) {
+            uint8_t* const to = (uint8_t*)a.data + row * HD + c0;
+            if constexpr (N == 8) *(uint2*)to = make_uint2(to_fp8x4(x[0], x[1], x[2], x[3], inv), to_fp8x4(x[4], x[5], x[6], x[7], inv));
+            else *(uint32_t*)to = to_fp8x4(x[0], x[1], x[2], x[3], inv);
             if (in_row == 0) a.scales[row] = (uint8_t)(e + 127);
           }
         }
@@ -180,12 +185,16 @@ __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
   const uint32_t task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^24 + 2^14, see cut()
   const int64_t t = task / (uint32_t)a.runs;
   if (t >= a.n_tokens) return;
-  const int first = (int)(task % (uint32_t)a.runs) * a.per_run, last = first + a.per_run < a.n_rows ? first + a.per_run : a.n_rows;
+  int run = (int)(task % (uint32_t)a.runs);
+  const bool is_v = run >= a.runs_k;
+  run -= is_v ? a.runs_k : 0;
+  const int first = run * a.per_k, last = first + a.per_k < a.hk ? first + a.per_k : a.hk;
   const int32_t slot = a.slot[t];
   const bool kept = slot >= 0 && slot < a.n_slots;
   const int64_t page = kept ? slot >> a.page_shift : 0, in_page = kept ? slot & ((1 << a.page_shift) - 1) : 0;
-  T* const k = (T*)a.ko + t * a.ko_ts + c0;
-  T* const v = (T*)a.qo + t * a.qo_ts + c0;                   // the values take the place of the queries
+  const int64_t row0 = (((page * 2 + is_v) * a.hk) << a.page_shift) + in_page;
+  const int64_t hs = is_v ? a.qo_hs : a.ko_hs;                // the values take the place of the queries
+  T* const dst = (is_v ? (T*)a.qo + t * a.qo_ts : (T*)a.ko + t * a.ko_ts) + c0;
   for (int r0 = first; r0 < last; r0 += U * ROWS) {
     typename std::conditional<CODES, typename std::conditional<N == 8, uint2, uint32_t>::type, uint4>::type raw[U];
     uint32_t byte[U];
@@ -193,8 +202,7 @@ __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
     for (int u = 0; u < U; ++u) {
       int r = r0 + u * ROWS + lane / LANES;
       if (r >= last) r = last - 1;
-      const bool is_v = r >= a.hk;
-      const int64_t row = (((page * 2 + is_v) * a.hk + (r - (is_v ? a.hk : 0))) << a.page_shift) + in_page;
+      const int64_t row = row0 + ((int64_t)r << a.page_shift);
       if constexpr (CODES) {
         raw[u] = *(const decltype(&raw[u]))((const uint8_t*)a.data + row * HD + c0);
         byte[u] = a.scales[row];
@@ -211,19 +219,27 @@ __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
       else if constexpr (N == 8) out = fp8x8_to_bf16(raw[u], __uint_as_float(byte[u] << 23));
       else { const float4 f = fp8x4_to_f32(raw[u], __uint_as_float(byte[u] << 23)); out = __builtin_bit_cast(uint4, f); }
       if (!kept) out = uint4{};
-      *(uint4*)(r < a.hk ? k + r * a.ko_hs : v + (r - a.hk) * a.qo_hs) = out;
+      *(uint4*)(dst + r * hs) = out;
     }
   }
 }
 
-// Runs of heads: as many as give the chip 16384 wavefronts, twice what it holds at the kernels' registers, but none shorter than one trip.
-void cut(RowArgs& a, int rows_per_trip) {
-  int64_t runs = (a.n_rows + rows_per_trip - 1) / rows_per_trip;
-  const int64_t want = (16384 + a.n_tokens - 1) / a.n_tokens;
-  if (runs > want) runs = want;
-  const int64_t trips = ((a.n_rows + runs - 1) / runs + rows_per_trip - 1) / rows_per_trip;
-  a.per_run = (int32_t)(trips * rows_per_trip);
-  a.runs = (a.n_rows + a.per_run - 1) / a.per_run;
+// Runs of heads: as many as give the chip 16384 wavefronts, twice what it holds at the kernels' registers, but none shorter than one of the U
+// trips (rows) that a wavefront has under way.
+void cut(RowArgs& a, int rows, bool values) {
+  const int64_t want = (16384 + a.n_tokens - 1) / a.n_tokens, sections = (a.hq > 0) + 1 + values;
+  auto runs = [&](int heads, int32_t& per) -> int32_t {
+    if (!heads) return 0;
+    int64_t n = (heads + rows - 1) / rows;
+    const int64_t most = (want + sections - 1) / sections;
+    if (n > most) n = most;
+    const int64_t trips = ((heads + n - 1) / n + rows - 1) / rows;
+    per = (int32_t)(trips * rows);
+    return (heads + per - 1) / per;
+  };
+  a.runs_q = runs(a.hq, a.per_q);
+  a.runs_k = runs(a.hk, a.per_k);
+  a.runs = a.runs_q + (values ? 2 : 1) * a.runs_k;
 }
 unsigned blocks_of(const RowArgs& a) { return (unsigned)((a.n_tokens * a.runs + 3) / 4); }
 
@@ -248,9 +264,9 @@ template <typename T, int HD, bool NORM> void launch_to(const RowArgs& a, int to
   else if (to == TO_PAGES) k_head_rows<T, HD, NORM, TO_PAGES><<<g, 256, 0, st>>>(a);
   else if constexpr (NORM) k_head_rows<T, HD, NORM, TO_ROWS><<<g, 256, 0, st>>>(a);
 }
-template <bool NORM> int launch_rows(RowArgs& a, int hd, int dtype, int to, void* stream, const char* entry) {
+template <bool NORM> int launch_rows(RowArgs& a, int hd, int dtype, int to, bool values, void* stream, const char* entry) {
   const hipStream_t st = (hipStream_t)stream;
-  cut(a, 64 / (hd / (dtype == DP_BF16 ? 8 : 4)) * 4);
+  cut(a, 64 / (hd / (dtype == DP_BF16 ? 8 : 4)), values);
   (void)hipGetLastError();
   if (dtype == DP_BF16) { if (hd == 128) launch_to<bf16_t, 128, NORM>(a, to, st); else launch_to<bf16_t, 64, NORM>(a, to, st); }
   else { if (hd == 128) launch_to<float, 128, NORM>(a, to, st); else launch_to<float, 64, NORM>(a, to, st); }
@@ -290,11 +306,10 @@ extern "C" int dp_qk_norm_rope(const dp_norm_rope* c, const dp_rows* q, const dp
   REFUSE_IF(why_not_rows(ko, n, c->kv_heads, c->head_dim, c->dtype, true));
   RowArgs a{};
   SET_ROWS(q, q); SET_ROWS(k, k); SET_ROWS(qo, qo); SET_ROWS(ko, ko);
-  a.v = k->data;                                              // never read
   a.pos = c->pos; a.gq = c->gq; a.gk = c->gk; a.eps = c->eps; a.n_tokens = n;
-  a.hq = c->q_heads; a.hk = c->kv_heads; a.n_rows = a.hq + a.hk;
+  a.hq = c->q_heads; a.hk = c->kv_heads;
   set_powers(a, c->head_dim, c->rope_theta);
-  return launch_rows<true>(a, c->head_dim, c->dtype, TO_ROWS, stream, entry);
+  return launch_rows<true>(a, c->head_dim, c->dtype, TO_ROWS, false, stream, entry);
 }
 
 extern "C" int dp_kv_write(const dp_kv_cache* c, const dp_rows* k, const dp_rows* v, const int32_t* slot, int64_t n, void* stream) {
@@ -308,8 +323,8 @@ extern "C" int dp_kv_write(const dp_kv_cache* c, const dp_rows* k, const dp_rows
   RowArgs a{};
   SET_ROWS(k, k); SET_ROWS(v, v);
   set_cache(a, c);
-  a.slot = slot; a.n_tokens = n; a.n_rows = 2 * a.hk;
-  return launch_rows<false>(a, c->head_dim, c->dtype, c->format == DP_KV_FP8 ? TO_CODES : TO_PAGES, stream, entry);
+  a.slot = slot; a.n_tokens = n;
+  return launch_rows<false>(a, c->head_dim, c->dtype, c->format == DP_KV_FP8 ? TO_CODES : TO_PAGES, true, stream, entry);
 }
 
 extern "C" int dp_kv_write_qkv(const dp_kv_cache* c, const dp_norm_rope* m, const dp_rows* q, const dp_rows* k, const dp_rows* v, const int32_t* slot,
@@ -330,9 +345,9 @@ extern "C" int dp_kv_write_qkv(const dp_kv_cache* c, const dp_norm_rope* m, cons
   SET_ROWS(q, q); SET_ROWS(k, k); SET_ROWS(v, v); SET_ROWS(qo, qo);
   set_cache(a, c);
   a.pos = m->pos; a.gq = m->gq; a.gk = m->gk; a.eps = m->eps; a.slot = slot; a.n_tokens = n;
-  a.hq = m->q_heads; a.n_rows = a.hq + 2 * a.hk;
+  a.hq = m->q_heads;
   set_powers(a, c->head_dim, m->rope_theta);
-  return launch_rows<true>(a, c->head_dim, c->dtype, c->format == DP_KV_FP8 ? TO_CODES : TO_PAGES, stream, entry);
+  return launch_rows<true>(a, c->head_dim, c->dtype, c->format == DP_KV_FP8 ? TO_CODES : TO_PAGES, true, stream, entry);
 }
 
 extern "C" int dp_kv_read(const dp_kv_cache* c, const int32_t* slot, int64_t n, const dp_rows* ko, const dp_rows* vo, void* stream) {
@@ -347,9 +362,9 @@ extern "C" int dp_kv_read(const dp_kv_cache* c, const int32_t* slot, int64_t n, 
   set_cache(a, c);
   SET_ROWS(ko, ko);
   SET_ROWS(qo, vo);
-  a.slot = slot; a.n_tokens = n; a.n_rows = 2 * a.hk;
+  a.slot = slot; a.n_tokens = n;
   const hipStream_t st = (hipStream_t)stream;
-  cut(a, 64 / (c->head_dim / (c->dtype == DP_BF16 ? 8 : 4)) * 4);
+  cut(a, 64 / (c->head_dim / (c->dtype == DP_BF16 ? 8 : 4)), true);
   const unsigned g = blocks_of(a);
   const bool codes = c->format == DP_KV_FP8;
   (void)hipGetLastError();

@@ -9,26 +9,31 @@ L = B._lib
 AT = 1 << 20                                                  # an aligned address that no refused call looks at
 
 
+def packed(struct):
+    """The bytes that the binding hands over, None as a null pointer."""
+    return bytes(struct)
+
+
 def cache(**kw):
     d = dict(kv_heads=2, head_dim=128, page_tokens=16, n_pages=8, dtype=B.DP_BF16, format=1, data=AT, scales=AT)
     d.update(kw)
-    return B.KvCacheDesc(**d)
+    return packed(B.KvCacheDesc(**d))
 
 
 def norm(**kw):
     d = dict(q_heads=4, kv_heads=2, head_dim=128, dtype=B.DP_BF16, rope_theta=1e4, eps=1e-6, gq=AT, gk=AT, pos=AT)
     d.update(kw)
-    return B.NormRope(**d)
+    return packed(B.NormRope(**d))
 
 
 def attn(**kw):
     d = dict(q_heads=4, n_seqs=3, max_q=5, max_kv=60, table_width=4, causal_group=0, scale=0.1)
     d.update(kw)
-    return B.AttnConfig(**d)
+    return packed(B.AttnConfig(**d))
 
 
 def rows(heads, d=128, data=AT, ts=None, hs=None):
-    return B.KvRows(data, heads * d if ts is None else ts, d if hs is None else hs)
+    return packed(B.KvRows(data, heads * d if ts is None else ts, d if hs is None else hs))
 
 
 BAD_CACHE = [dict(kv_heads=0), dict(kv_heads=1025), dict(head_dim=96), dict(page_tokens=8), dict(page_tokens=48), dict(page_tokens=1 << 17),
