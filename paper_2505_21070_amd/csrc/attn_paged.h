@@ -12,9 +12,12 @@ struct PagedArgs {
   const int32_t *q_start, *kv_len, *table;
   int32_t n_pages, page_shift, hk, shared, n_seqs, max_q, max_kv, table_width, group;
   float scale;                            // of the scores, times log2(e): softmax in powers of two
-  // the launch: tiles of rows (of all sequences), the most a sequence has, ranges of keys a tile's work is cut into and keys of a range
-  int32_t tiles, tiles_of_seq, parts, part_keys;
-  float* partial;                         // parts > 1: [tile and head][part] of m[QB], l[QB], O[QB][head_dim]
+  // The launch: tiles of rows (of all sequences) and the most a sequence has.  A block has one tile's range of keys with one key head: of `parts` ranges
+  // of part_keys keys each.  Or, with a plan, the work of all tiles and heads lies in one line, in units of a number of keys, and each of `runs` blocks
+  // has an equal run of it: the end of one tile's keys, all of some, the beginning of another's.
+  int32_t tiles, tiles_of_seq, parts, part_keys, runs;
+  int32_t* plan;                          // null, or units before each tile and of all [tiles + 1], sequence [tiles], tile of the sequence [tiles]
+  float* partial;                         // of each range, or of the incomplete first [0] and last [1] tile of each run: m[QB], l[QB], O[QB][head_dim]
 };
 
 // read through the scalar cache: uniform addresses of arrays that no kernel here writes
@@ -24,6 +27,15 @@ __device__ __forceinline__ int32_t uniform_i32(const int32_t* p) {
 #else
   return *p;
 #endif
+}
+
+// the lane, read anew for each piece of work: what is made of it is not kept in registers from one piece to the next
+__device__ __forceinline__ int fresh_lane() {
+  int lane = threadIdx.x & 63;
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(lane));
+#endif
+  return lane;
 }
 
 // a sequence's new tokens and keys, whatever the arrays hold
@@ -51,24 +63,49 @@ __device__ __forceinline__ int seen_keys(const PagedArgs& a, int i, int n, int k
   return end < keys ? (int)end : keys;
 }
 
-// The rows and keys of a block: tile `tile` of the call's tiles of QB rows, with key head `hk`.  Rows are (new token, shared head) pairs.
+// Rows and keys: a tile of QB rows of a sequence, with key head `hk`.  Rows are (new token, shared head) pairs.
 struct Block {
   int b, hk;                              // sequence, key head
-  int first, rows;                        // its first row and one past the sequence's last
+  int first, rows;                        // the tile's first row and one past the sequence's last
   Seq s;
   int held;                               // keys that exist for this sequence
-  int end, whole;                         // keys that its last row sees, that its first row (and so every row) sees
+  int end, whole;                         // keys that the last row sees, that the first row (and so every row) sees
 };
-// false: nothing to do.  Uniform; called by whole wavefronts.
+// the rb-th tile of sequence b; false: there is none
+template <int QB> __device__ __forceinline__ bool tile_of(const PagedArgs& a, Block& k, int b, int rb, int hk) {
+  k.b = b;
+  k.hk = hk;
+  k.s = sequence(a, b);
+  k.rows = k.s.rows * a.shared;
+  const int of_seq = (k.rows + QB - 1) / QB;
+  if (rb >= of_seq) return false;
+  // the last tile of a sequence first: under a causal border it has the most keys
+  k.first = (of_seq - 1 - rb) * QB;
+  k.held = held_keys(a, k.s.keys);
+  const int last = (k.first + QB < k.rows ? k.first + QB : k.rows) - 1;
+  const int e = seen_keys(a, last / a.shared, k.s.n, k.s.keys), w = seen_keys(a, k.first / a.shared, k.s.n, k.s.keys);
+  k.end = e < k.held ? e : k.held;
+  k.whole = w < k.held ? w : k.held;
+  return true;
+}
+// What is the same in all lanes goes into scalar registers, so that page tables are read through the scalar cache.
+__device__ __forceinline__ void make_uniform(Block& k) {
+  k.b = __builtin_amdgcn_readfirstlane(k.b);
+  k.hk = __builtin_amdgcn_readfirstlane(k.hk);
+  k.first = __builtin_amdgcn_readfirstlane(k.first);
+  k.end = __builtin_amdgcn_readfirstlane(k.end);
+  k.whole = __builtin_amdgcn_readfirstlane(k.whole);
+}
+// Tile `tile` of all.  false: nothing to do.  Uniform; called by whole wavefronts.
 template <int QB> __device__ __forceinline__ bool locate(const PagedArgs& a, int tile, int hk, Block& k) {
-  int rb = 0;
-  if (a.tiles_of_seq == 1) k.b = tile;
-  else if (a.n_seqs == 1) { k.b = 0; rb = tile; }
+  int b = -1, rb = 0;
+  if (a.tiles_of_seq == 1) b = tile;
+  else if (a.n_seqs == 1) { b = 0; rb = tile; }
+  else if (a.plan) { b = uniform_i32(a.plan + a.tiles + 1 + tile); rb = uniform_i32(a.plan + 2 * a.tiles + 1 + tile); }
   else {
     // tiles are numbered through the sequences: 64 of them at a time, a lane each
     const int lane = threadIdx.x & 63;
     int base = 0;
-    k.b = -1;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
       const int sq = s0 + lane < a.n_seqs ? s0 + lane : a.n_seqs - 1;
       const Seq s = sequence(a, a.q_start[sq], a.q_start[sq + 1], 0);
@@ -79,31 +116,118 @@ template <int QB> __device__ __forceinline__ bool locate(const PagedArgs& a, int
       const unsigned long long beyond = __ballot(base + upto > tile);
       if (beyond) {
         const int l = __builtin_ctzll(beyond);
-        k.b = s0 + l;
+        b = s0 + l;
         rb = tile - base - (__shfl(upto, l, 64) - __shfl(n, l, 64));
         break;
       }
       base += __shfl(upto, 63, 64);
     }
-    if (k.b < 0) return false;
   }
-  // what follows is the same in all lanes: kept in scalar registers, so that page tables are read through the scalar cache
-  k.b = __builtin_amdgcn_readfirstlane(k.b);
-  k.hk = __builtin_amdgcn_readfirstlane(hk);
+  b = __builtin_amdgcn_readfirstlane(b);
   rb = __builtin_amdgcn_readfirstlane(rb);
-  k.s = sequence(a, k.b);
-  k.rows = k.s.rows * a.shared;
-  // the last tile of a sequence first: under a causal border it has the most keys
-  const int of_seq = (k.rows + QB - 1) / QB;
-  if (rb >= of_seq) return false;
-  k.first = __builtin_amdgcn_readfirstlane((of_seq - 1 - rb) * QB);
-  k.held = held_keys(a, k.s.keys);
-  const int last = (k.first + QB < k.rows ? k.first + QB : k.rows) - 1;
-  const int e = seen_keys(a, last / a.shared, k.s.n, k.s.keys), w = seen_keys(a, k.first / a.shared, k.s.n, k.s.keys);
-  k.end = __builtin_amdgcn_readfirstlane(e < k.held ? e : k.held);
-  k.whole = __builtin_amdgcn_readfirstlane(w < k.held ? w : k.held);
+  hk = __builtin_amdgcn_readfirstlane(hk);
+  if (b < 0 || !tile_of<QB>(a, k, b, rb, hk)) return false;
+  make_uniform(k);
   return true;
 }
+
+// sums over a block of 1024 threads of what lies before each; total: of all
+__device__ __forceinline__ int before(int v, int* waves, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) { const int x = __shfl_up(upto, o, 64); upto += lane >= o ? x : 0; }
+  __syncthreads();
+  if (lane == 63) waves[wave] = upto;
+  __syncthreads();
+  int base = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) { base += w < wave ? waves[w] : 0; total += waves[w]; }
+  return base + upto - v;
+}
+// Writes the plan of a call: one block.  UNIT keys are a unit; a tile that sees no key has one.
+template <int QB, int UNIT>
+__global__ __launch_bounds__(1024) void k_paged_plan(const PagedArgs a) {
+  __shared__ int waves[16];
+  int32_t* const units = a.plan;
+  int32_t* const seq = a.plan + a.tiles + 1;
+  int32_t* const rb = seq + a.tiles;
+  int tiles = 0;
+  for (int s0 = 0; s0 < a.n_seqs; s0 += 1024) {
+    const int s = s0 + (int)threadIdx.x;
+    const int n = s < a.n_seqs ? (int)(((int64_t)sequence(a, a.q_start[s], a.q_start[s + 1], 0).rows * a.shared + QB - 1) / QB) : 0;
+    int total;
+    const int at = tiles + before(n, waves, total);
+    for (int i = 0; i < n && at + i < a.tiles; ++i) { seq[at + i] = s; rb[at + i] = i; }
+    tiles += total;
+  }
+  __threadfence_block();
+  __syncthreads();
+  int sum = 0;
+  for (int t0 = 0; t0 < a.tiles; t0 += 1024) {
+    const int t = t0 + (int)threadIdx.x;
+    int n = 0;
+    if (t < a.tiles) {
+      if (t >= tiles) seq[t] = -1;
+      Block k;
+      if (t < tiles && tile_of<QB>(a, k, seq[t], rb[t], 0)) n = k.end > 0 ? (k.end + UNIT - 1) / UNIT : 1;
+    }
+    int total;
+    const int at = sum + before(n, waves, total);
+    if (t < a.tiles) units[t] = at;
+    sum += total;
+  }
+  if (threadIdx.x == 0) units[a.tiles] = sum;
+}
+
+// The work of one block, piece by piece: a tile's keys [k0, k1) with a head.
+struct Piece { Block b; int k0, k1, slot; };   // slot: of the partial result, or -1: these are all of the tile's keys
+// run g of a.runs begins at unit first_of(g) of `all`; run_of(x) is the one that unit x lies in
+__device__ __forceinline__ int64_t first_of(const PagedArgs& a, int g, int64_t all) { return g * all / a.runs; }
+__device__ __forceinline__ int run_of(const PagedArgs& a, int64_t x, int64_t all) { return (int)(((x + 1) * a.runs - 1) / all); }
+template <int QB, int UNIT, bool PLAN> struct Walk {
+  int id;                                 // the block's number
+  int64_t x, x1;                          // with a plan: units to do
+  __device__ __forceinline__ Walk(const PagedArgs& a, int block) : id(block), x(0), x1(0) {
+    if constexpr (PLAN) {
+      const int64_t all = (int64_t)uniform_i32(a.plan + a.tiles) * a.hk;
+      x = first_of(a, id, all);
+      x1 = first_of(a, id + 1, all);
+    }
+  }
+  __device__ __forceinline__ bool next(const PagedArgs& a, Piece& p) {
+    if constexpr (!PLAN) {                                    // one piece
+      const int part = __builtin_amdgcn_readfirstlane(id % a.parts), at = id / a.parts;
+      p.slot = a.parts > 1 ? id : -1;
+      if (!locate<QB>(a, at % a.tiles, at / a.tiles, p.b)) return false;
+      p.k0 = part * a.part_keys;
+      p.k1 = p.b.end < p.k0 + a.part_keys || a.parts == 1 ? p.b.end : p.k0 + a.part_keys;
+      return p.k0 < p.k1 || part == 0;
+    } else {
+      if (x >= x1) return false;
+      const int of_head = uniform_i32(a.plan + a.tiles), hk = (int)(x / of_head), r = (int)(x - (int64_t)hk * of_head), lane = threadIdx.x & 63;
+      // the last tile that begins at r or before, 64 of them at a look
+      int lo = 0, hi = a.tiles;
+      while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+        const int n = __popcll(__ballot(at < hi && a.plan[at < hi ? at : lo] <= r));
+        lo += (n - 1) * step;
+        hi = lo + step < hi ? lo + step : hi;
+      }
+      lo = __builtin_amdgcn_readfirstlane(lo);
+      const int u0 = r - uniform_i32(a.plan + lo), units = uniform_i32(a.plan + lo + 1) - uniform_i32(a.plan + lo);
+      const int n = units - u0 < x1 - x ? units - u0 : (int)(x1 - x);
+      x += n;
+      if (!locate<QB>(a, lo, hk, p.b)) return false;            // never: only tiles that are there have units
+      p.k0 = __builtin_amdgcn_readfirstlane(u0 * UNIT);
+      const int k1 = (u0 + n) * UNIT;
+      p.k1 = __builtin_amdgcn_readfirstlane(k1 < p.b.end ? k1 : p.b.end);
+      p.slot = __builtin_amdgcn_readfirstlane(u0 == 0 && n == units ? -1 : 2 * id + (u0 == 0));
+      return true;
+    }
+  }
+};
 // what a row of the block sees; 0 beyond the sequence's rows
 __device__ __forceinline__ int row_end(const PagedArgs& a, const Block& k, int row) {
   if (row >= k.rows) return 0;
@@ -186,13 +310,13 @@ __device__ __forceinline__ float over_lanes(float v) { v += __shfl_xor(v, 16, 64
 __device__ __forceinline__ void store_four(float* p, f32x4 v) { *(f32x4*)p = v; }
 __device__ __forceinline__ void store_four(bf16_t* p, f32x4 v) { *(uint2*)p = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
 
-// The end of a block whose four wavefronts have the same NT * 16 rows and keys of their own: joined 16 rows at a time, every wavefront's m and l and its
-// O^T by rows, added up in wavefront order at the common reference.  smem: 4 * 16 * (2 + HD + 4) floats, which every wavefront is done with.
-template <typename T, int HD, int NT>
-__device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, float* smem, const Soft (&z)[NT], const f32x4 (&o)[HD / 16][NT], int wave, int lane) {
+// The end of a block whose W wavefronts have the same NT * 16 rows and keys of their own: joined 16 rows at a time, every wavefront's m and l and its
+// O^T by rows, added up in wavefront order at the common reference.  smem: W * 16 * (2 + HD + 4) floats, which every wavefront is done with.
+template <typename T, int HD, int NT, int W>
+__device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, float* smem, const Soft (&z)[NT], const f32x4 (&o)[HD / 16][NT], int slot, int wave, int lane) {
   constexpr int OS = HD + 4, QB = NT * 16;
-  float* const ml = smem;                                    // [4][16][2]
-  float* const os = ml + 4 * 16 * 2;                         // [4][16][OS]
+  float* const ml = smem;                                    // [W][16][2]
+  float* const os = ml + W * 16 * 2;                         // [W][16][OS]
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (b.first + t * 16 >= b.rows) break;
@@ -202,25 +326,25 @@ __device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, f
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) *(f32x4*)(os + (wave * 16 + (lane & 15)) * OS + d * 16 + (lane >> 4) * 4) = o[d][t];
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * (HD / 4); i += 256) {
+    for (int i = threadIdx.x; i < 16 * (HD / 4); i += W * 64) {
       const int r = i / (HD / 4), c = i % (HD / 4) * 4, row = t * 16 + r;
       if (b.first + row >= b.rows) continue;
       float m = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
+      for (int w = 0; w < W; ++w) m = fmaxf(m, ml[(w * 16 + r) * 2]);
       const float ref = m == -INFINITY ? 0.f : m;
       float l = 0.f;
       f32x4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - ref);
         l += ml[(w * 16 + r) * 2 + 1] * f;
         v += *(const f32x4*)(os + (w * 16 + r) * OS + c) * f;
       }
-      if (a.parts == 1) {
+      if (slot < 0) {
         store_four((T*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c, v * inverse(l));
       } else {
-        float* const ps = a.partial + (size_t)blockIdx.x * (QB * (2 + HD));
+        float* const ps = a.partial + (size_t)slot * (QB * (2 + HD));
         if (c == 0) { ps[row] = m; ps[QB + row] = l; }
         *(f32x4*)(ps + 2 * QB + row * HD + c) = v;
       }
@@ -235,16 +359,31 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
   const int id = blockIdx.x / (QB / ROWS), row = blockIdx.x % (QB / ROWS) * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
   Block b;
   if (!locate<QB>(a, id % a.tiles, id / a.tiles, b) || b.first + row >= b.rows) return;
-  int parts = (int)(((int64_t)b.end + a.part_keys - 1) / a.part_keys);
-  if (parts < 1) parts = 1;                                  // the first range is always there
-  const float* const ps = a.partial + (size_t)id * a.parts * (QB * (2 + HD));
+  int parts, first;                                          // partial results, and the slot of the first;
+  if (a.plan) {
+    const int tile = id % a.tiles, of_head = uniform_i32(a.plan + a.tiles);
+    const int64_t all = (int64_t)of_head * a.hk, x = (int64_t)(id / a.tiles) * of_head + uniform_i32(a.plan + tile);
+    const int g = run_of(a, x, all);
+    parts = run_of(a, (int64_t)(id / a.tiles) * of_head + uniform_i32(a.plan + tile + 1) - 1, all) - g + 1;
+    if (parts < 2) return;                                   // one run had all of it
+    first = 2 * g + 1;
+  } else {
+    parts = (int)(((int64_t)b.end + a.part_keys - 1) / a.part_keys);
+    if (parts < 1) parts = 1;                                // the first range is always there
+    first = id * a.parts;
+  }
+  auto at = [&](int i) __attribute__((always_inline)) {
+    return a.partial + (size_t)(a.plan && i > 0 ? first - 1 + 2 * i : first + i) * (QB * (2 + HD));
+  };
   float m = -INFINITY;
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, ps[(size_t)i * (QB * (2 + HD)) + row]);
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, at(i)[row]);
   const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int i = 0; i < parts; ++i) {
-    const float* const p = ps + (size_t)i * (QB * (2 + HD));
+    const float* const p = at(i);
     const float f = __builtin_amdgcn_exp2f(p[row] - ref);
     l += p[QB + row] * f;
     v += *(const f32x4*)(p + 2 * QB + row * HD + c) * f;

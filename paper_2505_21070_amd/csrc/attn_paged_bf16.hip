@@ -78,11 +78,19 @@ template <int HD, int TK, int W, bool CODES> struct Carry {
   typedef typename std::conditional<LB == 16, u32x4, u32x2>::type Raw;
   Raw raw[N];
   uint32_t byte[CODES ? N : 1];
-  // keys key0 .. of the block's sequence; keys_or_values: rows between a head's keys and its values
-  __device__ __forceinline__ void load(const PagedArgs& a, const Block& b, int key0, int64_t to_values, int w, int lane) {
+  // where the trips' rows lie in the pages, for keys key0 .. of the block's sequence: uniform
+  struct Rows { int64_t at[N]; };
+  static __device__ __forceinline__ Rows rows(const PagedArgs& a, const Block& b, int key0, int w) {
+    Rows r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.at[i] = page_row(a, b, key0 + (i * W + w) * RW);
+    return r;
+  }
+  // to_values: rows between a head's keys and its values
+  __device__ __forceinline__ void load(const PagedArgs& a, const Rows& rows, int64_t to_values, int lane) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t row = page_row(a, b, key0 + (i * W + w) * RW) + to_values;
+      const int64_t row = rows.at[i] + to_values;
       raw[i] = *(const Raw*)((const char*)a.data + row * ROW + lane * LB);
       if constexpr (CODES) byte[i] = (a.scales + row)[lane / (ROW / LB)];
     }
@@ -247,44 +255,52 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
   }
 }
 
-// Few rows: NT * 16 of them, four wavefronts that deal the block's keys out in tiles of 32 (wavefront w: tiles w, w + 4, ...), each through its own piece of
-// LDS, the next tile on its way in registers; nobody waits for anybody until the four results are joined in LDS, in wavefront order.  Two
-// blocks to a CU keep 128 KB (codes: 64 KB) under way.  What bounds it: memory.
-template <int HD, int NT, bool CODES>
-__global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
+// Few rows: NT * 16 of them, W wavefronts that deal the block's keys out in tiles of 32 (wavefront w: tiles w, w + W, ...), each through its own piece of
+// LDS, the next tile on its way in registers; nobody waits for anybody until the results are joined in LDS, in wavefront order.  W = 4: two blocks to a
+// CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory.  W = 8: short sequences, bound by latency, one block each.
+template <int HD, int NT, int W, bool CODES, bool PLAN>
+__global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
   constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
-  __shared__ uint4 smem[4 * 2 * TILE];
-  static_assert(sizeof(smem) >= sizeof(float) * 4 * 16 * (2 + HD + 4), "join_waves");
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x % a.parts), id = blockIdx.x / a.parts;
-  Block b;
-  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b)) return;
-  const int k0 = part * a.part_keys, k1 = b.end < k0 + a.part_keys || a.parts == 1 ? b.end : k0 + a.part_keys;
-  if (k0 >= k1 && part > 0) return;
-  bf16x8 qf[NT][HD / 32];
-  int end[NT];
-  load_queries<HD, NT>(a, b, b.first, qf, end, lane);
+  __shared__ uint4 smem[W * 2 * TILE];
+  static_assert(sizeof(smem) >= sizeof(float) * W * 16 * (2 + HD + 4), "join_waves");
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t kt = lds_address(smem) + wave * 2 * TILE * 16, vt = kt + TILE * 16;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
-  Soft z[NT];
-  f32x4 o[HD / 16][NT];
+  Walk<QB, 128, PLAN> walk(a, blockIdx.x);
+  Piece p;
+  if (!walk.next(a, p)) return;
+  do {
+    if constexpr (PLAN) __syncthreads();                     // the piece before is done with LDS
+    const int lane = fresh_lane();
+    const Block& b = p.b;
+    bf16x8 qf[NT][HD / 32];
+    int end[NT];
+    load_queries<HD, NT>(a, b, b.first, qf, end, lane);
+    Soft z[NT];
+    f32x4 o[HD / 16][NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    z[t] = Soft{-INFINITY, 0.f};
+    for (int t = 0; t < NT; ++t) {
+      z[t] = Soft{-INFINITY, 0.f};
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  Carry<HD, 32, 1, CODES> ck, cv;
-  int key = k0 + wave * 32;
-  if (key < k1) { ck.load(a, b, key, 0, 0, lane); cv.load(a, b, key, to_values, 0, lane); }
-  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
-  for (; key < k1; key += 128) {
-    ck.template store<false>(kt, 0, lane);
-    cv.template store<true>(vt, 0, lane);
-    if (key + 128 < k1) { ck.load(a, b, key + 128, 0, 0, lane); cv.load(a, b, key + 128, to_values, 0, lane); }
-    step<HD, KT, NT>(a, b, kt, vt, qf, key, key + 32 > b.whole || gaps, end, gaps, z, o, lane);
-  }
-  join_waves<bf16_t, HD, NT>(a, b, (float*)smem, z, o, wave, lane);
+      for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    Carry<HD, 32, 1, CODES> ck, cv;
+    int key = p.k0 + wave * 32;
+    auto load = [&](int at) __attribute__((always_inline)) {
+      const auto rows = ck.rows(a, b, at, 0);
+      ck.load(a, rows, 0, lane);
+      cv.load(a, rows, to_values, lane);
+    };
+    if (key < p.k1) load(key);
+    const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1));
+    for (; key < p.k1; key += W * 32) {
+      ck.template store<false>(kt, 0, lane);
+      cv.template store<true>(vt, 0, lane);
+      if (key + W * 32 < p.k1) load(key + W * 32);
+      step<HD, KT, NT>(a, b, kt, vt, qf, key, key + 32 > b.whole || gaps, end, gaps, z, o, lane);
+    }
+    join_waves<bf16_t, HD, NT, W>(a, b, (float*)smem, z, o, p.slot, wave, lane);
+  } while (PLAN && walk.next(a, p));
 }
 
 // Many rows: eight wavefronts of 32 rows (two columns of 16), key tiles of 64.  KG = 1: all share every tile, a block has 256 rows and its halves are the
@@ -296,23 +312,25 @@ __global__ __launch_bounds__(256, 2) void k_paged_few(const PagedArgs a) {
 // fp32 sums have 8 exponent bits, so nothing is lost until a sum is beyond 2^100; such a block, or one that is not finite, is done again by the
 // classical online softmax (step), which also does the tiles that hold a border.
 // What bounds it: the matrix pipes.
-template <int HD, int KG, bool CODES>
+template <int HD, int KG, bool CODES, bool PLAN>
 __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
   constexpr int KS = HD / 32, DT = HD / 16, TILE = 64 * HD * 2;   // bytes
   constexpr int QG = 8 / KG, QB = QG * 32;   // wavefronts that share a tile; rows per block
   constexpr int NS = KG == 1 ? 3 : 2;        // LDS stages of either
   extern __shared__ uint4 smem[];            // per key group: NS key tiles, NS value tiles
-  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qt = wave % QG, kg = wave / QG;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qt = wave % QG, kg = wave / QG;
   // blocks are handed out to the eight XCDs in turn: each gets a run of tiles, whose neighbours share keys in its L2
-  const int total = a.tiles * a.hk * a.parts, per = (total + 7) >> 3;
+  const int total = PLAN ? a.runs : a.tiles * a.hk * a.parts, per = (total + 7) >> 3;
   const int pid = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per || pid >= total) return;
-  const int part = __builtin_amdgcn_readfirstlane(pid % a.parts), id = pid / a.parts;
-  Block b;
-  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b)) return;
-  const int k0 = part * a.part_keys, k1 = b.end < k0 + a.part_keys || a.parts == 1 ? b.end : k0 + a.part_keys;
-  if (k0 >= k1 && part > 0) return;
+  Walk<QB, KG * 64, PLAN> walk(a, pid);
+  Piece p;
+  if (!walk.next(a, p)) return;
+  do {
+  if constexpr (PLAN) __syncthreads();       // the piece before is done with LDS
+  const int lane = fresh_lane(), lr = lane & 15, lg = lane >> 4;
+  const Block& b = p.b;
+  const int k0 = p.k0, k1 = p.k1;
   bf16x8 qf[2][KS];
   int end[2];
   load_queries<HD, 2>(a, b, b.first + qt * 32, qf, end, lane);
@@ -352,8 +370,9 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
   };
   // tiles past the range: its first one again, never used
   auto key_of_tile = [&](int j) __attribute__((always_inline)) { return (w0 + (j < cw ? j : 0)) * 64; };
-  auto load_k = [&](int j) __attribute__((always_inline)) { ck.load(a, b, key_of_tile(j), 0, qt, lane); };
-  auto load_v = [&](int j) __attribute__((always_inline)) { cv.load(a, b, key_of_tile(j), to_values, qt, lane); };
+  auto rows_of = [&](int j) __attribute__((always_inline)) { return ck.rows(a, b, key_of_tile(j), qt); };
+  auto load_k = [&](const auto& rows) __attribute__((always_inline)) { ck.load(a, rows, 0, lane); };
+  auto load_v = [&](const auto& rows) __attribute__((always_inline)) { cv.load(a, rows, to_values, lane); };
   auto store_k = [&](int j) __attribute__((always_inline)) { ck.template store<false>(kst + (j % NS) * TILE, qt, lane); };
   auto store_v = [&](int j) __attribute__((always_inline)) { cv.template store<true>(vst + (j % NS) * TILE, qt, lane); };
   // keys of tile j at channels ks * 32 ..; the g-th four of the values' tiles (32-key half f / DT, channels f % DT * 16 ..)
@@ -393,11 +412,15 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
   int done = 0;                              // whole tiles that are in the sums
   if (nw > 0) {
     // tiles 0 and 1 of either, and keys of tile 2, one behind the other; then the first scores, their maximum, their weights
-    load_k(0); load_v(0);
+    auto rows = rows_of(0);
+    load_k(rows); load_v(rows);
+    rows = rows_of(1);
     store_k(0); store_v(0);
-    load_k(1); load_v(1);
+    load_k(rows); load_v(rows);
+    rows = rows_of(2);
     store_k(1); store_v(1);
-    load_k(2); load_v(2);
+    load_k(rows); load_v(rows);
+    rows = rows_of(3);
     turn();
     static_for<KS>([&](auto k_) __attribute__((always_inline)) { read_keys(0, k_); score_step(k_); });
 #pragma unroll
@@ -406,7 +429,7 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
     read_keys(1, I0{}); read_keys(1, I1{});
     turn();
     store_k(2);
-    load_k(3);
+    load_k(rows);
     turn();
     if (wave >= 4) turn();                   // the second half starts half a turn later
     for (int j = 0; j < nw - 1; ++j) {
@@ -415,6 +438,8 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
         turn();
         continue;
       }
+      const auto rows_v = rows;              // the pages' table is read a turn ahead of the rows
+      rows = rows_of(j + 4);
       asm volatile("" : "+v"(klane), "+v"(vlane));   // a dozen addresses made of them each time, not kept in registers that the loop has none of
       __builtin_amdgcn_s_setprio(1);
       static_for<KS>([&](auto k_) __attribute__((always_inline)) {
@@ -440,8 +465,8 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
       store_k(j + 3);
       store_v(j + 2);
       __builtin_amdgcn_sched_barrier(0);
-      load_k(j + 4);
-      load_v(j + 3);
+      load_v(rows_v);
+      load_k(rows);
       __builtin_amdgcn_sched_barrier(0);
       weights();
       turn();
@@ -460,7 +485,10 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
   const int again = done ? 0 : nw;
   auto tile_at = [&](int j) __attribute__((always_inline)) { return j < again ? (j < cw ? w0 + j : -1) : j - again < cb ? b0 + j - again : -1; };
   int tile = tile_at(0);
-  auto load_both = [&](int at) __attribute__((always_inline)) { ck.load(a, b, at * 64, 0, qt, lane); cv.load(a, b, at * 64, to_values, qt, lane); };
+  auto load_both = [&](int at) __attribute__((always_inline)) {
+    const auto rows = ck.rows(a, b, at * 64, qt);
+    load_k(rows); load_v(rows);
+  };
   if (tile >= 0) load_both(tile);
   for (int j = 0; j < again + nb; ++j) {
     const int next = tile_at(j + 1);
@@ -483,7 +511,7 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
         for (int t = 0; t < 2; ++t) xch[(1 + 2 * d + t) * 64] = make_float4(o[d][t][0], o[d][t][1], o[d][t][2], o[d][t][3]);
     }
     __syncthreads();
-    if (kg == 1) return;
+    if (kg == 1) continue;
     const float4 ml = xch[0];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -498,8 +526,8 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
       }
     }
   }
-  if (a.parts > 1) {
-    float* const ps = a.partial + (size_t)pid * (QB * (2 + HD));
+  if (p.slot >= 0) {
+    float* const ps = a.partial + (size_t)p.slot * (QB * (2 + HD));
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int row = qt * 32 + t * 16 + lr;
@@ -526,19 +554,20 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
     const uint4* const stg16 = (const uint4*)stg;
 #pragma unroll
     for (int it = 0; it < 32 / RPI; ++it) {
-      const int row = it * RPI + lane / CPR, p = lane % CPR;
-      uint4 dv = stg16[row * CPR + p];
-      // units 2p and 2p+1 of the exchanged row are the halves of chunk p ^ (exchange >> 1), the other way round for odd rows
+      const int row = it * RPI + lane / CPR, ch = lane % CPR;
+      uint4 dv = stg16[row * CPR + ch];
+      // units 2 ch and 2 ch + 1 of the exchanged row are the halves of chunk ch ^ (exchange >> 1), the other way round for odd rows
       if (row & 1) dv = make_uint4(dv.z, dv.w, dv.x, dv.y);
-      const int c = p ^ ((row & (UPR - 1)) >> 1), r = b.first + qt * 32 + row;
+      const int c = ch ^ ((row & (UPR - 1)) >> 1), r = b.first + qt * 32 + row;
       if (r < b.rows) *(uint4*)((bf16_t*)a.out + row_at(a, b, r, a.o_ts, a.o_hs) + c * 8) = dv;
     }
   }
+  } while (PLAN && walk.next(a, p));
 }
 
-// What a call takes: rows per block, and ranges that a block's keys are cut into
-struct Route { int qb, parts, part_keys; int64_t tiles, tiles_of_seq; };
-Route route(const PagedArgs& a) {
+// What a call takes: rows per block, and ranges that a block's keys are cut into, or a plan of equal runs
+struct Route { int qb, parts, part_keys, runs; int64_t tiles, tiles_of_seq; };
+Route route(const PagedArgs& a, int head_dim) {
   Route r{};
   const int64_t rows = (int64_t)a.max_q * a.shared;          // of a sequence, at most
   auto tiles = [&](int qb) {
@@ -546,74 +575,89 @@ Route route(const PagedArgs& a) {
     return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
   };
   const int64_t keys = a.max_kv;
+  r.parts = 1;
+  r.part_keys = (int)keys;
   if (rows <= 32) {
     r.qb = rows <= 16 ? 16 : 32;
     r.tiles = tiles(r.qb);
-    const int64_t blocks = r.tiles * a.hk;
-    // one range for as many blocks as keep the chip full several times over; none shorter than two trips of the four wavefronts
-    int64_t parts = ((a.n_seqs > 1 ? 8192 : 2048) + blocks - 1) / blocks;
-    if (parts > (keys + 255) / 256) parts = (keys + 255) / 256;
-    if (parts > 256) parts = 256;
-    if (parts < 1) parts = 1;
-    r.part_keys = (int)(((keys + parts - 1) / parts + 127) / 128 * 128);
+    // Two blocks to a CU, with equal runs.  Not for sequences up to 2048 keys, whose one block each takes about as long as a plan and a join, nor for
+    // very many.
+    const int64_t units = (keys + 127) / 128, blocks = r.tiles * a.hk;
+    if (units > 16 && blocks < 8192) r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
   } else {
     // Blocks of either shape, one to a CU; a step of 64 keys x 256 rows, or 2 x 64 keys x 128 rows, is 1.7 us at heads of 128, and what a
-    // block does around its steps about 5 of them.  One sequence, seen whole: rounds of 256 blocks.  Sequences of several lengths and causal borders: all the work, with
-    // ranges of half the bound on average, and one block's at the end.  Ranges cost a launch and the traffic of partial results (7 MB a step).
+    // block does around its steps about 5 of them.  In rounds of 256 blocks, with ranges that fill the last round; or in 256 equal runs, which cost a plan, and on average one
+    // more tile begun and one more joined.  Partial results are written and read: 7 MB a step.  Sequences of several lengths and causal
+    // borders: half the bound's keys on average, and in rounds a block with all of them at the end.
     const bool even = a.n_seqs == 1 && a.group == 0;
     int64_t best = INT64_MAX;
     const int64_t key_tiles = (keys + 63) / 64;
-    for (int qb = 256; qb >= 128; qb -= 128)
-      for (int64_t parts = 1; parts <= 16; ++parts) {
-        const int64_t n = tiles(qb), blocks = n * a.hk * parts, of_part = (key_tiles + parts - 1) / parts, steps = qb == 256 ? of_part : (of_part + 1) / 2;
+    for (int qb = 256; qb >= 128; qb -= 128) {
+      const int64_t n = tiles(qb), part_cost = 256 * qb * (head_dim + 2) * 8;
+      auto steps_of = [&](int64_t of_part) { return qb == 256 ? of_part : (of_part + 1) / 2; };
+      for (int64_t parts = 1; parts <= 32; ++parts) {
+        const int64_t blocks = n * a.hk * parts, of_part = (key_tiles + parts - 1) / parts, steps = steps_of(of_part);
         if (parts > 1 && of_part < 8) break;
         const int64_t work = even ? (blocks + 255) / 256 * (steps + 5) : blocks * (steps / 2 + 5) / 256 + steps + 5;
-        const int64_t cost = work + (parts > 1 ? 4 + blocks * qb * 520 / 7000000 : 0);
-        if (cost < best) { best = cost; r.qb = qb; r.tiles = n; r.part_keys = (int)(of_part * 64); }
+        const int64_t cost = work + (parts > 1 ? 4 + blocks * part_cost / 256 / 7000000 : 0);
+        if (cost < best) { best = cost; r.qb = qb; r.tiles = n; r.parts = (int)parts; r.part_keys = (int)(of_part * 64); r.runs = 0; }
       }
+      const int64_t units = n * a.hk * steps_of(key_tiles) / (even ? 1 : 2), cost = units / 256 + n * a.hk * 5 / 256 + 12 + 2 * part_cost / 7000000;
+      if (units >= 256 * 4 && n * steps_of(key_tiles) < 0x7fffffff && cost < best) {
+        best = cost; r.qb = qb; r.tiles = n; r.parts = 1; r.part_keys = (int)keys; r.runs = 256;
+      }
+    }
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
-  r.parts = r.part_keys > 0 ? (int)((keys + r.part_keys - 1) / r.part_keys) : 1;
-  if (r.parts < 1) r.parts = 1;
   return r;
 }
 
-template <int HD, int NT> void few(const PagedArgs& a, bool codes, hipStream_t st) {
-  const unsigned g = (unsigned)((int64_t)a.tiles * a.hk * a.parts);
-  if (codes) k_paged_few<HD, NT, true><<<g, 256, 0, st>>>(a); else k_paged_few<HD, NT, false><<<g, 256, 0, st>>>(a);
+template <int HD, int NT, bool CODES> void few(const PagedArgs& a, hipStream_t st) {
+  constexpr int QB = NT * 16;
+  const int64_t blocks = (int64_t)a.tiles * a.hk;
+  if (a.plan) {
+    k_paged_plan<QB, 128><<<1, 1024, 0, st>>>(a);
+    k_paged_few<HD, NT, 4, CODES, true><<<(unsigned)a.runs, 256, 0, st>>>(a);
+  } else if (blocks <= 256 && a.max_kv > 128) {
+    k_paged_few<HD, NT, 8, CODES, false><<<(unsigned)blocks, 512, 0, st>>>(a);
+  } else {
+    k_paged_few<HD, NT, 4, CODES, false><<<(unsigned)blocks, 256, 0, st>>>(a);
+  }
 }
-template <int HD, int KG, bool CODES> void turns_of(const PagedArgs& a, hipStream_t st) {
+template <int HD, int KG, bool CODES, bool PLAN> void turns_of(const PagedArgs& a, int64_t total, hipStream_t st) {
   constexpr int tile = 64 * HD * 2, lds = KG == 1 ? 6 * tile : 8 * tile;
   static std::atomic<uint64_t> done;
-  allow_dynamic_lds((const void*)k_paged_turns<HD, KG, CODES>, lds, done);
-  const int64_t total = (int64_t)a.tiles * a.hk * a.parts;
-  k_paged_turns<HD, KG, CODES><<<(unsigned)((total + 7) / 8 * 8), 512, lds, st>>>(a);
+  allow_dynamic_lds((const void*)k_paged_turns<HD, KG, CODES, PLAN>, lds, done);
+  k_paged_turns<HD, KG, CODES, PLAN><<<(unsigned)((total + 7) / 8 * 8), 512, lds, st>>>(a);
 }
-template <int HD, int KG> void turns(const PagedArgs& a, bool codes, hipStream_t st) {
-  if (codes) turns_of<HD, KG, true>(a, st); else turns_of<HD, KG, false>(a, st);
-}
-template <int HD> void launch(const PagedArgs& a, int qb, bool codes, hipStream_t st) {
-  const unsigned joins = (unsigned)((int64_t)a.tiles * a.hk * qb * (HD / 4) / 256);
-  if (qb == 16) {
-    few<HD, 1>(a, codes, st);
-    if (a.parts > 1) k_paged_join<bf16_t, HD, 16><<<joins, 256, 0, st>>>(a);
-  } else if (qb == 32) {
-    few<HD, 2>(a, codes, st);
-    if (a.parts > 1) k_paged_join<bf16_t, HD, 32><<<joins, 256, 0, st>>>(a);
-  } else if (qb == 128) {
-    turns<HD, 2>(a, codes, st);
-    if (a.parts > 1) k_paged_join<bf16_t, HD, 128><<<joins, 256, 0, st>>>(a);
+template <int HD, int KG, bool CODES> void turns(const PagedArgs& a, hipStream_t st) {
+  if (a.plan) {
+    k_paged_plan<256 / KG, KG * 64><<<1, 1024, 0, st>>>(a);
+    turns_of<HD, KG, CODES, true>(a, a.runs, st);
   } else {
-    turns<HD, 1>(a, codes, st);
-    if (a.parts > 1) k_paged_join<bf16_t, HD, 256><<<joins, 256, 0, st>>>(a);
+    turns_of<HD, KG, CODES, false>(a, (int64_t)a.tiles * a.hk * a.parts, st);
   }
+}
+template <int HD, int QB> void join(const PagedArgs& a, hipStream_t st) {
+  if (a.plan || a.parts > 1) k_paged_join<bf16_t, HD, QB><<<(unsigned)((int64_t)a.tiles * a.hk * QB * (HD / 4) / 256), 256, 0, st>>>(a);
+}
+template <int HD, bool CODES> void launch(const PagedArgs& a, int qb, hipStream_t st) {
+  if (qb == 16) { few<HD, 1, CODES>(a, st); join<HD, 16>(a, st); }
+  else if (qb == 32) { few<HD, 2, CODES>(a, st); join<HD, 32>(a, st); }
+  else if (qb == 128) { turns<HD, 2, CODES>(a, st); join<HD, 128>(a, st); }
+  else { turns<HD, 1, CODES>(a, st); join<HD, 256>(a, st); }
 }
 
 }  // namespace
 
 size_t launch_attn_paged_bf16(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st) {
-  const Route r = route(a);
-  a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys;
-  if (go) { if (head_dim == 128) launch<128>(a, r.qb, codes, st); else launch<64>(a, r.qb, codes, st); }
-  return r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts * ((size_t)r.qb * (2 + head_dim) * sizeof(float)) : 0;
+  const Route r = route(a, head_dim);
+  a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys; a.runs = r.runs;
+  const size_t partial = (r.runs ? (size_t)r.runs * 2 : r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts : 0) * r.qb * (2 + head_dim) * sizeof(float);
+  if (go) {
+    a.plan = r.runs ? (int32_t*)((char*)a.partial + partial) : nullptr;
+    if (head_dim == 128) { if (codes) launch<128, true>(a, r.qb, st); else launch<128, false>(a, r.qb, st); }
+    else { if (codes) launch<64, true>(a, r.qb, st); else launch<64, false>(a, r.qb, st); }
+  }
+  return partial + (r.runs ? (3 * (size_t)r.tiles + 1) * sizeof(int32_t) : 0);
 }

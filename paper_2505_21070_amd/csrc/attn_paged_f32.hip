@@ -151,11 +151,11 @@ __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
   constexpr int JOIN = QG == 1 ? 4 * 16 * 2 + 4 * 16 * RS : 0, SIZE = KG * 2 * TILE;
   __shared__ __align__(16) float smem[SIZE > JOIN ? SIZE : JOIN];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qt = wave % QG, kg = wave / QG;
-  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x % a.parts), id = blockIdx.x / a.parts;
-  Block b;
-  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b)) return;
-  const int k0 = part * a.part_keys, k1 = b.end < k0 + a.part_keys || a.parts == 1 ? b.end : k0 + a.part_keys;
-  if (k0 >= k1 && part > 0) return;
+  Walk<QB, KG * TK, false> walk(a, blockIdx.x);
+  Piece p;
+  if (!walk.next(a, p)) return;
+  const Block& b = p.b;
+  const int k0 = p.k0, k1 = p.k1;
   f32x4 qf[NT][HD / 16], o[HD / 16][NT];
   int end[NT];
   Soft z[NT];
@@ -191,20 +191,20 @@ __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
       const int row = (qt * NT + t) * 16 + (lane & 15);
       const float l = over_lanes(z[t].l);
       if (b.first + row >= b.rows) continue;
-      if (a.parts == 1) {
+      if (p.slot < 0) {
         float* const out = (float*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + (lane >> 4) * 4;
         const float inv = inverse(l);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) *(f32x4*)(out + d * 16) = o[d][t] * inv;
       } else {
-        float* const ps = a.partial + (size_t)blockIdx.x * (QB * (2 + HD));
+        float* const ps = a.partial + (size_t)p.slot * (QB * (2 + HD));
         if (lane < 16) { ps[row] = z[t].m; ps[QB + row] = l; }
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) *(f32x4*)(ps + 2 * QB + row * HD + d * 16 + (lane >> 4) * 4) = o[d][t];
       }
     }
   } else {
-    join_waves<float, HD, NT>(a, b, smem, z, o, wave, lane);
+    join_waves<float, HD, NT, 4>(a, b, smem, z, o, p.slot, wave, lane);
   }
 }
 
