@@ -199,10 +199,10 @@ template <int QB, int UNIT, bool PLAN> struct Walk {
   __device__ __forceinline__ bool next(const PagedArgs& a, Piece& p) {
     if constexpr (!PLAN) {                                    // one piece
       const int part = __builtin_amdgcn_readfirstlane(id % a.parts), at = id / a.parts;
-      p.slot = a.parts > 1 ? id : -1;
       if (!locate<QB>(a, at % a.tiles, at / a.tiles, p.b)) return false;
       p.k0 = part * a.part_keys;
       p.k1 = p.b.end < p.k0 + a.part_keys || a.parts == 1 ? p.b.end : p.k0 + a.part_keys;
+      p.slot = a.parts > 1 && p.b.end > a.part_keys ? id : -1;
       return p.k0 < p.k1 || part == 0;
     } else {
       if (x >= x1) return false;
@@ -365,13 +365,12 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
     const int64_t all = (int64_t)of_head * a.hk, x = (int64_t)(id / a.tiles) * of_head + uniform_i32(a.plan + tile);
     const int g = run_of(a, x, all);
     parts = run_of(a, (int64_t)(id / a.tiles) * of_head + uniform_i32(a.plan + tile + 1) - 1, all) - g + 1;
-    if (parts < 2) return;                                   // one run had all of it
     first = 2 * g + 1;
   } else {
     parts = (int)(((int64_t)b.end + a.part_keys - 1) / a.part_keys);
-    if (parts < 1) parts = 1;                                // the first range is always there
     first = id * a.parts;
   }
+  if (parts < 2) return;                                     // one block had all of it
   auto at = [&](int i) __attribute__((always_inline)) {
     return a.partial + (size_t)(a.plan && i > 0 ? first - 1 + 2 * i : first + i) * (QB * (2 + HD));
   };

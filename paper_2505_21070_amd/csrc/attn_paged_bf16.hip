@@ -303,253 +303,324 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
   } while (PLAN && walk.next(a, p));
 }
 
-// Many rows: eight wavefronts of 32 rows (two columns of 16), key tiles of 64.  KG = 1: all share every tile, a block has 256 rows and its halves are the
-// wavefronts 0-3 and 4-7.  KG = 2: the halves have the same 128 rows and one part of the keys each, with tiles of their own, and meet in LDS at the end.
-// Whole tiles: the two wavefronts of a SIMD (one of each half) take turns, with a barrier at every change: one multiplies, the scores
-// of tile j + 1 and the weighted sum of tile j, and reads tile j's values from LDS between the products; the other turns its scores
-// of tile j + 1 into weights, reads tile j + 2's keys, and moves tiles to come: from registers into LDS (keys of j + 3, values of j + 2), the ones behind
-// them from the pages into registers.  The softmax's reference is fixed to a row's maximum over the first 32 keys: weights (bf16) and
-// fp32 sums have 8 exponent bits, so nothing is lost until a sum is beyond 2^100; such a block, or one that is not finite, is done again by the
-// classical online softmax (step), which also does the tiles that hold a border.
-// What bounds it: the matrix pipes.
-template <int HD, int KG, bool CODES, bool PLAN>
-__global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
-  constexpr int KS = HD / 32, DT = HD / 16, TILE = 64 * HD * 2;   // bytes
-  constexpr int QG = 8 / KG, QB = QG * 32;   // wavefronts that share a tile; rows per block
-  constexpr int NS = KG == 1 ? 3 : 2;        // LDS stages of either
-  extern __shared__ uint4 smem[];            // per key group: NS key tiles, NS value tiles
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qt = wave % QG, kg = wave / QG;
-  // blocks are handed out to the eight XCDs in turn: each gets a run of tiles, whose neighbours share keys in its L2
-  const int total = PLAN ? a.runs : a.tiles * a.hk * a.parts, per = (total + 7) >> 3;
-  const int pid = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || pid >= total) return;
-  Walk<QB, KG * 64, PLAN> walk(a, pid);
-  Piece p;
-  if (!walk.next(a, p)) return;
-  do {
-  if constexpr (PLAN) __syncthreads();       // the piece before is done with LDS
-  const int lane = fresh_lane(), lr = lane & 15, lg = lane >> 4;
-  const Block& b = p.b;
-  const int k0 = p.k0, k1 = p.k1;
-  bf16x8 qf[2][KS];
-  int end[2];
-  load_queries<HD, 2>(a, b, b.first + qt * 32, qf, end, lane);
-  const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
-  // tiles of this range: whole ones from t0 on, then those with a border up to t1; of two key groups each has half of either
-  const int t0 = k0 / 64, t1 = (k1 + 63) / 64;
-  int whole = gaps ? 0 : (b.whole < k1 ? b.whole : k1) / 64 - t0;
-  if (whole < KG) whole = 0;
-  const int n_border = t1 - t0 - whole;
-  const int nw = KG == 2 ? (whole + 1) / 2 : whole, nb = KG == 2 ? (n_border + 1) / 2 : n_border;   // trip counts for everyone
-  const int cw = kg ? whole - nw : nw, cb = kg ? n_border - nb : nb;
-  const int w0 = t0 + (kg ? nw : 0), b0 = t0 + whole + (kg ? nb : 0);
-  const uint32_t kst = lds_address(smem) + kg * 2 * NS * TILE, vst = kst + NS * TILE;
-  uint32_t klane = k_lane<HD>(lane), vlane = v_lane<HD>(lane);
-  const int64_t to_values = (int64_t)a.hk << a.page_shift;
-  Carry<HD, 64, QG, CODES> ck, cv;
+// LDS by typed address.  In the loop over whole tiles, tiles arrive by direct loads while others are read; what says that the two do not meet are the
+// restricted pointers of `round`, without which the compiler has every read of LDS wait for all loads on their way.
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ bf16x8 lds_get(const lds_char* p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return __builtin_bit_cast(bf16x8, *(const __attribute__((address_space(3))) u32x4*)p);
+#else
+  return bf16x8{};
+#endif
+}
+__device__ __forceinline__ bf16x8 lds_get_v(const lds_char* p, int u_bytes) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p));
+  const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p + u_bytes)));
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+#else
+  return bf16x8{};
+#endif
+}
+// this wavefront's LDS traffic is done, and none of what is written before the barrier moves behind it or the other way round
+__device__ __forceinline__ void turn() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
 
-  bf16x8 kf[2][4], vf[2][4];                 // operands two steps of the head dim, two groups of four values' tiles ahead
+// A tile of 64 keys or values on its way from the pages into LDS by direct loads: 64 lanes of 16 bytes a trip, whose places in the rows are
+// exchanged at the source.
+template <int HD, int W> struct Direct {
+  static constexpr int CR = HD / 8, RW = 64 / CR, N = HD / (W * 8);          // chunks and rows of a trip of one wavefront, trips
+  static_assert(N * W * RW == 64 && (W * RW) % 16 == 0, "the same exchange in every trip");
+  uint32_t k, v;                             // this lane's place in a trip's rows
+  __device__ __forceinline__ Direct(int w, int lane) {
+    const int row = w * RW + lane / CR, c = lane % CR;
+    k = (lane / CR) * HD * 2 + ((c ^ k_swizzle<HD>(row)) * 16);
+    v = (lane / CR) * HD * 2 + ((c ^ v_swizzle<HD>(row)) * 16);
+  }
+  template <typename Rows> static __device__ __forceinline__ void load(const PagedArgs& a, const Rows& rows, int64_t to_values, uint32_t place, lds_char* tile, int w) {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const char* const from = (const char*)a.data + (rows.at[i] + to_values) * (HD * 2);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7fffffff, 0x00020000), (lds_void_t*)(tile + (i * W + w) * 1024), 16, place, 0, 0, 0);
+    }
+#endif
+  }
+};
+
+// What a wavefront of k_paged_turns has in registers through its whole tiles.
+template <int HD> struct State {
+  static constexpr int KS = HD / 32, DT = HD / 16;
+  bf16x8 qf[2][KS], kf[2][4], vf[2][4];      // operands two steps of the head dim, two groups of four values' tiles ahead
   f32x4 o[DT][2], sc[2][4];
   uint4 pf[2][2];
   Soft z[2];
-  auto clear = [&]() __attribute__((always_inline)) {
+  float ref[2];
+  uint32_t klane, vlane;
+  // keys at channels ks * 32 ..; the g-th four of the values' tiles (32-key half f / DT, channels f % DT * 16 ..)
+  template <int ks> __device__ __forceinline__ void read_keys(const lds_char* tile) {
+    const lds_char* const p = tile + (klane ^ (ks * 64));
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) kf[ks & 1][kt] = lds_get(p + kt * 16 * HD * 2);
+  }
+  template <int g> __device__ __forceinline__ void read_values(const lds_char* tile) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vf[g & 1][i] = lds_get_v(tile + (vlane ^ ((g * 4 + i) % DT * 32)) + (g * 4 + i) / DT * 32 * HD * 2, 16 * HD * 2);
+  }
+  template <int ks> __device__ __forceinline__ void score_step() {
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) sc[t][kt] = mfma(kf[ks & 1][kt], qf[t][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[t][kt]);
+  }
+  template <int g> __device__ __forceinline__ void sum_step() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) o[(g * 4 + i) % DT][t] = mfma(vf[g & 1][i], __builtin_bit_cast(bf16x8, pf[t][(g * 4 + i) / DT]), o[(g * 4 + i) % DT][t]);
+  }
+  __device__ __forceinline__ void weights(float scale) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) weigh<4>(sc[t], scale, ref[t], z[t].l, pf[t]);
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       z[t] = Soft{-INFINITY, 0.f};
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-  };
-  // LDS traffic of this wavefront is done before the barrier, and none of what follows is moved ahead of it
-  auto turn = [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  // tiles past the range: its first one again, never used
-  auto key_of_tile = [&](int j) __attribute__((always_inline)) { return (w0 + (j < cw ? j : 0)) * 64; };
-  auto rows_of = [&](int j) __attribute__((always_inline)) { return ck.rows(a, b, key_of_tile(j), qt); };
-  auto load_k = [&](const auto& rows) __attribute__((always_inline)) { ck.load(a, rows, 0, lane); };
-  auto load_v = [&](const auto& rows) __attribute__((always_inline)) { cv.load(a, rows, to_values, lane); };
-  auto store_k = [&](int j) __attribute__((always_inline)) { ck.template store<false>(kst + (j % NS) * TILE, qt, lane); };
-  auto store_v = [&](int j) __attribute__((always_inline)) { cv.template store<true>(vst + (j % NS) * TILE, qt, lane); };
-  // keys of tile j at channels ks * 32 ..; the g-th four of the values' tiles (32-key half f / DT, channels f % DT * 16 ..)
-  auto read_keys = [&](int j, auto ks_) __attribute__((always_inline)) {
-    constexpr int ks = decltype(ks_)::value;
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt) kf[ks & 1][kt] = read_k<HD>(kst + (j % NS) * TILE, klane, kt, ks);
-  };
-  auto read_values = [&](int j, auto g_) __attribute__((always_inline)) {
-    constexpr int g = decltype(g_)::value;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) vf[g & 1][i] = read_v<HD>(vst + (j % NS) * TILE, vlane, (g * 4 + i) / DT, (g * 4 + i) % DT);
-  };
-  auto score_step = [&](auto ks_) __attribute__((always_inline)) {
-    constexpr int ks = decltype(ks_)::value;
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) sc[t][kt] = mfma(kf[ks & 1][kt], qf[t][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[t][kt]);
-  };
-  auto sum_step = [&](auto g_) __attribute__((always_inline)) {
-    constexpr int g = decltype(g_)::value;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) o[(g * 4 + i) % DT][t] = mfma(vf[g & 1][i], __builtin_bit_cast(bf16x8, pf[t][(g * 4 + i) / DT]), o[(g * 4 + i) % DT][t]);
-  };
-  typedef std::integral_constant<int, 0> I0;
-  typedef std::integral_constant<int, 1> I1;
-  float ref[2];
-  auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) weigh<4>(sc[t], a.scale, ref[t], z[t].l, pf[t]);
-  };
+  }
+};
 
-  clear();
-  int done = 0;                              // whole tiles that are in the sums
-  if (nw > 0) {
-    // tiles 0 and 1 of either, and keys of tile 2, one behind the other; then the first scores, their maximum, their weights
-    auto rows = rows_of(0);
+// The turn of products: scores of the tile whose keys are at k1 (its first two steps are in kf), weighted sum of the one whose values are at v0
+template <int HD> __device__ __forceinline__ void products(State<HD>& s, const lds_char* k1, const lds_char* v0) {
+  constexpr int KS = HD / 32;
+#ifdef __HIP_DEVICE_COMPILE__
+  asm volatile("" : "+v"(s.klane), "+v"(s.vlane));   // a dozen addresses made of them each time, not kept in registers that the loop has none of
+#endif
+  __builtin_amdgcn_s_setprio(1);
+  static_for<KS>([&](auto k_) __attribute__((always_inline)) {
+    constexpr int ks = decltype(k_)::value;
+    s.template score_step<ks>();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (ks + 2 < KS) s.template read_keys<ks + 2>(k1);
+    else s.template read_values<ks + 2 - KS>(v0);
+    __builtin_amdgcn_sched_barrier(0);
+  });
+  static_for<KS>([&](auto g_) __attribute__((always_inline)) {
+    constexpr int g = decltype(g_)::value;
+    s.template sum_step<g>();
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (g + 2 < KS) s.template read_values<g + 2>(v0);
+    __builtin_amdgcn_sched_barrier(0);
+  });
+  __builtin_amdgcn_s_setprio(0);
+  __builtin_amdgcn_sched_barrier(0);
+}
+// Round j of the loop over whole tiles: the turn of exponentials (weights of tile j + 1, the first keys of tile j + 2), in which `move` sends tiles to come on
+// their way to k_to and v_to; then the turn of products (scores of tile j + 2, weighted sum of tile j + 1).
+template <int HD, typename Move, typename Between>
+__device__ __forceinline__ void round(State<HD>& s, float scale, const lds_char* __restrict__ k2, const lds_char* __restrict__ v1, lds_char* __restrict__ k_to,
+                                      lds_char* __restrict__ v_to, Move&& move, Between&& between) {
+  s.template read_keys<0>(k2);
+  s.template read_keys<1>(k2);
+  __builtin_amdgcn_sched_barrier(0);
+  move(k_to, v_to);
+  __builtin_amdgcn_sched_barrier(0);
+  s.weights(scale);
+  __builtin_amdgcn_sched_barrier(0);
+  between();
+  products(s, k2, v1);
+}
+
+// Many rows: wavefronts of 32 rows (two columns of 16) that share key tiles of 64.  WIDE: eight of them, 256 rows, one block to a CU, whose halves (0-3 and
+// 4-7) are half a round apart, with a barrier at every turn: of the two wavefronts of a SIMD one multiplies while the other does exponentials.
+// Else four, 128 rows, two blocks to a CU, which do the same for each other as it comes, one barrier a round; what a block does before and after its
+// tiles hides behind the other.
+// Rows as they are come by direct loads into LDS (four stages, or two); codes through registers, converted on the way (three, or two).
+// The softmax's reference is fixed to a row's maximum over the first 32 keys: weights (bf16) and fp32 sums have 8 exponent bits, so nothing is lost until
+// a sum is beyond 2^100; such a block, or one that is not finite, is done again by the classical online softmax (step), which also does
+// the tiles that hold a border.
+// What bounds it: the matrix pipes.
+template <int HD, bool WIDE, bool CODES>
+__global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const PagedArgs a) {
+  constexpr int KS = HD / 32, DT = HD / 16, TILE = 64 * HD * 2;   // bytes
+  constexpr int W = WIDE ? 8 : 4, QB = W * 32, NS = WIDE ? (CODES ? 3 : 4) : 2;   // wavefronts, rows of a block, LDS stages of keys and of values
+  extern __shared__ uint4 smem[];            // NS key tiles, NS value tiles
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // blocks are handed out to the eight XCDs in turn: each gets a run of tiles, whose neighbours share keys in its L2
+  const int total = a.tiles * a.hk * a.parts, per = (total + 7) >> 3;
+  const int pid = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || pid >= total) return;
+  Walk<QB, 64, false> walk(a, pid);
+  Piece p;
+  if (!walk.next(a, p)) return;
+  const Block& b = p.b;
+  // tiles of this range: whole ones from t0 on, then those with a border up to t1
+  const int t0 = p.k0 / 64, t1 = (p.k1 + 63) / 64;
+  int whole = (b.whole < p.k1 ? b.whole : p.k1) / 64 - t0;
+  if (whole < 0) whole = 0;
+  bool gaps = false;
+  const uint32_t kst = lds_address(smem), vst = kst + NS * TILE;
+  lds_char* const kst_ = (lds_char*)(lds_void_t*)smem;
+  lds_char* const vst_ = kst_ + NS * TILE;
+  const int64_t to_values = (int64_t)a.hk << a.page_shift;
+  typedef Carry<HD, 64, W, CODES> Registers;
+  Registers ck, cv;
+  typedef Direct<HD, W> Loads;
+  const Loads direct(wave, lane);
+  // tiles past the whole ones: the first again, never used
+  auto rows_of = [&](int j) __attribute__((always_inline)) { return Registers::rows(a, b, (t0 + (j < whole ? j : 0)) * 64, wave); };
+  typedef decltype(rows_of(0)) Rows;
+  auto direct_k = [&](const Rows& rows, lds_char* to) __attribute__((always_inline)) { Loads::load(a, rows, 0, direct.k, to, wave); };
+  auto direct_v = [&](const Rows& rows, lds_char* to) __attribute__((always_inline)) { Loads::load(a, rows, to_values, direct.v, to, wave); };
+  auto load_k = [&](const Rows& rows) __attribute__((always_inline)) { ck.load(a, rows, 0, lane); };
+  auto load_v = [&](const Rows& rows) __attribute__((always_inline)) { cv.load(a, rows, to_values, lane); };
+  auto store_k = [&](int j) __attribute__((always_inline)) { ck.template store<false>(kst + (j % NS) * TILE, wave, lane); };
+  auto store_v = [&](int j) __attribute__((always_inline)) { cv.template store<true>(vst + (j % NS) * TILE, wave, lane); };
+  auto kt = [&](int j) __attribute__((always_inline)) { return kst_ + (j % NS) * TILE; };
+  auto vt = [&](int j) __attribute__((always_inline)) { return vst_ + (j % NS) * TILE; };
+
+  // Round j sends keys of tile j + AHEAD and values of the one before it, whose place in the pages it has from the round before.  Direct loads land a round
+  // later, or (four stages) two; from registers, tiles go into LDS a round later and into the matrix pipe two.
+  constexpr int AHEAD = CODES || WIDE ? 4 : 3;
+  // what the first scores need, on its way before the queries and the look at the pages
+  Rows rows = rows_of(0);
+  bool loaded = p.k0 < p.k1 && (CODES || whole == 0);         // whether `tile`, the next that goes through registers in the end, is in them
+  if (loaded) {
     load_k(rows); load_v(rows);
-    rows = rows_of(1);
-    store_k(0); store_v(0);
-    load_k(rows); load_v(rows);
-    rows = rows_of(2);
-    store_k(1); store_v(1);
-    load_k(rows); load_v(rows);
-    rows = rows_of(3);
-    turn();
-    static_for<KS>([&](auto k_) __attribute__((always_inline)) { read_keys(0, k_); score_step(k_); });
+  } else if (whole > 0) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) z[t].m = ref[t] = maximum<4>(sc[t], 2) * a.scale;
-    weights();
-    read_keys(1, I0{}); read_keys(1, I1{});
+    for (int j = 0; j < AHEAD - 1; ++j) {
+      direct_k(rows, kt(j)); direct_v(rows, vt(j));
+      rows = rows_of(j + 1);
+    }
+    if constexpr (WIDE) direct_k(rows, kt(3));
+  }
+  State<HD> s;
+  int end[2];
+  load_queries<HD, 2>(a, b, b.first + wave * 32, s.qf, end, lane);
+  s.klane = k_lane<HD>(lane);
+  s.vlane = v_lane<HD>(lane);
+  if (__builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1))) { whole = 0; gaps = true; loaded = loaded && CODES; }
+  s.clear();
+  int tile = t0;
+  if (whole > 0) {
+    if constexpr (CODES) {
+      rows = rows_of(1);
+      store_k(0); store_v(0);
+      load_k(rows); load_v(rows);
+      rows = rows_of(2);
+      store_k(1); store_v(1);
+      load_k(rows); load_v(rows);
+      rows = rows_of(3);
+    } else {
+      vm_wait<0>();
+    }
     turn();
-    store_k(2);
-    load_k(rows);
+    static_for<KS>([&](auto k_) __attribute__((always_inline)) {
+      constexpr int ks = decltype(k_)::value;
+      s.template read_keys<ks>(kt(0));
+      s.template score_step<ks>();
+    });
+#pragma unroll
+    for (int t = 0; t < 2; ++t) s.z[t].m = s.ref[t] = maximum<4>(s.sc[t], 2) * a.scale;
+    s.weights(a.scale);
+    s.template read_keys<0>(kt(1));
+    s.template read_keys<1>(kt(1));
     turn();
-    if (wave >= 4) turn();                   // the second half starts half a turn later
-    for (int j = 0; j < nw - 1; ++j) {
-      if (KG == 2 && j >= cw - 1) {          // this key group is a tile shorter: it only keeps step
-        turn();
-        turn();
-        continue;
-      }
-      const auto rows_v = rows;              // the pages' table is read a turn ahead of the rows
-      rows = rows_of(j + 4);
-      asm volatile("" : "+v"(klane), "+v"(vlane));   // a dozen addresses made of them each time, not kept in registers that the loop has none of
-      __builtin_amdgcn_s_setprio(1);
-      static_for<KS>([&](auto k_) __attribute__((always_inline)) {
-        constexpr int ks = decltype(k_)::value;
-        score_step(k_);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (ks + 2 < KS) read_keys(j + 1, std::integral_constant<int, ks + 2>{});
-        else read_values(j, std::integral_constant<int, ks + 2 - KS>{});
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      static_for<KS>([&](auto g_) __attribute__((always_inline)) {
-        constexpr int g = decltype(g_)::value;
-        sum_step(g_);
-        __builtin_amdgcn_sched_barrier(0);
-        if constexpr (g + 2 < KS) read_values(j, std::integral_constant<int, g + 2>{});
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      __builtin_amdgcn_s_setprio(0);
-      turn();
-      // the other half multiplies
-      read_keys(j + 2, I0{}); read_keys(j + 2, I1{});
-      __builtin_amdgcn_sched_barrier(0);
-      store_k(j + 3);
-      store_v(j + 2);
-      __builtin_amdgcn_sched_barrier(0);
-      load_v(rows_v);
+    if constexpr (CODES) {
+      store_k(2);
       load_k(rows);
-      __builtin_amdgcn_sched_barrier(0);
-      weights();
+    } else if constexpr (!WIDE) {
+      direct_k(rows, kt(2));
+    }
+    if (WIDE && wave >= 4) turn();           // the second half starts half a round later
+    products(s, kt(1), vt(0));
+    if constexpr (!CODES && !WIDE) vm_wait<0>();
+    turn();
+    for (int j = 0; j < whole - 1; ++j) {
+      const Rows before = rows;              // the pages' table is read before the rows are asked for
+      rows = rows_of(j + AHEAD);
+      round(s, a.scale, kt(j + 2), vt(j + 1), kt(j + AHEAD), vt(j + AHEAD - 1),
+            [&](lds_char* k_to, lds_char* v_to) __attribute__((always_inline)) {
+              if constexpr (CODES) {
+                store_k(j + 3);
+                store_v(j + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                load_v(before);
+                load_k(rows);
+              } else {
+                direct_v(before, v_to);
+                direct_k(rows, k_to);
+              }
+            },
+            [&]() __attribute__((always_inline)) {
+              if constexpr (!CODES && WIDE) vm_wait<2 * Loads::N>();   // what was requested a round ago
+              if constexpr (WIDE) turn();
+            });
+      if constexpr (!CODES && !WIDE) vm_wait<0>();            // what was requested in this round
       turn();
     }
-    // the last tile's weighted sum
-    static_for<KS>([&](auto g_) __attribute__((always_inline)) { read_values(cw - 1, g_); sum_step(g_); });
-    if (wave < 4) turn();                    // the halves meet again
-    done = whole;
-    const float l0 = over_lanes(z[0].l), l1 = over_lanes(z[1].l);
+    if constexpr (!CODES) vm_wait<0>();      // nothing lands in LDS any more
+    tile = t0 + whole;
+    loaded = tile < t1;
+    if (loaded) {
+      rows = Registers::rows(a, b, tile * 64, wave);
+      load_k(rows); load_v(rows);
+    }
+    if (WIDE && wave < 4) turn();            // the halves meet again
+    const float l0 = over_lanes(s.z[0].l), l1 = over_lanes(s.z[1].l);
     if (__syncthreads_or(!(l0 <= 0x1p100f) || !(l1 <= 0x1p100f))) {
-      clear();
-      done = 0;
+      s.clear();
+      tile = t0;
+      loaded = false;
     }
   }
   // tile by tile: what is left, or everything once more; the next one on its way, in stages 0 and 1 in turn
-  const int again = done ? 0 : nw;
-  auto tile_at = [&](int j) __attribute__((always_inline)) { return j < again ? (j < cw ? w0 + j : -1) : j - again < cb ? b0 + j - again : -1; };
-  int tile = tile_at(0);
-  auto load_both = [&](int at) __attribute__((always_inline)) {
-    const auto rows = ck.rows(a, b, at * 64, qt);
-    load_k(rows); load_v(rows);
-  };
-  if (tile >= 0) load_both(tile);
-  for (int j = 0; j < again + nb; ++j) {
-    const int next = tile_at(j + 1);
-    if (tile >= 0) { store_k(j & 1); store_v(j & 1); }
-    if (j + 1 < again + nb && next >= 0) load_both(next);
+  for (int j = 0; tile < t1; ++j, ++tile) {
+    auto load_both = [&](int at) __attribute__((always_inline)) {
+      rows = Registers::rows(a, b, at * 64, wave);
+      load_k(rows); load_v(rows);
+    };
+    if (!loaded) load_both(tile);
+    store_k(j & 1); store_v(j & 1);
+    loaded = tile + 1 < t1;
+    if (loaded) load_both(tile + 1);
     __syncthreads();
-    if (tile >= 0) step<HD, 4, 2>(a, b, kst + (j & 1) * TILE, vst + (j & 1) * TILE, qf, tile * 64, j >= again, end, gaps, z, o, lane);
-    tile = next;
+    step<HD, 4, 2>(a, b, kst + (j & 1) * TILE, vst + (j & 1) * TILE, s.qf, tile * 64, tile >= t0 + whole, end, gaps, s.z, s.o, lane);
   }
-  float l[2] = {over_lanes(z[0].l), over_lanes(z[1].l)};
-  __syncthreads();
-  if constexpr (KG == 2) {
-    // the two key groups meet in LDS: group 1 publishes m, l, O^T, and group 0 goes on with both
-    float4* const xch = (float4*)smem + (size_t)qt * (2 * DT + 1) * 64 + lane;     // [qt][2 * DT + 1][64 lanes]
-    if (kg == 1) {
-      xch[0] = make_float4(z[0].m, z[1].m, l[0], l[1]);
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) xch[(1 + 2 * d + t) * 64] = make_float4(o[d][t][0], o[d][t][1], o[d][t][2], o[d][t][3]);
-    }
-    __syncthreads();
-    if (kg == 1) continue;
-    const float4 ml = xch[0];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const float m1 = t ? ml.y : ml.x, l1 = t ? ml.w : ml.z, m = fmaxf(z[t].m, m1), to = m == -INFINITY ? 0.f : m;
-      const float f0 = __builtin_amdgcn_exp2f(z[t].m - to), f1 = __builtin_amdgcn_exp2f(m1 - to);
-      z[t].m = m;
-      l[t] = l[t] * f0 + l1 * f1;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const float4 v = xch[(1 + 2 * d + t) * 64];
-        o[d][t] = o[d][t] * f0 + f32x4{v.x, v.y, v.z, v.w} * f1;
-      }
-    }
-  }
+  const float l[2] = {over_lanes(s.z[0].l), over_lanes(s.z[1].l)};
   if (p.slot >= 0) {
     float* const ps = a.partial + (size_t)p.slot * (QB * (2 + HD));
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int row = qt * 32 + t * 16 + lr;
+      const int row = wave * 32 + t * 16 + lr;
       if (b.first + row >= b.rows) continue;
-      if (lg == 0) { ps[row] = z[t].m; ps[QB + row] = l[t]; }
+      if (lg == 0) { ps[row] = s.z[t].m; ps[QB + row] = l[t]; }
 #pragma unroll
-      for (int d = 0; d < DT; ++d) *(f32x4*)(ps + 2 * QB + row * HD + d * 16 + lg * 4) = o[d][t];
+      for (int d = 0; d < DT; ++d) *(f32x4*)(ps + 2 * QB + row * HD + d * 16 + lg * 4) = s.o[d][t];
     }
   } else {
     // a lane holds 4 consecutive channels of a row per accumulator tile.  The 32 x HD tile of this wavefront goes through LDS (a wavefront
     // only touches its own rows, and LDS serves a wavefront's accesses in order) so that global memory sees whole rows, 16 bytes
     // per lane.  8-byte units are exchanged by the row.
     constexpr int UPR = HD / 4, CPR = HD / 8, RPI = 64 / CPR;      // units, 16-byte chunks per row; rows per read
-    constexpr int STG0 = KG == 2 ? QG * (2 * DT + 1) * 64 : 0;     // behind the exchange area
-    uint2* const stg = (uint2*)(smem + STG0) + qt * 32 * UPR;
+    __syncthreads();
+    uint2* const stg = (uint2*)smem + wave * 32 * UPR;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const float inv = inverse(l[t]);
       const int row = t * 16 + lr;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        stg[row * UPR + ((d * 4 + lg) ^ (row & (UPR - 1)))] = make_uint2(pack_bf16x2(o[d][t][0] * inv, o[d][t][1] * inv), pack_bf16x2(o[d][t][2] * inv, o[d][t][3] * inv));
+        stg[row * UPR + ((d * 4 + lg) ^ (row & (UPR - 1)))] = make_uint2(pack_bf16x2(s.o[d][t][0] * inv, s.o[d][t][1] * inv), pack_bf16x2(s.o[d][t][2] * inv, s.o[d][t][3] * inv));
     }
     const uint4* const stg16 = (const uint4*)stg;
 #pragma unroll
@@ -558,11 +629,10 @@ __global__ __launch_bounds__(512) void k_paged_turns(const PagedArgs a) {
       uint4 dv = stg16[row * CPR + ch];
       // units 2 ch and 2 ch + 1 of the exchanged row are the halves of chunk ch ^ (exchange >> 1), the other way round for odd rows
       if (row & 1) dv = make_uint4(dv.z, dv.w, dv.x, dv.y);
-      const int c = ch ^ ((row & (UPR - 1)) >> 1), r = b.first + qt * 32 + row;
+      const int c = ch ^ ((row & (UPR - 1)) >> 1), r = b.first + wave * 32 + row;
       if (r < b.rows) *(uint4*)((bf16_t*)a.out + row_at(a, b, r, a.o_ts, a.o_hs) + c * 8) = dv;
     }
   }
-  } while (PLAN && walk.next(a, p));
 }
 
 // What a call takes: rows per block, and ranges that a block's keys are cut into, or a plan of equal runs
@@ -585,26 +655,20 @@ Route route(const PagedArgs& a, int head_dim) {
     const int64_t units = (keys + 127) / 128, blocks = r.tiles * a.hk;
     if (units > 16 && blocks < 8192) r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
   } else {
-    // Blocks of either shape, one to a CU; a step of 64 keys x 256 rows, or 2 x 64 keys x 128 rows, is 1.7 us at heads of 128, and what a
-    // block does around its steps about 5 of them.  In rounds of 256 blocks, with ranges that fill the last round; or in 256 equal runs, which cost a plan, and on average one
-    // more tile begun and one more joined.  Partial results are written and read: 7 MB a step.  Sequences of several lengths and causal
-    // borders: half the bound's keys on average, and in rounds a block with all of them at the end.
+    // Blocks of 256 rows, one to a CU, or of 128, two; a step of 64 keys is 1.7 us of either at heads of 128, and what a block does around its
+    // steps about 5 of them.  One sequence, seen whole: rounds of 256 (512) blocks.  Sequences of several lengths and causal borders: all the work, with half the
+    // bound's keys on average, and one block with all of them at the end.  Ranges cost a launch and the traffic of partial results (7 MB a step).
     const bool even = a.n_seqs == 1 && a.group == 0;
     int64_t best = INT64_MAX;
     const int64_t key_tiles = (keys + 63) / 64;
     for (int qb = 256; qb >= 128; qb -= 128) {
-      const int64_t n = tiles(qb), part_cost = 256 * qb * (head_dim + 2) * 8;
-      auto steps_of = [&](int64_t of_part) { return qb == 256 ? of_part : (of_part + 1) / 2; };
+      const int64_t n = tiles(qb), slots = qb == 256 ? 256 : 512;
       for (int64_t parts = 1; parts <= 32; ++parts) {
-        const int64_t blocks = n * a.hk * parts, of_part = (key_tiles + parts - 1) / parts, steps = steps_of(of_part);
-        if (parts > 1 && of_part < 8) break;
-        const int64_t work = even ? (blocks + 255) / 256 * (steps + 5) : blocks * (steps / 2 + 5) / 256 + steps + 5;
-        const int64_t cost = work + (parts > 1 ? 4 + blocks * part_cost / 256 / 7000000 : 0);
-        if (cost < best) { best = cost; r.qb = qb; r.tiles = n; r.parts = (int)parts; r.part_keys = (int)(of_part * 64); r.runs = 0; }
-      }
-      const int64_t units = n * a.hk * steps_of(key_tiles) / (even ? 1 : 2), cost = units / 256 + n * a.hk * 5 / 256 + 12 + 2 * part_cost / 7000000;
-      if (units >= 256 * 4 && n * steps_of(key_tiles) < 0x7fffffff && cost < best) {
-        best = cost; r.qb = qb; r.tiles = n; r.parts = 1; r.part_keys = (int)keys; r.runs = 256;
+        const int64_t blocks = n * a.hk * parts, steps = (key_tiles + parts - 1) / parts;
+        if (parts > 1 && steps < 8) break;
+        const int64_t work = even ? (blocks + slots - 1) / slots * (steps + 5) : blocks * (steps / 2 + 5) / slots + steps + 5;
+        const int64_t cost = work + (parts > 1 ? 4 + blocks * qb * (head_dim + 2) * 8 / 7000000 : 0);
+        if (cost < best) { best = cost; r.qb = qb; r.tiles = n; r.parts = (int)parts; r.part_keys = (int)(steps * 64); }
       }
     }
   }
@@ -624,19 +688,12 @@ template <int HD, int NT, bool CODES> void few(const PagedArgs& a, hipStream_t s
     k_paged_few<HD, NT, 4, CODES, false><<<(unsigned)blocks, 256, 0, st>>>(a);
   }
 }
-template <int HD, int KG, bool CODES, bool PLAN> void turns_of(const PagedArgs& a, int64_t total, hipStream_t st) {
-  constexpr int tile = 64 * HD * 2, lds = KG == 1 ? 6 * tile : 8 * tile;
+template <int HD, bool WIDE, bool CODES> void turns(const PagedArgs& a, hipStream_t st) {
+  constexpr int lds = (WIDE ? (CODES ? 3 : 4) : 2) * 2 * 64 * HD * 2;
   static std::atomic<uint64_t> done;
-  allow_dynamic_lds((const void*)k_paged_turns<HD, KG, CODES, PLAN>, lds, done);
-  k_paged_turns<HD, KG, CODES, PLAN><<<(unsigned)((total + 7) / 8 * 8), 512, lds, st>>>(a);
-}
-template <int HD, int KG, bool CODES> void turns(const PagedArgs& a, hipStream_t st) {
-  if (a.plan) {
-    k_paged_plan<256 / KG, KG * 64><<<1, 1024, 0, st>>>(a);
-    turns_of<HD, KG, CODES, true>(a, a.runs, st);
-  } else {
-    turns_of<HD, KG, CODES, false>(a, (int64_t)a.tiles * a.hk * a.parts, st);
-  }
+  allow_dynamic_lds((const void*)k_paged_turns<HD, WIDE, CODES>, lds, done);
+  const int64_t total = (int64_t)a.tiles * a.hk * a.parts;
+  k_paged_turns<HD, WIDE, CODES><<<(unsigned)((total + 7) / 8 * 8), WIDE ? 512 : 256, lds, st>>>(a);
 }
 template <int HD, int QB> void join(const PagedArgs& a, hipStream_t st) {
   if (a.plan || a.parts > 1) k_paged_join<bf16_t, HD, QB><<<(unsigned)((int64_t)a.tiles * a.hk * QB * (HD / 4) / 256), 256, 0, st>>>(a);
@@ -644,8 +701,8 @@ template <int HD, int QB> void join(const PagedArgs& a, hipStream_t st) {
 template <int HD, bool CODES> void launch(const PagedArgs& a, int qb, hipStream_t st) {
   if (qb == 16) { few<HD, 1, CODES>(a, st); join<HD, 16>(a, st); }
   else if (qb == 32) { few<HD, 2, CODES>(a, st); join<HD, 32>(a, st); }
-  else if (qb == 128) { turns<HD, 2, CODES>(a, st); join<HD, 128>(a, st); }
-  else { turns<HD, 1, CODES>(a, st); join<HD, 256>(a, st); }
+  else if (qb == 128) { turns<HD, false, CODES>(a, st); join<HD, 128>(a, st); }
+  else { turns<HD, true, CODES>(a, st); join<HD, 256>(a, st); }
 }
 
 }  // namespace
