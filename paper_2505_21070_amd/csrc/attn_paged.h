@@ -1,6 +1,8 @@
 // What the attention kernels over a paged cache share: a call's arguments, which rows and keys a block of them owns, the way from a key
 // to its row in the pages.
 #pragma once
+#include <limits.h>
+
 #include "paged.h"
 
 struct PagedArgs {
@@ -389,6 +391,40 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
   }
   const float inv = inverse(l);
   store_four((T*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c, v * inv);
+}
+
+// ---- host: what a call takes
+struct Route { int qb, parts, part_keys, runs; int64_t tiles, tiles_of_seq; };   // rows of a block, ranges of its keys, or runs of a plan
+inline int64_t tiles_of_call(const PagedArgs& a, int qb) {
+  const int64_t each = ((int64_t)a.max_q * a.shared + qb - 1) / qb, all = a.n_tokens * a.shared / qb + a.n_seqs;
+  return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
+}
+// A kind of block: its rows, how many the chip holds, the keys of a step, and in units of 10 ns a step where all of them are held, a step where no more
+// than half are, and what is done around the steps.
+struct Kind { int qb, slots, keys; int64_t full, half, around; };
+// The kind and the ranges by an estimate of the time.  One sequence, seen whole: rounds of equal blocks.  Sequences of several lengths and causal borders: all
+// the work, with a little over half of the bound's keys on average, and half of the longest block at the end; at least that block.  Ranges cost a launch
+// and their partial results, written and read at 4.2 TB/s.
+inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_dim, Route& r) {
+  const bool even = a.n_seqs == 1 && a.group == 0;
+  int64_t best = INT64_MAX;
+  for (const Kind* k = kinds; k < kinds + n_kinds; ++k) {
+    const int64_t n = tiles_of_call(a, k->qb), key_tiles = (a.max_kv + k->keys - 1) / k->keys;
+    for (int64_t parts = 1; parts <= 32; ++parts) {
+      const int64_t blocks = n * a.hk * parts, steps = (key_tiles + parts - 1) / parts, last = blocks % k->slots;
+      if (parts > 1 && steps < 8) break;
+      const int64_t whole = steps * k->full + k->around, thin = steps * k->half + k->around;
+      int64_t cost = 0;
+      if (even) {
+        cost = blocks / k->slots * whole + (last > k->slots / 2 ? whole : last > 0 ? thin : 0);
+      } else {
+        cost = blocks * (steps * k->full * 11 / 20 + k->around) / k->slots + steps * k->half / 2;
+        cost = cost > thin ? cost : thin;
+      }
+      if (parts > 1) cost += 800 + blocks * k->qb * (head_dim + 2) * 8 / 42000;
+      if (cost < best) { best = cost; r.qb = k->qb; r.tiles = n; r.parts = (int)parts; r.part_keys = (int)(steps * k->keys); }
+    }
+  }
 }
 
 // ---- the launches; each fills in the launch fields of a and returns the bytes of partial results it needs (partial == null: only that)

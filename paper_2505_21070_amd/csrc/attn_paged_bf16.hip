@@ -154,7 +154,7 @@ template <int HD, int NT>
 __device__ __forceinline__ void weighted_sum_checked(uint32_t tile, uint32_t vlane, int s, const uint4 (&pf)[NT], const uint4 (&seen)[NT], f32x4 (&o)[HD / 16][NT]) {
 #pragma unroll
   for (int d = 0; d < HD / 16; ++d) {
-    uint4 v = __builtin_bit_cast(uint4, read_v<HD>(tile, vlane, s, d));
+    const uint4 v = __builtin_bit_cast(uint4, read_v<HD>(tile, vlane, s, d));
     const bool bad = not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
     if (!__any(bad)) {
 #pragma unroll
@@ -195,23 +195,10 @@ __device__ __forceinline__ uint4 ones_of(const f32x4& x, const f32x4& y) {
   auto pair = [](float p, float q) __attribute__((always_inline)) { return (p == -INFINITY ? 0u : 0x3f80u) | (q == -INFINITY ? 0u : 0x3f800000u); };
   return make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(y[0], y[1]), pair(y[2], y[3]));
 }
-// One tile of KT * 16 keys in plain order: scores, what a row does not see, the classical online softmax, the weighted sum.
+// The rest of a tile of KT * 16 keys whose scores are in sc: what a row does not see (border), the classical online softmax, the weighted sum.
 template <int HD, int KT, int NT>
-__device__ __forceinline__ void step(const PagedArgs& a, const Block& b, uint32_t ktile, uint32_t vtile, const bf16x8 (&qf)[NT][HD / 32], int key0, bool border,
-                                     const int (&end)[NT], bool gaps, Soft (&z)[NT], f32x4 (&o)[HD / 16][NT], int lane) {
-  f32x4 sc[NT][KT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) sc[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int ks = 0; ks < HD / 32; ++ks)
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const bf16x8 kf = read_k<HD>(ktile, k_lane<HD>(lane), kt, ks);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) sc[t][kt] = mfma(kf, qf[t][ks], sc[t][kt]);
-    }
+__device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uint32_t vtile, f32x4 (&sc)[NT][KT], int key0, bool border, const int (&end)[NT], bool gaps,
+                                         Soft (&z)[NT], f32x4 (&o)[HD / 16][NT], int lane) {
   uint4 pf[NT][KT / 2];
   const uint32_t gone = gaps ? missing<KT>(a, b, key0, lane) : 0;
 #pragma unroll
@@ -243,6 +230,19 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, uint32_
     }
   }
 }
+// scores of a tile in plain order
+template <int HD, int KT, int NT>
+__device__ __forceinline__ void score_tile(uint32_t ktile, const bf16x8 (&qf)[NT][HD / 32], f32x4 (&sc)[NT][KT], int lane) {
+#pragma unroll
+  for (int ks = 0; ks < HD / 32; ++ks)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      const bf16x8 kf = read_k<HD>(ktile, k_lane<HD>(lane), kt, ks);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sc[t][kt] = mfma(kf, qf[t][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[t][kt]);
+    }
+}
+
 template <int HD, int NT>
 __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b, int row0, bf16x8 (&qf)[NT][HD / 32], int (&end)[NT], int lane) {
 #pragma unroll
@@ -297,7 +297,9 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
       ck.template store<false>(kt, 0, lane);
       cv.template store<true>(vt, 0, lane);
       if (key + W * 32 < p.k1) load(key + W * 32);
-      step<HD, KT, NT>(a, b, kt, vt, qf, key, key + 32 > b.whole || gaps, end, gaps, z, o, lane);
+      f32x4 sc[NT][KT];
+      score_tile<HD, KT, NT>(kt, qf, sc, lane);
+      sum_tile<HD, KT, NT>(a, b, vt, sc, key, key + 32 > b.whole || gaps, end, gaps, z, o, lane);
     }
     join_waves<bf16_t, HD, NT, W>(a, b, (float*)smem, z, o, p.slot, wave, lane);
   } while (PLAN && walk.next(a, p));
@@ -475,8 +477,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   Registers ck, cv;
   typedef Direct<HD, W> Loads;
   const Loads direct(wave, lane);
-  // tiles past the whole ones: the first again, never used
-  auto rows_of = [&](int j) __attribute__((always_inline)) { return Registers::rows(a, b, (t0 + (j < whole ? j : 0)) * 64, wave); };
+  // tiles past the range: its first again, never used
+  auto rows_of = [&](int j) __attribute__((always_inline)) { return Registers::rows(a, b, (t0 + j < t1 ? t0 + j : t0) * 64, wave); };
   typedef decltype(rows_of(0)) Rows;
   auto direct_k = [&](const Rows& rows, lds_char* to) __attribute__((always_inline)) { Loads::load(a, rows, 0, direct.k, to, wave); };
   auto direct_v = [&](const Rows& rows, lds_char* to) __attribute__((always_inline)) { Loads::load(a, rows, to_values, direct.v, to, wave); };
@@ -484,6 +486,10 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   auto load_v = [&](const Rows& rows) __attribute__((always_inline)) { cv.load(a, rows, to_values, lane); };
   auto store_k = [&](int j) __attribute__((always_inline)) { ck.template store<false>(kst + (j % NS) * TILE, wave, lane); };
   auto store_v = [&](int j) __attribute__((always_inline)) { cv.template store<true>(vst + (j % NS) * TILE, wave, lane); };
+  auto load_both = [&](int at) __attribute__((always_inline)) {
+    const Rows both = Registers::rows(a, b, at * 64, wave);
+    load_k(both); load_v(both);
+  };
   auto kt = [&](int j) __attribute__((always_inline)) { return kst_ + (j % NS) * TILE; };
   auto vt = [&](int j) __attribute__((always_inline)) { return vst_ + (j % NS) * TILE; };
 
@@ -511,6 +517,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   if (__builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1))) { whole = 0; gaps = true; loaded = loaded && CODES; }
   s.clear();
   int tile = t0;
+  bool scored = false;                       // whether the scores of `tile` are there, and its values in LDS
   if (whole > 0) {
     if constexpr (CODES) {
       rows = rows_of(1);
@@ -569,32 +576,34 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
       turn();
     }
     if constexpr (!CODES) vm_wait<0>();      // nothing lands in LDS any more
+    // of the first tile with a border, the scores are there and the values in LDS; the one after it goes on its way
     tile = t0 + whole;
-    loaded = tile < t1;
-    if (loaded) {
-      rows = Registers::rows(a, b, tile * 64, wave);
-      load_k(rows); load_v(rows);
-    }
+    loaded = tile + 1 < t1;
+    if (loaded) load_both(tile + 1);
     if (WIDE && wave < 4) turn();            // the halves meet again
     const float l0 = over_lanes(s.z[0].l), l1 = over_lanes(s.z[1].l);
     if (__syncthreads_or(!(l0 <= 0x1p100f) || !(l1 <= 0x1p100f))) {
       s.clear();
       tile = t0;
       loaded = false;
+    } else {
+      scored = true;
     }
   }
   // tile by tile: what is left, or everything once more; the next one on its way, in stages 0 and 1 in turn
   for (int j = 0; tile < t1; ++j, ++tile) {
-    auto load_both = [&](int at) __attribute__((always_inline)) {
-      rows = Registers::rows(a, b, at * 64, wave);
-      load_k(rows); load_v(rows);
-    };
-    if (!loaded) load_both(tile);
-    store_k(j & 1); store_v(j & 1);
-    loaded = tile + 1 < t1;
-    if (loaded) load_both(tile + 1);
-    __syncthreads();
-    step<HD, 4, 2>(a, b, kst + (j & 1) * TILE, vst + (j & 1) * TILE, s.qf, tile * 64, tile >= t0 + whole, end, gaps, s.z, s.o, lane);
+    uint32_t values = vst + (whole % NS) * TILE;
+    if (!scored) {
+      if (!loaded) load_both(tile);
+      store_k(j & 1); store_v(j & 1);
+      loaded = tile + 1 < t1;
+      if (loaded) load_both(tile + 1);
+      __syncthreads();
+      score_tile<HD, 4, 2>(kst + (j & 1) * TILE, s.qf, s.sc, lane);
+      values = vst + (j & 1) * TILE;
+    }
+    sum_tile<HD, 4, 2>(a, b, values, s.sc, tile * 64, tile >= t0 + whole, end, gaps, s.z, s.o, lane);
+    if (scored) { scored = false; __syncthreads(); }          // stages are written again
   }
   const float l[2] = {over_lanes(s.z[0].l), over_lanes(s.z[1].l)};
   if (p.slot >= 0) {
@@ -635,42 +644,24 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   }
 }
 
-// What a call takes: rows per block, and ranges that a block's keys are cut into, or a plan of equal runs
-struct Route { int qb, parts, part_keys, runs; int64_t tiles, tiles_of_seq; };
 Route route(const PagedArgs& a, int head_dim) {
   Route r{};
-  const int64_t rows = (int64_t)a.max_q * a.shared;          // of a sequence, at most
-  auto tiles = [&](int qb) {
-    const int64_t each = (rows + qb - 1) / qb, all = a.n_tokens * a.shared / qb + a.n_seqs;
-    return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
-  };
-  const int64_t keys = a.max_kv;
+  const int64_t rows = (int64_t)a.max_q * a.shared, keys = a.max_kv;          // of a sequence, at most
   r.parts = 1;
   r.part_keys = (int)keys;
   if (rows <= 32) {
     r.qb = rows <= 16 ? 16 : 32;
-    r.tiles = tiles(r.qb);
+    r.tiles = tiles_of_call(a, r.qb);
     // Two blocks to a CU, with equal runs.  Not for sequences up to 2048 keys, whose one block each takes about as long as a plan and a join, nor for
     // very many.
     const int64_t units = (keys + 127) / 128, blocks = r.tiles * a.hk;
     if (units > 16 && blocks < 8192) r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
   } else {
-    // Blocks of 256 rows, one to a CU, or of 128, two; a step of 64 keys is 1.7 us of either at heads of 128, and what a block does around its
-    // steps about 5 of them.  One sequence, seen whole: rounds of 256 (512) blocks.  Sequences of several lengths and causal borders: all the work, with half the
-    // bound's keys on average, and one block with all of them at the end.  Ranges cost a launch and the traffic of partial results (7 MB a step).
-    const bool even = a.n_seqs == 1 && a.group == 0;
-    int64_t best = INT64_MAX;
-    const int64_t key_tiles = (keys + 63) / 64;
-    for (int qb = 256; qb >= 128; qb -= 128) {
-      const int64_t n = tiles(qb), slots = qb == 256 ? 256 : 512;
-      for (int64_t parts = 1; parts <= 32; ++parts) {
-        const int64_t blocks = n * a.hk * parts, steps = (key_tiles + parts - 1) / parts;
-        if (parts > 1 && steps < 8) break;
-        const int64_t work = even ? (blocks + slots - 1) / slots * (steps + 5) : blocks * (steps / 2 + 5) / slots + steps + 5;
-        const int64_t cost = work + (parts > 1 ? 4 + blocks * qb * (head_dim + 2) * 8 / 7000000 : 0);
-        if (cost < best) { best = cost; r.qb = qb; r.tiles = n; r.parts = (int)parts; r.part_keys = (int)(steps * 64); }
-      }
-    }
+    // Measured: heads of 128, 6240 x 9360 x 40: 955 us with 256 rows, 986 with 128; 1560 x 20280 x 12: 256 rows in three ranges 206, 128 rows in one 408 (half the
+    // chip's blocks), in eight 224; sequences of 2000, 1000, 3000 x 2000, 5000, 3000 x 16, causal: 191 and 163, in two ranges 231 and 191.  Heads of 64, 8192 x
+    // 8192 x 32: 541 and 504.
+    static const Kind wide[2] = {{256, 256, 64, 157, 157, 800}, {128, 512, 64, 163, 130, 600}}, narrow[2] = {{256, 256, 64, 100, 100, 800}, {128, 512, 64, 94, 80, 600}};
+    choose(a, head_dim == 128 ? wide : narrow, 2, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
   return r;

@@ -208,26 +208,26 @@ __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
   }
 }
 
-// What a call takes: wavefronts side by side over the rows, and ranges that a block's keys are cut into
-struct Route { int qb, parts, part_keys; int64_t tiles, tiles_of_seq; };
-Route route(const PagedArgs& a) {
+Route route(const PagedArgs& a, int head_dim) {
   Route r{};
-  const int64_t rows = (int64_t)a.max_q * a.shared;          // of a sequence, at most
-  auto tiles = [&](int qb) {
-    const int64_t each = (rows + qb - 1) / qb, all = a.n_tokens * a.shared / qb + a.n_seqs;
-    return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
-  };
-  r.qb = rows <= 16 ? 16 : rows <= 64 || tiles(128) * a.hk < 512 ? 64 : 128;
+  const int64_t rows = (int64_t)a.max_q * a.shared, keys = a.max_kv;          // of a sequence, at most
+  if (rows <= 16) {
+    r.qb = 16;
+    r.tiles = tiles_of_call(a, 16);
+    // ranges for four times as many blocks as there are CUs, none shorter than two trips of the four wavefronts
+    const int64_t blocks = r.tiles * a.hk;
+    int64_t parts = (1024 + blocks - 1) / blocks;
+    if (parts > (keys + 127) / 128) parts = (keys + 127) / 128;
+    if (parts > 256) parts = 256;
+    if (parts < 1) parts = 1;
+    r.part_keys = (int)(((keys + parts - 1) / parts + 63) / 64 * 64);
+    r.parts = r.part_keys > 0 ? (int)((keys + r.part_keys - 1) / r.part_keys) : 1;
+    if (r.parts < 1) r.parts = 1;
+  } else {
+    static const Kind wide[2] = {{64, 512, 32, 370, 200, 800}, {128, 512, 32, 720, 380, 800}}, narrow[2] = {{64, 512, 32, 190, 110, 800}, {128, 512, 32, 370, 200, 800}};
+    choose(a, head_dim == 128 ? wide : narrow, rows <= 64 ? 1 : 2, head_dim, r);
+  }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
-  r.tiles = tiles(r.qb);
-  const int64_t blocks = r.tiles * a.hk, keys = a.max_kv, least = r.qb == 16 ? 128 : 256;
-  int64_t parts = (1024 + blocks - 1) / blocks;
-  if (parts > (keys + least - 1) / least) parts = (keys + least - 1) / least;
-  if (parts > 256) parts = 256;
-  if (parts < 1) parts = 1;
-  r.part_keys = (int)(((keys + parts - 1) / parts + 63) / 64 * 64);
-  r.parts = r.part_keys > 0 ? (int)((keys + r.part_keys - 1) / r.part_keys) : 1;
-  if (r.parts < 1) r.parts = 1;
   return r;
 }
 template <int HD, int NT, int QG> void launch(const PagedArgs& a, bool codes, hipStream_t st) {
@@ -246,7 +246,7 @@ template <int HD> void launch(const PagedArgs& a, int qb, bool codes, hipStream_
 }  // namespace
 
 size_t launch_attn_paged_f32(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st) {
-  const Route r = route(a);
+  const Route r = route(a, head_dim);
   a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys;
   if (go) { if (head_dim == 128) launch<128>(a, r.qb, codes, st); else launch<64>(a, r.qb, codes, st); }
   return r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts * ((size_t)r.qb * (2 + head_dim) * sizeof(float)) : 0;
