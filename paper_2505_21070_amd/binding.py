@@ -419,17 +419,15 @@ def _rows(t, heads, n, d, td, device):
     return _PACK_ROWS(t.data_ptr(), ts, hs)
 
 
-def _current_device():
-    try:
-        return torch._C._cuda_getDevice()
-    except AttributeError:
-        return torch.cuda.current_device()
-
-
 def _stream_on(device, stream):
     """The stream handle of a call on `device`, which has to be the current one: the library launches there."""
-    assert device.type == "cuda" and device.index == _current_device(), f"tensors on {device}, not on the current device"
-    return _stream_handle(stream)
+    try:
+        now = torch._C._cuda_getDevice()
+        handle = torch._C._cuda_getCurrentRawStream(now) if stream is None else stream.cuda_stream
+    except AttributeError:                  # see _stream_handle
+        now, handle = torch.cuda.current_device(), _stream_handle(stream)
+    assert device.type == "cuda" and device.index == now, f"tensors on {device}, not on the current device"
+    return handle
 
 
 def _new(shape, like, stream, dtype=None):
@@ -438,6 +436,14 @@ def _new(shape, like, stream, dtype=None):
     if stream is not None:
         t.record_stream(stream)
     return t
+
+
+def _result(t, like, heads, n, d, td, device, stream):
+    """The caller's rows for a result, or new ones, and their description."""
+    if t is not None:
+        return t, _rows(t, heads, n, d, td, device)
+    t = _new((n, heads, d), like, stream)
+    return t, _PACK_ROWS(t.data_ptr(), heads * d, d)
 
 
 def _norm_rope(q, hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps):
@@ -453,12 +459,9 @@ def qk_norm_rope(q, k, gq, gk, pos, rope_theta=1e4, eps=1e-6, q_out=None, k_out=
     (n, hq, d), hk, td, dev = q.shape, k.shape[1], q.dtype, q.device
     st = _stream_on(dev, stream)
     cfg = _norm_rope(q, hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps)
-    if q_out is None:
-        q_out = _new((n, hq, d), q, stream)
-    if k_out is None:
-        k_out = _new((n, hk, d), q, stream)
-    _check(_lib.dp_qk_norm_rope(cfg, _rows(q, hq, n, d, td, dev), _rows(k, hk, n, d, td, dev), n, _rows(q_out, hq, n, d, td, dev),
-                                _rows(k_out, hk, n, d, td, dev), st), "dp_qk_norm_rope")
+    q_out, to_q = _result(q_out, q, hq, n, d, td, dev, stream)
+    k_out, to_k = _result(k_out, q, hk, n, d, td, dev, stream)
+    _check(_lib.dp_qk_norm_rope(cfg, _rows(q, hq, n, d, td, dev), _rows(k, hk, n, d, td, dev), n, to_q, to_k, st), "dp_qk_norm_rope")
     return q_out, k_out
 
 
@@ -508,10 +511,9 @@ class KVCache:
         st = _stream_on(dev, stream)
         cfg = _norm_rope(q, hq, self.kv_heads, n, d, td, dev, gq, gk, pos, rope_theta, eps)
         assert slot.shape[0] == n
-        if q_out is None:
-            q_out = _new((n, hq, d), q, stream)
+        q_out, to_q = _result(q_out, q, hq, n, d, td, dev, stream)
         _check(_lib.dp_kv_write_qkv(self._desc, cfg, _rows(q, hq, n, d, td, dev), _rows(k, self.kv_heads, n, d, td, dev),
-                                    _rows(v, self.kv_heads, n, d, td, dev), self._slots(slot), n, _rows(q_out, hq, n, d, td, dev), st), "dp_kv_write_qkv")
+                                    _rows(v, self.kv_heads, n, d, td, dev), self._slots(slot), n, to_q, st), "dp_kv_write_qkv")
         return q_out
 
     def read(self, slot, stream=None):
@@ -532,13 +534,12 @@ class KVCache:
         assert q_start.shape == (b + 1,) and kv_len.dim() == 1 and page_table.shape == (b, width)
         for t in (q_start, kv_len, page_table):
             assert t.dtype == torch.int32 and t.device == dev and t.is_contiguous()
-        if out is None:
-            out = _new((n, hq, d), q, stream)
+        out, to_out = _result(out, q, hq, n, d, td, dev, stream)
         cfg = _PACK_ATTN(hq, b, max_q, max_kv, width, causal_group, d ** -0.5 if scale is None else scale)
         nbytes = _lib.dp_attn_paged_workspace_bytes(self._desc, cfg, n)
         work = _new(nbytes, self.data, stream, torch.uint8) if nbytes else None
         _check(_lib.dp_attn_paged(self._desc, cfg, _rows(q, hq, n, d, td, dev), n, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
-                                  _rows(out, hq, n, d, td, dev), work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
+                                  to_out, work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
         return out
 
 

@@ -312,9 +312,22 @@ __device__ __forceinline__ float over_lanes(float v) { v += __shfl_xor(v, 16, 64
 __device__ __forceinline__ void store_four(float* p, f32x4 v) { *(f32x4*)p = v; }
 __device__ __forceinline__ void store_four(bf16_t* p, f32x4 v) { *(uint2*)p = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
 
+// A lane's channels of a row, of tiles of 16: tile d holds channels d * 16 .. (lane >> 4) * 4 + r of them in register r; SPREAD: channel row * (HD / 16) + d of
+// row (lane >> 4) * 4 + r.
+template <int HD, int NT, bool SPREAD> __device__ __forceinline__ void put_row(float* to, const f32x4 (&o)[HD / 16][NT], int t, int lg, float f) {
+  if constexpr (SPREAD) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int d = 0; d < HD / 16; d += 4) *(f32x4*)(to + (lg * 4 + r) * (HD / 16) + d) = f32x4{o[d][t][r], o[d + 1][t][r], o[d + 2][t][r], o[d + 3][t][r]} * f;
+  } else {
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) *(f32x4*)(to + d * 16 + lg * 4) = o[d][t] * f;
+  }
+}
 // The end of a block whose W wavefronts have the same NT * 16 rows and keys of their own: joined 16 rows at a time, every wavefront's m and l and its
 // O^T by rows, added up in wavefront order at the common reference.  smem: W * 16 * (2 + HD + 4) floats, which every wavefront is done with.
-template <typename T, int HD, int NT, int W>
+template <typename T, int HD, int NT, int W, bool SPREAD>
 __device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, float* smem, const Soft (&z)[NT], const f32x4 (&o)[HD / 16][NT], int slot, int wave, int lane) {
   constexpr int OS = HD + 4, QB = NT * 16;
   float* const ml = smem;                                    // [W][16][2]
@@ -325,8 +338,7 @@ __device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, f
     __syncthreads();
     const float lsum = over_lanes(z[t].l);
     if (lane < 16) { ml[(wave * 16 + lane) * 2] = z[t].m; ml[(wave * 16 + lane) * 2 + 1] = lsum; }
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) *(f32x4*)(os + (wave * 16 + (lane & 15)) * OS + d * 16 + (lane >> 4) * 4) = o[d][t];
+    put_row<HD, NT, SPREAD>(os + (wave * 16 + (lane & 15)) * OS, o, t, lane >> 4, 1.f);
     __syncthreads();
     for (int i = threadIdx.x; i < 16 * (HD / 4); i += W * 64) {
       const int r = i / (HD / 4), c = i % (HD / 4) * 4, row = t * 16 + r;
@@ -399,12 +411,12 @@ inline int64_t tiles_of_call(const PagedArgs& a, int qb) {
   const int64_t each = ((int64_t)a.max_q * a.shared + qb - 1) / qb, all = a.n_tokens * a.shared / qb + a.n_seqs;
   return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
 }
-// A kind of block: its rows, how many the chip holds, the keys of a step, and in units of 10 ns a step where all of them are held, a step where no more
-// than half are, and what is done around the steps.
-struct Kind { int qb, slots, keys; int64_t full, half, around; };
+// A kind of block: its rows, how many the chip holds, the keys of a step, the steps that a range has at least, and in units of 10 ns a step where all of them are
+// held, a step where no more than half are, and what is done around the steps.
+struct Kind { int qb, slots, keys, least; int64_t full, half, around; };
 // The kind and the ranges by an estimate of the time.  One sequence, seen whole: rounds of equal blocks.  Sequences of several lengths and causal borders: all
 // the work, with a little over half of the bound's keys on average, and half of the longest block at the end; at least that block.  Ranges cost a launch
-// and their partial results, written and read at 4.2 TB/s.
+// and their partial results, written and read at 4.2 TB/s, and a little for each that the estimate does not see.
 inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_dim, Route& r) {
   const bool even = a.n_seqs == 1 && a.group == 0;
   int64_t best = INT64_MAX;
@@ -412,7 +424,7 @@ inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_
     const int64_t n = tiles_of_call(a, k->qb), key_tiles = (a.max_kv + k->keys - 1) / k->keys;
     for (int64_t parts = 1; parts <= 32; ++parts) {
       const int64_t blocks = n * a.hk * parts, steps = (key_tiles + parts - 1) / parts, last = blocks % k->slots;
-      if (parts > 1 && steps < 8) break;
+      if (parts > 1 && steps < k->least) break;
       const int64_t whole = steps * k->full + k->around, thin = steps * k->half + k->around;
       int64_t cost = 0;
       if (even) {
@@ -421,12 +433,20 @@ inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_
         cost = blocks * (steps * k->full * 11 / 20 + k->around) / k->slots + steps * k->half / 2;
         cost = cost > thin ? cost : thin;
       }
-      if (parts > 1) cost += 800 + blocks * k->qb * (head_dim + 2) * 8 / 42000;
+      if (parts > 1) cost += 775 + 25 * parts + blocks * k->qb * (head_dim + 2) * 8 / 42000;
       if (cost < best) { best = cost; r.qb = k->qb; r.tiles = n; r.parts = (int)parts; r.part_keys = (int)(steps * k->keys); }
     }
   }
 }
 
-// ---- the launches; each fills in the launch fields of a and returns the bytes of partial results it needs (partial == null: only that)
-size_t launch_attn_paged_bf16(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st);
-size_t launch_attn_paged_f32(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st);
+// ---- what a call takes, the bytes of its workspace (partial results, then the plan), and the launches
+inline size_t partial_bytes(const PagedArgs& a, const Route& r, int head_dim) {
+  return (r.runs ? (size_t)r.runs * 2 : r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts : 0) * r.qb * (2 + head_dim) * sizeof(float);
+}
+inline size_t workspace_bytes(const PagedArgs& a, const Route& r, int head_dim) {
+  return partial_bytes(a, r, head_dim) + (r.runs ? (3 * (size_t)r.tiles + 1) * sizeof(int32_t) : 0);
+}
+Route route_attn_paged_bf16(const PagedArgs& a, int head_dim);
+Route route_attn_paged_f32(const PagedArgs& a, int head_dim);
+void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st);
+void launch_attn_paged_f32(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st);

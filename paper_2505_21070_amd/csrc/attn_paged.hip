@@ -44,12 +44,12 @@ extern "C" size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* c, const dp_a
   if (!why) why = why_not_tokens(n_tokens, cfg);
   if (why) { refuse("dp_attn_paged_workspace_bytes", why); return 0; }
   if (n_tokens == 0 || cfg->n_seqs == 0 || cfg->max_q == 0) return 0;
-  return (c->dtype == DP_BF16 ? launch_attn_paged_bf16 : launch_attn_paged_f32)(arguments(c, cfg, n_tokens), c->head_dim, c->format == DP_KV_FP8, false, nullptr);
+  const PagedArgs a = arguments(c, cfg, n_tokens);
+  return workspace_bytes(a, c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim) : route_attn_paged_f32(a, c->head_dim), c->head_dim);
 }
 
 extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, const dp_rows* q, int64_t n_tokens, const int32_t* q_start,
-                             const int32_t* kv_len, const int32_t* page_table, const dp_rows* out, void* workspace, size_t workspace_bytes,
-                             void* stream) {
+                             const int32_t* kv_len, const int32_t* page_table, const dp_rows* out, void* workspace, size_t have, void* stream) {
   static const char entry[] = "dp_attn_paged";
   REFUSE_IF(why_not_attn(c, cfg));
   REFUSE_IF(why_not_tokens(n_tokens, cfg));
@@ -63,15 +63,16 @@ extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, co
   a.q_ts = q->token_stride; a.q_hs = q->head_stride; a.o_ts = out->token_stride; a.o_hs = out->head_stride;
   a.q_start = q_start; a.kv_len = kv_len; a.table = page_table;
   const hipStream_t st = (hipStream_t)stream;
-  const bool codes = c->format == DP_KV_FP8;
-  auto* const launch = c->dtype == DP_BF16 ? launch_attn_paged_bf16 : launch_attn_paged_f32;
-  if (const size_t need = launch(a, c->head_dim, codes, false, nullptr)) {
+  const Route r = c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim) : route_attn_paged_f32(a, c->head_dim);
+  a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys; a.runs = r.runs;
+  if (const size_t need = workspace_bytes(a, r, c->head_dim)) {
     REFUSE_IF((uintptr_t)workspace & 255 ? "the workspace must be 256-byte aligned" : nullptr);
-    if (!workspace || workspace_bytes < need) return dp_set_error(DP_ENOMEM, "dp_attn_paged: workspace too small");
+    if (!workspace || have < need) return dp_set_error(DP_ENOMEM, "dp_attn_paged: workspace too small");
     a.partial = (float*)workspace;
+    if (r.runs) a.plan = (int32_t*)((char*)workspace + partial_bytes(a, r, c->head_dim));
   }
   (void)hipGetLastError();
-  launch(a, c->head_dim, codes, true, st);
+  (c->dtype == DP_BF16 ? launch_attn_paged_bf16 : launch_attn_paged_f32)(a, r, c->head_dim, c->format == DP_KV_FP8, st);
   if (hipGetLastError() != hipSuccess) return dp_set_error(DP_EHIP, "dp_attn_paged: the launch failed");
   return DP_OK;
 }

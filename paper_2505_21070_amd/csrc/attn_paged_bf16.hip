@@ -195,9 +195,10 @@ __device__ __forceinline__ uint4 ones_of(const f32x4& x, const f32x4& y) {
   auto pair = [](float p, float q) __attribute__((always_inline)) { return (p == -INFINITY ? 0u : 0x3f80u) | (q == -INFINITY ? 0u : 0x3f800000u); };
   return make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(y[0], y[1]), pair(y[2], y[3]));
 }
-// The rest of a tile of KT * 16 keys whose scores are in sc: what a row does not see (border), the classical online softmax, the weighted sum.
+// The rest of a tile of KT * 16 keys whose scores are in sc: what a row does not see (border), the classical online softmax (of_row: whether this tile may raise
+// a row's reference), the weighted sum.
 template <int HD, int KT, int NT>
-__device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uint32_t vtile, f32x4 (&sc)[NT][KT], int key0, bool border, const int (&end)[NT], bool gaps,
+__device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uint32_t vtile, f32x4 (&sc)[NT][KT], int key0, bool border, const bool (&of_row)[NT], const int (&end)[NT], bool gaps,
                                          Soft (&z)[NT], f32x4 (&o)[HD / 16][NT], int lane) {
   uint4 pf[NT][KT / 2];
   const uint32_t gone = gaps ? missing<KT>(a, b, key0, lane) : 0;
@@ -205,7 +206,7 @@ __device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uin
   for (int t = 0; t < NT; ++t) {
     if (border) hide<KT>(sc[t], key0, end[t], gone, lane);
     float ref;
-    const float alpha = raise(z[t], maximum<KT>(sc[t], KT) * a.scale, ref);
+    const float alpha = raise(z[t], of_row[t] ? maximum<KT>(sc[t], KT) * a.scale : -INFINITY, ref);
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) o[d][t] *= alpha;
     weigh<KT>(sc[t], a.scale, ref, z[t].l, pf[t]);
@@ -299,9 +300,12 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
       if (key + W * 32 < p.k1) load(key + W * 32);
       f32x4 sc[NT][KT];
       score_tile<HD, KT, NT>(kt, qf, sc, lane);
-      sum_tile<HD, KT, NT>(a, b, vt, sc, key, key + 32 > b.whole || gaps, end, gaps, z, o, lane);
+      bool all[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) all[t] = true;
+      sum_tile<HD, KT, NT>(a, b, vt, sc, key, key + 32 > b.whole || gaps, all, end, gaps, z, o, lane);
     }
-    join_waves<bf16_t, HD, NT, W>(a, b, (float*)smem, z, o, p.slot, wave, lane);
+    join_waves<bf16_t, HD, NT, W, false>(a, b, (float*)smem, z, o, p.slot, wave, lane);
   } while (PLAN && walk.next(a, p));
 }
 
@@ -447,8 +451,8 @@ __device__ __forceinline__ void round(State<HD>& s, float scale, const lds_char*
 // tiles hides behind the other.
 // Rows as they are come by direct loads into LDS (four stages, or two); codes through registers, converted on the way (three, or two).
 // The softmax's reference is fixed to a row's maximum over the first 32 keys: weights (bf16) and fp32 sums have 8 exponent bits, so nothing is lost until
-// a sum is beyond 2^100; such a block, or one that is not finite, is done again by the classical online softmax (step), which also does
-// the tiles that hold a border.
+// a sum is beyond 2^100; a block with such a row, or one that is not finite, is done again tile by tile, with the reference of those rows raised as in the
+// classical online softmax (the other rows get the same bits).  So are the tiles that hold a border, for all rows.
 // What bounds it: the matrix pipes.
 template <int HD, bool WIDE, bool CODES>
 __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const PagedArgs a) {
@@ -517,6 +521,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   if (__builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1))) { whole = 0; gaps = true; loaded = loaded && CODES; }
   s.clear();
   int tile = t0;
+  bool over[2] = {};                         // rows whose sums leave no room for their reference
   bool scored = false;                       // whether the scores of `tile` are there, and its values in LDS
   if (whole > 0) {
     if constexpr (CODES) {
@@ -581,9 +586,12 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
     loaded = tile + 1 < t1;
     if (loaded) load_both(tile + 1);
     if (WIDE && wave < 4) turn();            // the halves meet again
-    const float l0 = over_lanes(s.z[0].l), l1 = over_lanes(s.z[1].l);
-    if (__syncthreads_or(!(l0 <= 0x1p100f) || !(l1 <= 0x1p100f))) {
+    over[0] = !(over_lanes(s.z[0].l) <= 0x1p100f);
+    over[1] = !(over_lanes(s.z[1].l) <= 0x1p100f);
+    if (__syncthreads_or(over[0] || over[1])) {
       s.clear();
+#pragma unroll
+      for (int t = 0; t < 2; ++t) s.z[t].m = over[t] ? -INFINITY : s.ref[t];
       tile = t0;
       loaded = false;
     } else {
@@ -602,7 +610,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
       score_tile<HD, 4, 2>(kst + (j & 1) * TILE, s.qf, s.sc, lane);
       values = vst + (j & 1) * TILE;
     }
-    sum_tile<HD, 4, 2>(a, b, values, s.sc, tile * 64, tile >= t0 + whole, end, gaps, s.z, s.o, lane);
+    const bool border = tile >= t0 + whole, of_row[2] = {border || over[0], border || over[1]};
+    sum_tile<HD, 4, 2>(a, b, values, s.sc, tile * 64, border, of_row, end, gaps, s.z, s.o, lane);
     if (scored) { scored = false; __syncthreads(); }          // stages are written again
   }
   const float l[2] = {over_lanes(s.z[0].l), over_lanes(s.z[1].l)};
@@ -613,8 +622,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
       const int row = wave * 32 + t * 16 + lr;
       if (b.first + row >= b.rows) continue;
       if (lg == 0) { ps[row] = s.z[t].m; ps[QB + row] = l[t]; }
-#pragma unroll
-      for (int d = 0; d < DT; ++d) *(f32x4*)(ps + 2 * QB + row * HD + d * 16 + lg * 4) = s.o[d][t];
+      put_row<HD, 2, false>(ps + 2 * QB + row * HD, s.o, t, lg, 1.f);
     }
   } else {
     // a lane holds 4 consecutive channels of a row per accumulator tile.  The 32 x HD tile of this wavefront goes through LDS (a wavefront
@@ -660,7 +668,8 @@ Route route(const PagedArgs& a, int head_dim) {
     // Measured: heads of 128, 6240 x 9360 x 40: 955 us with 256 rows, 986 with 128; 1560 x 20280 x 12: 256 rows in three ranges 206, 128 rows in one 408 (half the
     // chip's blocks), in eight 224; sequences of 2000, 1000, 3000 x 2000, 5000, 3000 x 16, causal: 191 and 163, in two ranges 231 and 191.  Heads of 64, 8192 x
     // 8192 x 32: 541 and 504.
-    static const Kind wide[2] = {{256, 256, 64, 157, 157, 800}, {128, 512, 64, 163, 130, 600}}, narrow[2] = {{256, 256, 64, 100, 100, 800}, {128, 512, 64, 94, 80, 600}};
+    static const Kind wide[2] = {{256, 256, 64, 8, 157, 157, 800}, {128, 512, 64, 8, 163, 130, 600}},
+                      narrow[2] = {{256, 256, 64, 8, 100, 100, 800}, {128, 512, 64, 8, 94, 80, 600}};
     choose(a, head_dim == 128 ? wide : narrow, 2, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
@@ -698,14 +707,8 @@ template <int HD, bool CODES> void launch(const PagedArgs& a, int qb, hipStream_
 
 }  // namespace
 
-size_t launch_attn_paged_bf16(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st) {
-  const Route r = route(a, head_dim);
-  a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys; a.runs = r.runs;
-  const size_t partial = (r.runs ? (size_t)r.runs * 2 : r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts : 0) * r.qb * (2 + head_dim) * sizeof(float);
-  if (go) {
-    a.plan = r.runs ? (int32_t*)((char*)a.partial + partial) : nullptr;
-    if (head_dim == 128) { if (codes) launch<128, true>(a, r.qb, st); else launch<128, false>(a, r.qb, st); }
-    else { if (codes) launch<64, true>(a, r.qb, st); else launch<64, false>(a, r.qb, st); }
-  }
-  return partial + (r.runs ? (3 * (size_t)r.tiles + 1) * sizeof(int32_t) : 0);
+Route route_attn_paged_bf16(const PagedArgs& a, int head_dim) { return route(a, head_dim); }
+void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st) {
+  if (head_dim == 128) { if (codes) launch<128, true>(a, r.qb, st); else launch<128, false>(a, r.qb, st); }
+  else { if (codes) launch<64, true>(a, r.qb, st); else launch<64, false>(a, r.qb, st); }
 }

@@ -3,7 +3,8 @@
 // As in bf16 (attn_paged_bf16.hip), on v_mfma_f32_16x16x4_f32: S^T = K Q^T, whose accumulators, once turned into weights, are the B operand of O^T = V^T P^T
 // register by register (register r of a lane is key (lane >> 4) * 4 + r, and step r of the second product takes just those four keys).  The
 // head dim's order in the first product is free: a lane takes 16 bytes of a key's or query's row and uses their four values in four steps.
-// LDS rows are padded by 16 bytes: 16 rows of 16 bytes, and four rows of 64, four apart, spread over the 64 banks.
+// LDS rows are padded by 16 bytes, so that 16 rows of 16 bytes spread over the 64 banks.  The order of O^T's rows is free as well: a lane reads its
+// channels of a value's row with 16-byte reads.
 // The matrix pipe does 1/16 of bf16's rate, so everything else hides behind it.
 #include <math.h>
 
@@ -51,23 +52,42 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) sc[t][kt] = odd[t][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int c = 0; c < HD / 16; c += 2) {
-    f32x4 k[2][KT];
+  // operands are read from LDS a batch of products before they are used
+  f32x4 k[2][2][KT];
+  auto read_k = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) k[h][kt] = *(const f32x4*)(ktile + (kt * 16 + lr) * RS + (c + h) * 16 + lg * 4);
+      for (int kt = 0; kt < KT; ++kt) k[(c / 2) & 1][h][kt] = *(const f32x4*)(ktile + (kt * 16 + lr) * RS + (c + h) * 16 + lg * 4);
+  };
+  read_k(0);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int c = 0; c < HD / 16; c += 2) {
+    if (c + 2 < HD / 16) read_k(c + 2);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          sc[t][kt] = mfma(k[0][kt][j], qf[t][c][j], sc[t][kt]);
-          odd[t][kt] = mfma(k[1][kt][j], qf[t][c + 1][j], odd[t][kt]);
+          sc[t][kt] = mfma(k[(c / 2) & 1][0][kt][j], qf[t][c][j], sc[t][kt]);
+          odd[t][kt] = mfma(k[(c / 2) & 1][1][kt][j], qf[t][c + 1][j], odd[t][kt]);
         }
+    __builtin_amdgcn_sched_barrier(0);
   }
+  // the values of this lane's first key: row n of channel tile d is channel n * (HD / 16) + d, so that a lane's channels lie together
+  float v[2][HD / 16];
+  auto read_v = [&](int i) __attribute__((always_inline)) {            // key (i / 4) * 16 + lg * 4 + i % 4
+    const float* const at = vtile + ((i >> 2) * 16 + lg * 4 + (i & 3)) * RS + lr * (HD / 16);
+#pragma unroll
+    for (int d = 0; d < HD / 16; d += 4) {
+      const f32x4 x = *(const f32x4*)(at + d);
+      v[i & 1][d] = x[0]; v[i & 1][d + 1] = x[1]; v[i & 1][d + 2] = x[2]; v[i & 1][d + 3] = x[3];
+    }
+  };
+  read_v(0);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -89,65 +109,50 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
         z[t].l += p[t][kt][r];
       }
   }
-  if (!border) {
+  // A value that is not finite must not meet the weight 0 of a row that does not see its key (0 * infinity is NaN): at a border it is multiplied as 0, and rows
+  // that do see +inf, -inf or NaN are found by products of ones and get it added.
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d) {
-          const float v = vtile[(kt * 16 + lg * 4 + r) * RS + d * 16 + lr];
-#pragma unroll
-          for (int t = 0; t < NT; ++t) o[d][t] = mfma(v, p[t][kt][r], o[d][t]);
-        }
-    return;
-  }
-  // A value that is not finite must not meet the weight 0 of a row that does not see its key (0 * infinity is NaN): it is multiplied as 0, and rows that do
-  // see +inf, -inf or NaN are found by products of ones and get it added.
-#pragma unroll
-  for (int d = 0; d < HD / 16; ++d) {
-    float v[KT][4];
+  for (int i = 0; i < KT * 4; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + 1 < KT * 4) read_v(i + 1);
+    __builtin_amdgcn_sched_barrier(0);
     bool bad = false;
+    float x[HD / 16];
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+    for (int d = 0; d < HD / 16; ++d) x[d] = v[i & 1][d];
+    if (border) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        v[kt][r] = vtile[(kt * 16 + lg * 4 + r) * RS + d * 16 + lr];
-        bad |= !(fabsf(v[kt][r]) < INFINITY);
-      }
+      for (int d = 0; d < HD / 16; ++d) bad |= !(fabsf(x[d]) < INFINITY);
+    }
+    if (border && __any(bad)) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
+      for (int d = 0; d < HD / 16; ++d) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+        for (int t = 0; t < NT; ++t) {
+          const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+          const float one = sc[t][i >> 2][i & 3] == -INFINITY ? 0.f : 1.f;
+          const f32x4 np = mfma(x[d] == INFINITY ? 1.f : 0.f, one, zero), nn = mfma(x[d] == -INFINITY ? 1.f : 0.f, one, zero), nx = mfma(x[d] != x[d] ? 1.f : 0.f, one, zero);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) o[d][t] = mfma(fabsf(v[kt][r]) < INFINITY ? v[kt][r] : 0.f, p[t][kt][r], o[d][t]);
-    if (!__any(bad)) continue;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      f32x4 np{0.f, 0.f, 0.f, 0.f}, nn = np, nx = np;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float x = v[kt][r], one = sc[t][kt][r] == -INFINITY ? 0.f : 1.f;
-          np = mfma(x == INFINITY ? 1.f : 0.f, one, np);
-          nn = mfma(x == -INFINITY ? 1.f : 0.f, one, nn);
-          nx = mfma(x != x ? 1.f : 0.f, one, nx);
+          for (int r = 0; r < 4; ++r) {
+            const float y = o[d][t][r] + (np[r] > 0.f ? INFINITY : 0.f) - (nn[r] > 0.f ? INFINITY : 0.f);
+            o[d][t][r] = nx[r] > 0.f ? __uint_as_float(0x7fc00000u) : y;
+          }
         }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float x = o[d][t][r] + (np[r] > 0.f ? INFINITY : 0.f) - (nn[r] > 0.f ? INFINITY : 0.f);
-        o[d][t][r] = nx[r] > 0.f ? __uint_as_float(0x7fc00000u) : x;
+        x[d] = fabsf(x[d]) < INFINITY ? x[d] : 0.f;
       }
     }
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[d][t] = mfma(x[d], p[t][i >> 2][i & 3], o[d][t]);
   }
 }
 
-// Four wavefronts.  QG = 4: each has NT * 16 rows of its own, and they share tiles of 32 keys.  QG = 1: all have the same NT * 16 rows and deal the keys
+// Four wavefronts.  QG = 4: each has 16 rows of its own, and they share tiles of 32 keys.  QG = 1: all have the same 16 rows and deal the keys
 // out in tiles of 16 (wavefront w: tiles w, w + 4, ...), and meet in LDS at the end.  Either way the next tile is on its way in registers.
-template <int HD, int NT, int QG, bool CODES>
+template <int HD, int QG, bool CODES>
 __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
-  constexpr int KG = 4 / QG, TK = QG == 1 ? 16 : 32, KT = TK / 16, RS = HD + 4, QB = QG * NT * 16, TILE = TK * RS;
+  constexpr int NT = 1, KG = 4 / QG, TK = QG == 1 ? 16 : 32, KT = TK / 16, RS = HD + 4, QB = QG * NT * 16, TILE = TK * RS;
   constexpr int JOIN = QG == 1 ? 4 * 16 * 2 + 4 * 16 * RS : 0, SIZE = KG * 2 * TILE;
   __shared__ __align__(16) float smem[SIZE > JOIN ? SIZE : JOIN];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qt = wave % QG, kg = wave / QG;
@@ -159,6 +164,13 @@ __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
   f32x4 qf[NT][HD / 16], o[HD / 16][NT];
   int end[NT];
   Soft z[NT];
+  float* const kt = smem + kg * 2 * TILE;
+  float* const vt = kt + TILE;
+  const int64_t to_values = (int64_t)a.hk << a.page_shift;
+  Carry<HD, TK, QG, CODES> ck, cv;
+  auto load = [&](int at) __attribute__((always_inline)) { ck.load(a, b, at, 0, qt, lane); cv.load(a, b, at, to_values, qt, lane); };
+  const int first = k0 + kg * TK;
+  if (first < k1) load(first);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = b.first + (qt * NT + t) * 16 + (lane & 15);
@@ -170,19 +182,13 @@ __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  float* const kt = smem + kg * 2 * TILE;
-  float* const vt = kt + TILE;
-  const int64_t to_values = (int64_t)a.hk << a.page_shift;
-  Carry<HD, TK, QG, CODES> ck, cv;
-  int key = k0 + kg * TK;
-  if (key < k1) { ck.load(a, b, key, 0, qt, lane); cv.load(a, b, key, to_values, qt, lane); }
   const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
-  for (; key < k1; key += KG * TK) {
+  for (int key = first; key < k1; key += KG * TK) {
     if constexpr (QG > 1) __syncthreads();
     ck.store(kt, qt, lane);
     cv.store(vt, qt, lane);
     if constexpr (QG > 1) __syncthreads();
-    if (key + KG * TK < k1) { ck.load(a, b, key + KG * TK, 0, qt, lane); cv.load(a, b, key + KG * TK, to_values, qt, lane); }
+    if (key + KG * TK < k1) load(key + KG * TK);
     step<HD, KT, NT>(a, b, kt, vt, qf, key, key + TK > b.whole || gaps, end, gaps, z, o, lane);
   }
   if constexpr (QG > 1) {
@@ -192,19 +198,15 @@ __global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
       const float l = over_lanes(z[t].l);
       if (b.first + row >= b.rows) continue;
       if (p.slot < 0) {
-        float* const out = (float*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + (lane >> 4) * 4;
-        const float inv = inverse(l);
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d) *(f32x4*)(out + d * 16) = o[d][t] * inv;
+        put_row<HD, NT, true>((float*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs), o, t, lane >> 4, inverse(l));
       } else {
         float* const ps = a.partial + (size_t)p.slot * (QB * (2 + HD));
         if (lane < 16) { ps[row] = z[t].m; ps[QB + row] = l; }
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d) *(f32x4*)(ps + 2 * QB + row * HD + d * 16 + (lane >> 4) * 4) = o[d][t];
+        put_row<HD, NT, true>(ps + 2 * QB + row * HD, o, t, lane >> 4, 1.f);
       }
     }
   } else {
-    join_waves<float, HD, NT, 4>(a, b, smem, z, o, p.slot, wave, lane);
+    join_waves<float, HD, NT, 4, true>(a, b, smem, z, o, p.slot, wave, lane);
   }
 }
 
@@ -224,30 +226,28 @@ Route route(const PagedArgs& a, int head_dim) {
     r.parts = r.part_keys > 0 ? (int)((keys + r.part_keys - 1) / r.part_keys) : 1;
     if (r.parts < 1) r.parts = 1;
   } else {
-    static const Kind wide[2] = {{64, 512, 32, 370, 200, 800}, {128, 512, 32, 720, 380, 800}}, narrow[2] = {{64, 512, 32, 190, 110, 800}, {128, 512, 32, 370, 200, 800}};
-    choose(a, head_dim == 128 ? wide : narrow, rows <= 64 ? 1 : 2, head_dim, r);
+    // Measured: 64 x 8192 keys x 16 heads of 128 2.9 us a step; 4096 x 4096 x 12 in rounds of 512 blocks and 256: 966 us.  Blocks of 128 rows (two columns a
+    // wavefront) are no faster at any size: 5.2 us a step, and 1026 us.
+    static const Kind wide{64, 512, 32, 4, 450, 290, 800}, narrow{64, 512, 32, 4, 250, 160, 800};
+    choose(a, head_dim == 128 ? &wide : &narrow, 1, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
   return r;
 }
-template <int HD, int NT, int QG> void launch(const PagedArgs& a, bool codes, hipStream_t st) {
-  constexpr int QB = QG * NT * 16;
+template <int HD, int QG> void launch(const PagedArgs& a, bool codes, hipStream_t st) {
+  constexpr int QB = QG * 16;
   const int64_t blocks = (int64_t)a.tiles * a.hk;
   const unsigned g = (unsigned)(blocks * a.parts);
-  if (codes) k_paged_f32<HD, NT, QG, true><<<g, 256, 0, st>>>(a); else k_paged_f32<HD, NT, QG, false><<<g, 256, 0, st>>>(a);
+  if (codes) k_paged_f32<HD, QG, true><<<g, 256, 0, st>>>(a); else k_paged_f32<HD, QG, false><<<g, 256, 0, st>>>(a);
   if (a.parts > 1) k_paged_join<float, HD, QB><<<(unsigned)(blocks * QB * (HD / 4) / 256), 256, 0, st>>>(a);
 }
 template <int HD> void launch(const PagedArgs& a, int qb, bool codes, hipStream_t st) {
-  if (qb == 16) launch<HD, 1, 1>(a, codes, st);
-  else if (qb == 64) launch<HD, 1, 4>(a, codes, st);
-  else launch<HD, 2, 4>(a, codes, st);
+  if (qb == 16) launch<HD, 1>(a, codes, st); else launch<HD, 4>(a, codes, st);
 }
 
 }  // namespace
 
-size_t launch_attn_paged_f32(PagedArgs a, int head_dim, bool codes, bool go, hipStream_t st) {
-  const Route r = route(a, head_dim);
-  a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys;
-  if (go) { if (head_dim == 128) launch<128>(a, r.qb, codes, st); else launch<64>(a, r.qb, codes, st); }
-  return r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts * ((size_t)r.qb * (2 + head_dim) * sizeof(float)) : 0;
+Route route_attn_paged_f32(const PagedArgs& a, int head_dim) { return route(a, head_dim); }
+void launch_attn_paged_f32(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st) {
+  if (head_dim == 128) launch<128>(a, r.qb, codes, st); else launch<64>(a, r.qb, codes, st);
 }
