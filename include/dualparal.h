@@ -351,7 +351,7 @@ typedef struct {
 
 /* RMSNorm of every head of q and k over its own head_dim values, times the gain, then the stage's 3D rotation of channel pairs
  * (2i, 2i+1), in one pass: y = R(pos) (x * rsqrt(mean(x^2) + eps) * g).  Statistics, angles (in 64 bits, any position) and products
- * are fp32; one rounding at the end.
+ * are fp32; one rounding at the end.  The sum of a row's squares has to be a normal fp32 number (or its mean small next to eps).
  *   gq, gk : device [head_dim], of dtype, shared by the heads;  pos : device int32 [n_tokens, 3], (frame, row, column) */
 typedef struct {
   int32_t q_heads, kv_heads;  /* 1 .. 1024 each                                                    */
@@ -397,10 +397,11 @@ int dp_kv_read(const dp_kv_cache* cache, const int32_t* slot, int64_t n_tokens, 
  * Scores, softmax and sums are fp32; with DP_BF16 the weights are rounded to bf16 before they meet the values.
  *   workspace  : device, 256-byte aligned, dp_attn_paged_workspace_bytes(cache, cfg, n_tokens) bytes (0 for many calls: then it may be
  *                NULL), used by one call at a time; nothing has to be kept in it between calls.
- * Errors: DP_EINVAL (null pointer, sizes, alignment or strides outside the limits, n_tokens * q_heads of 2^31 or more), DP_ENOMEM (workspace too small), DP_EHIP. */
+ * Errors: DP_EINVAL (null pointer, sizes, alignment or strides outside the limits, n_tokens * q_heads above
+ *         2^29, n_seqs * kv_heads above 2^21), DP_ENOMEM (workspace too small), DP_EHIP. */
 typedef struct {
   int32_t q_heads;            /* a multiple of kv_heads, <= 1024                                   */
-  int32_t n_seqs;             /* 0 .. 65535                                                        */
+  int32_t n_seqs;             /* 0 .. 65535, n_seqs * kv_heads <= 2^21                             */
   int32_t max_q;              /* 0 .. 2^24                                                         */
   int32_t max_kv;             /* 0 .. 2^31 - 1 - 65536                                             */
   int32_t table_width;        /* >= 0                                                              */

@@ -427,6 +427,7 @@ def _stream_on(device, stream):
     except AttributeError:                  # see _stream_handle
         now, handle = torch.cuda.current_device(), _stream_handle(stream)
     assert device.type == "cuda" and device.index == now, f"tensors on {device}, not on the current device"
+    assert stream is None or stream.device == device, f"a stream of {stream.device} for tensors on {device}"
     return handle
 
 

@@ -15,10 +15,10 @@ struct PagedArgs {
   int32_t n_pages, page_shift, hk, shared, n_seqs, max_q, max_kv, table_width, group;
   float scale;                            // of the scores, times log2(e): softmax in powers of two
   // The launch: tiles of rows (of all sequences) and the most a sequence has.  A block has one tile's range of keys with one key head: of `parts` ranges
-  // of part_keys keys each.  Or, with a plan, the work of all tiles and heads lies in one line, in units of a number of keys, and each of `runs` blocks
-  // has an equal run of it: the end of one tile's keys, all of some, the beginning of another's.
+  // of part_keys keys each.  Or, with a plan (sequences of one tile each), the work of all tiles and heads lies in one line, in units of a number of keys, and
+  // each of `runs` blocks has an equal run of it: the end of one tile's keys, all of some, the beginning of another's.
   int32_t tiles, tiles_of_seq, parts, part_keys, runs;
-  int32_t* plan;                          // null, or units before each tile and of all [tiles + 1], sequence [tiles], tile of the sequence [tiles]
+  int32_t* plan;                          // null, or units before each tile and of all [tiles + 1]
   float* partial;                         // of each range, or of the incomplete first [0] and last [1] tile of each run: m[QB], l[QB], O[QB][head_dim]
 };
 
@@ -103,7 +103,6 @@ template <int QB> __device__ __forceinline__ bool locate(const PagedArgs& a, int
   int b = -1, rb = 0;
   if (a.tiles_of_seq == 1) b = tile;
   else if (a.n_seqs == 1) { b = 0; rb = tile; }
-  else if (a.plan) { b = uniform_i32(a.plan + a.tiles + 1 + tile); rb = uniform_i32(a.plan + 2 * a.tiles + 1 + tile); }
   else {
     // tiles are numbered through the sequences: 64 of them at a time, a lane each
     const int lane = threadIdx.x & 63;
@@ -148,54 +147,40 @@ __device__ __forceinline__ int before(int v, int* waves, int& total) {
   for (int w = 0; w < 16; ++w) { base += w < wave ? waves[w] : 0; total += waves[w]; }
   return base + upto - v;
 }
-// Writes the plan of a call: one block.  UNIT keys are a unit; a tile that sees no key has one.
+// Writes the plan of a call: one block.  UNIT keys are a unit; a sequence that sees no key has one, a sequence without new tokens has none.
 template <int QB, int UNIT>
 __global__ __launch_bounds__(1024) void k_paged_plan(const PagedArgs a) {
   __shared__ int waves[16];
-  int32_t* const units = a.plan;
-  int32_t* const seq = a.plan + a.tiles + 1;
-  int32_t* const rb = seq + a.tiles;
-  int tiles = 0;
-  for (int s0 = 0; s0 < a.n_seqs; s0 += 1024) {
-    const int s = s0 + (int)threadIdx.x;
-    const int n = s < a.n_seqs ? (int)(((int64_t)sequence(a, a.q_start[s], a.q_start[s + 1], 0).rows * a.shared + QB - 1) / QB) : 0;
-    int total;
-    const int at = tiles + before(n, waves, total);
-    for (int i = 0; i < n && at + i < a.tiles; ++i) { seq[at + i] = s; rb[at + i] = i; }
-    tiles += total;
-  }
-  __threadfence_block();
-  __syncthreads();
   int sum = 0;
   for (int t0 = 0; t0 < a.tiles; t0 += 1024) {
     const int t = t0 + (int)threadIdx.x;
-    int n = 0;
-    if (t < a.tiles) {
-      if (t >= tiles) seq[t] = -1;
-      Block k;
-      if (t < tiles && tile_of<QB>(a, k, seq[t], rb[t], 0)) n = k.end > 0 ? (k.end + UNIT - 1) / UNIT : 1;
-    }
-    int total;
+    int n = 0, total;
+    Block k;
+    if (t < a.tiles && tile_of<QB>(a, k, t, 0, 0)) n = k.end > 0 ? (k.end + UNIT - 1) / UNIT : 1;
     const int at = sum + before(n, waves, total);
-    if (t < a.tiles) units[t] = at;
+    if (t < a.tiles) a.plan[t] = at;
     sum += total;
   }
-  if (threadIdx.x == 0) units[a.tiles] = sum;
+  if (threadIdx.x == 0) a.plan[a.tiles] = sum;
 }
 
 // The work of one block, piece by piece: a tile's keys [k0, k1) with a head.
 struct Piece { Block b; int k0, k1, slot; };   // slot: of the partial result, or -1: these are all of the tile's keys
-// run g of a.runs begins at unit first_of(g) of `all`; run_of(x) is the one that unit x lies in
-__device__ __forceinline__ int64_t first_of(const PagedArgs& a, int g, int64_t all) { return g * all / a.runs; }
-__device__ __forceinline__ int run_of(const PagedArgs& a, int64_t x, int64_t all) { return (int)(((x + 1) * a.runs - 1) / all); }
+// `all` units, at least one, are cut into a.runs runs, or as many as there are units, none empty: run g begins at unit first_of(g); run_of(x) is the one that
+// unit x lies in
+__device__ __forceinline__ int64_t runs_of(const PagedArgs& a, int64_t all) { return all < a.runs ? all : a.runs; }
+__device__ __forceinline__ int64_t first_of(const PagedArgs& a, int g, int64_t all) { return g * all / runs_of(a, all); }
+__device__ __forceinline__ int run_of(const PagedArgs& a, int64_t x, int64_t all) { return (int)(((x + 1) * runs_of(a, all) - 1) / all); }
 template <int QB, int UNIT, bool PLAN> struct Walk {
   int id;                                 // the block's number
   int64_t x, x1;                          // with a plan: units to do
   __device__ __forceinline__ Walk(const PagedArgs& a, int block) : id(block), x(0), x1(0) {
     if constexpr (PLAN) {
       const int64_t all = (int64_t)uniform_i32(a.plan + a.tiles) * a.hk;
-      x = first_of(a, id, all);
-      x1 = first_of(a, id + 1, all);
+      if (id < runs_of(a, all)) {
+        x = first_of(a, id, all);
+        x1 = first_of(a, id + 1, all);
+      }
     }
   }
   __device__ __forceinline__ bool next(const PagedArgs& a, Piece& p) {
@@ -209,7 +194,7 @@ template <int QB, int UNIT, bool PLAN> struct Walk {
     } else {
       if (x >= x1) return false;
       const int of_head = uniform_i32(a.plan + a.tiles), hk = (int)(x / of_head), r = (int)(x - (int64_t)hk * of_head), lane = threadIdx.x & 63;
-      // the last tile that begins at r or before, 64 of them at a look
+      // the last tile that begins at r or before (those without units lie before it), 64 of them at a look
       int lo = 0, hi = a.tiles;
       while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, at = lo + lane * step;
@@ -221,7 +206,7 @@ template <int QB, int UNIT, bool PLAN> struct Walk {
       const int u0 = r - uniform_i32(a.plan + lo), units = uniform_i32(a.plan + lo + 1) - uniform_i32(a.plan + lo);
       const int n = units - u0 < x1 - x ? units - u0 : (int)(x1 - x);
       x += n;
-      if (!locate<QB>(a, lo, hk, p.b)) return false;            // never: only tiles that are there have units
+      if (!locate<QB>(a, lo, hk, p.b)) return false;            // never: only sequences with new tokens have units
       p.k0 = __builtin_amdgcn_readfirstlane(u0 * UNIT);
       const int k1 = (u0 + n) * UNIT;
       p.k1 = __builtin_amdgcn_readfirstlane(k1 < p.b.end ? k1 : p.b.end);
@@ -416,7 +401,8 @@ inline int64_t tiles_of_call(const PagedArgs& a, int qb) {
 struct Kind { int qb, slots, keys, least; int64_t full, half, around; };
 // The kind and the ranges by an estimate of the time.  One sequence, seen whole: rounds of equal blocks.  Sequences of several lengths and causal borders: all
 // the work, with a little over half of the bound's keys on average, and half of the longest block at the end; at least that block.  Ranges cost a launch
-// and their partial results, written and read at 4.2 TB/s, and a little for each that the estimate does not see.
+// and their partial results, written and read at 4.2 TB/s, and a little for each that the estimate does not see.  Where blocks fill the chip many times over there
+// are none, which bounds the workspace.
 inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_dim, Route& r) {
   const bool even = a.n_seqs == 1 && a.group == 0;
   int64_t best = INT64_MAX;
@@ -424,7 +410,7 @@ inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_
     const int64_t n = tiles_of_call(a, k->qb), key_tiles = (a.max_kv + k->keys - 1) / k->keys;
     for (int64_t parts = 1; parts <= 32; ++parts) {
       const int64_t blocks = n * a.hk * parts, steps = (key_tiles + parts - 1) / parts, last = blocks % k->slots;
-      if (parts > 1 && steps < k->least) break;
+      if (parts > 1 && (steps < k->least || blocks > 16 * k->slots)) break;
       const int64_t whole = steps * k->full + k->around, thin = steps * k->half + k->around;
       int64_t cost = 0;
       if (even) {
@@ -444,7 +430,7 @@ inline size_t partial_bytes(const PagedArgs& a, const Route& r, int head_dim) {
   return (r.runs ? (size_t)r.runs * 2 : r.parts > 1 ? (size_t)r.tiles * a.hk * r.parts : 0) * r.qb * (2 + head_dim) * sizeof(float);
 }
 inline size_t workspace_bytes(const PagedArgs& a, const Route& r, int head_dim) {
-  return partial_bytes(a, r, head_dim) + (r.runs ? (3 * (size_t)r.tiles + 1) * sizeof(int32_t) : 0);
+  return partial_bytes(a, r, head_dim) + (r.runs ? ((size_t)r.tiles + 1) * sizeof(int32_t) : 0);
 }
 Route route_attn_paged_bf16(const PagedArgs& a, int head_dim);
 Route route_attn_paged_f32(const PagedArgs& a, int head_dim);

@@ -11,6 +11,7 @@ const char* why_not_attn(const dp_kv_cache* c, const dp_attn_config* cfg) {
   if (!cfg) return "null pointer";
   if (cfg->q_heads < 1 || cfg->q_heads > 1024 || cfg->q_heads % c->kv_heads) return "q_heads must be a multiple of kv_heads in [1, 1024]";
   if (cfg->n_seqs < 0 || cfg->n_seqs > 65535) return "n_seqs must be in [0, 65535]";
+  if ((int64_t)cfg->n_seqs * c->kv_heads > 1 << 21) return "n_seqs * kv_heads must be at most 2^21";
   if (cfg->max_q < 0 || cfg->max_q > (1 << 24)) return "max_q must be in [0, 2^24]";
   if (cfg->max_kv < 0 || cfg->max_kv > 0x7fffffff - 65536) return "max_kv must be in [0, 2^31 - 1 - 65536]";
   if (cfg->table_width < 0) return "table_width must not be negative";
@@ -34,8 +35,9 @@ PagedArgs arguments(const dp_kv_cache* c, const dp_attn_config* cfg, int64_t n_t
   a.scale = cfg->scale * 1.4426950408889634f;
   return a;
 }
+// 2^29 rows in blocks of at most 4 threads a row, and a block of at most 512 threads begun for each sequence and key head: launches stay below 2^32 threads
 const char* why_not_tokens(int64_t n, const dp_attn_config* cfg) {
-  return n < 0 || n > (1 << 24) || n * cfg->q_heads > 0x7fffffff ? "n_tokens must be in [0, 2^24], n_tokens * q_heads below 2^31" : nullptr;
+  return n < 0 || n > (1 << 24) || n * cfg->q_heads > 1 << 29 ? "n_tokens must be in [0, 2^24], n_tokens * q_heads at most 2^29" : nullptr;
 }
 }  // namespace
 

@@ -518,7 +518,11 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   load_queries<HD, 2>(a, b, b.first + wave * 32, s.qf, end, lane);
   s.klane = k_lane<HD>(lane);
   s.vlane = v_lane<HD>(lane);
-  if (__builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1))) { whole = 0; gaps = true; loaded = loaded && CODES; }
+  if (__builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1))) {
+    if (!CODES && whole > 0) { vm_wait<0>(); __syncthreads(); }   // nothing lands in LDS any more
+    whole = 0;
+    gaps = true;
+  }
   s.clear();
   int tile = t0;
   bool over[2] = {};                         // rows whose sums leave no room for their reference
@@ -661,9 +665,9 @@ Route route(const PagedArgs& a, int head_dim) {
     r.qb = rows <= 16 ? 16 : 32;
     r.tiles = tiles_of_call(a, r.qb);
     // Two blocks to a CU, with equal runs.  Not for sequences up to 2048 keys, whose one block each takes about as long as a plan and a join, nor for
-    // very many.
+    // very many; units are counted in 32 bits.
     const int64_t units = (keys + 127) / 128, blocks = r.tiles * a.hk;
-    if (units > 16 && blocks < 8192) r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
+    if (units > 16 && blocks < 8192 && blocks * units < INT_MAX) r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
   } else {
     // Measured: heads of 128, 6240 x 9360 x 40: 955 us with 256 rows, 986 with 128; 1560 x 20280 x 12: 256 rows in three ranges 206, 128 rows in one 408 (half the
     // chip's blocks), in eight 224; sequences of 2000, 1000, 3000 x 2000, 5000, 3000 x 16, causal: 191 and 163, in two ranges 231 and 191.  Heads of 64, 8192 x

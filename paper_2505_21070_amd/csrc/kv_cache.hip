@@ -182,7 +182,7 @@ template <typename T, int HD, bool CODES>
 __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
   constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = 4;
   const int lane = threadIdx.x & 63, c0 = lane % LANES * N;
-  const uint32_t task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^24 + 2^14, see cut()
+  const uint32_t task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^26, see cut()
   const int64_t t = task / (uint32_t)a.runs;
   if (t >= a.n_tokens) return;
   int run = (int)(task % (uint32_t)a.runs);

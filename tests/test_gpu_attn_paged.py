@@ -55,6 +55,41 @@ def test_empty_and_padded(dtype, fp8):
     attend_and_check(f, queries(6, 4, 128, dtype), [0, 0, 6, 0, 0], group=4)
 
 
+@pytest.mark.parametrize("most", [1, 3, 12])
+@pytest.mark.parametrize("dtype,fp8", STORES)
+def test_padded_batch_of_long_sequences(dtype, fp8, most):
+    """A batch some of whose places bring no new token, or have no keys, between sequences long enough to be split."""
+    q_len, keys = [0, 1, 0, 0, most, 1, 1, 0, 2], [2500, 2600, 0, 17, 3001, 0, 4100, 2100, 129]
+    f = Filled(keys, 2, 128, 16, dtype, fp8)
+    for group in (0, 1):
+        attend_and_check(f, queries(sum(q_len) + 2, 4, 128, dtype), q_len, group)
+
+
+@pytest.mark.parametrize("dtype,fp8", STORES)
+def test_bounds_larger_than_the_sequences(dtype, fp8):
+    """A launch made for far more new tokens and keys than there are, as one captured for all sizes is."""
+    q_len = [1, 0, 3, 40]
+    f = Filled([5, 70, 300, 140], 2, 64, 32, dtype, fp8)
+    f.table = torch.cat([f.table, torch.full((4, 500), -1, dtype=torch.int32, device="cuda")], dim=1).contiguous()
+    for max_q in (40, 1000, 1 << 24):
+        attend_and_check(f, queries(44, 4, 64, dtype), q_len, 1, max_q=max_q, max_kv=2 ** 31 - 1 - 65536)
+    attend_and_check(f, queries(4, 4, 64, dtype), [1, 0, 1, 2], 1, max_q=8, max_kv=2 ** 31 - 1 - 65536)
+
+
+@pytest.mark.parametrize("dtype,fp8", STORES)
+def test_sequences_that_share_pages(dtype, fp8):
+    """Pages in several tables, and one page twice in a table: reading does not mind."""
+    f = Filled([192], 2, 128, 64, dtype, fp8)
+    k, v = f.k[0], f.v[0]
+    own = f.table[0].tolist()
+    f.table = torch.tensor([own, [own[1], own[1], own[0]], own], dtype=torch.int32, device="cuda")
+    twice = np.concatenate([np.arange(64, 128), np.arange(64, 128), np.arange(64)])
+    f.keys = [192, 170, 100]
+    f.k, f.v = [k, k[twice[:170]], k[:100]], [v, v[twice[:170]], v[:100]]
+    for n in (1, 90):
+        attend_and_check(f, queries(3 * n, 4, 128, dtype), [n] * 3, group=1)
+
+
 @pytest.mark.parametrize("rows_", [1, 20, 200])
 @pytest.mark.parametrize("dtype,fp8", STORES)
 def test_what_is_not_seen_does_not_count(dtype, fp8, rows_):

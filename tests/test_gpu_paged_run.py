@@ -170,3 +170,14 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for s in range(2):
         assert all(torch.equal(y, want[s]) for y in got[s])
+
+
+def test_a_stream_of_another_device_is_refused():
+    from paper_2505_21070_amd import binding as B
+    cache = B.KVCache.empty(2, HK, PAGE, D)
+
+    class Other:
+        device, cuda_stream = torch.device("cuda", torch.cuda.current_device() + 1), 0
+
+    with pytest.raises(AssertionError):
+        cache.read(torch.zeros(1, dtype=torch.int32, device="cuda"), stream=Other())

@@ -142,6 +142,20 @@ def test_workspaces():
         assert attend(a=big, n=1, work=work, nbytes=nbytes) == B.DP_ENOMEM and "workspace" in B.last_error()
     refused(attend(a=big, n=1, work=AT + 128, nbytes=need), "dp_attn_paged")
     refused(attend(a=attn(q_heads=512), n=1 << 22, q=rows(512), out=rows(512)), "dp_attn_paged")
+    refused(attend(a=attn(q_heads=512), n=(1 << 20) + 1, q=rows(512), out=rows(512)), "dp_attn_paged")
+    refused(attend(c=cache(kv_heads=64), a=attn(q_heads=64, n_seqs=(1 << 15) + 1), q=rows(64), out=rows(64)), "dp_attn_paged")
+
+
+def test_workspaces_stay_bounded():
+    """Partial results take at most 16 times as many blocks as the chip holds, whatever the bounds of the launch."""
+    for dtype in (B.DP_F32, B.DP_BF16):
+        for heads, d in ((1, 64), (40, 128), (1024, 64)):
+            for n_seqs in (1, 40, 2000):
+                for max_q in (1, 30, 100, 5000, 1 << 24):
+                    for max_kv in (1, 5000, 2 ** 31 - 1 - 65536):
+                        c = cache(dtype=dtype, kv_heads=heads, head_dim=d, page_tokens=65536)
+                        a = attn(q_heads=heads, n_seqs=n_seqs, max_q=max_q, max_kv=max_kv, table_width=1 << 16)
+                        assert L.dp_attn_paged_workspace_bytes(c, a, min(1 << 24, (1 << 29) // heads)) <= 16 * 512 * 128 * (d + 2) * 4
 
 
 def test_nothing_to_do():
