@@ -451,7 +451,7 @@ __device__ __forceinline__ void round(State<HD>& s, float scale, const lds_char*
 // tiles hides behind the other.
 // Rows as they are come by direct loads into LDS (four stages, or two); codes through registers, converted on the way (three, or two).
 // The softmax's reference is fixed to a row's maximum over the first 32 keys: weights (bf16) and fp32 sums have 8 exponent bits, so nothing is lost until
-// a sum is beyond 2^100; a block with such a row, or one that is not finite, is done again tile by tile, with the reference of those rows raised as in the
+// a sum, of weights or of weighted values, is beyond 2^100; a block with such a row, or one that is not finite, is done again tile by tile, with the reference of those rows raised as in the
 // classical online softmax (the other rows get the same bits).  So are the tiles that hold a border, for all rows.
 // What bounds it: the matrix pipes.
 template <int HD, bool WIDE, bool CODES>
@@ -590,8 +590,16 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
     loaded = tile + 1 < t1;
     if (loaded) load_both(tile + 1);
     if (WIDE && wave < 4) turn();            // the halves meet again
-    over[0] = !(over_lanes(s.z[0].l) <= 0x1p100f);
-    over[1] = !(over_lanes(s.z[1].l) <= 0x1p100f);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      int bad = !(over_lanes(s.z[t].l) <= 0x1p100f);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bad |= !(fabsf(s.o[d][t][r]) <= 0x1p100f);
+      bad |= __shfl_xor(bad, 16, 64);
+      over[t] = bad | __shfl_xor(bad, 32, 64);
+    }
     if (__syncthreads_or(over[0] || over[1])) {
       s.clear();
 #pragma unroll

@@ -144,6 +144,18 @@ def test_scores_far_apart(dtype, fp8, rows_):
     attend_and_check(f, q, [rows_] * 3, group=0, scale=3.0)
 
 
+@pytest.mark.parametrize("rows_", [2, 30, 150, 500])
+@pytest.mark.parametrize("dtype,fp8", STORES)
+def test_large_values_behind_small_scores(dtype, fp8, rows_):
+    """Scores rise by about 60 after the first keys, which is 2^86 in weights that still refer to them, and the values lie around 2^50: each fits
+    fp32, their product does not."""
+    def change(b, k, v):
+        k[64:] += 5.0
+        v *= 2.0 ** 50
+    f = Filled([700], 2, 128, 64, dtype, fp8, change=change)
+    attend_and_check(f, queries(rows_, 2, 128, dtype).abs(), [rows_], group=0)
+
+
 @pytest.mark.parametrize("rows_", [2, 30, 150])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_scores_of_minus_infinity(dtype, rows_):
