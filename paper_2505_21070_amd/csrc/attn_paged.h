@@ -351,14 +351,27 @@ __device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, f
   }
 }
 
-// Joins the key ranges of a block's rows: a lane has four channels of a row.
-template <typename T, int HD, int QB>
+// Joins the partial results of a tile's rows: a lane has four channels of a row.  SPLIT groups of lanes deal a row's partial results out (8 where rows are
+// few and results may be many: 235 of them took 45 us one behind the other) and meet in LDS, in their order.
+template <int HD, int SPLIT> struct Joined {
+  static constexpr int LANES = HD / 4, ROWS = 256 / LANES / SPLIT;           // lanes of a row, rows of a block
+  static __host__ __device__ __forceinline__ int blocks_of_tile(const PagedArgs& a, int qb) {
+    const int64_t most = (int64_t)a.max_q * a.shared;
+    return ((most < qb ? (int)most : qb) + ROWS - 1) / ROWS;
+  }
+};
+template <typename T, int HD, int QB, int SPLIT>
 __global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
-  constexpr int LANES = HD / 4, ROWS = 256 / LANES;
-  const int id = blockIdx.x / (QB / ROWS), row = blockIdx.x % (QB / ROWS) * ROWS + threadIdx.x / LANES, c = threadIdx.x % LANES * 4;
+  typedef Joined<HD, SPLIT> J;
+  constexpr int LANES = J::LANES;
+  __shared__ float ms[SPLIT > 1 ? 256 / LANES : 1], ls[SPLIT > 1 ? 256 / LANES : 1];
+  __shared__ f32x4 vs[SPLIT > 1 ? 256 : 1];
+  const int per = J::blocks_of_tile(a, QB), id = blockIdx.x / per, group = threadIdx.x / LANES, split = group % SPLIT;
+  const int row = (int)(blockIdx.x % per) * J::ROWS + group / SPLIT, c = threadIdx.x % LANES * 4;
   Block b;
-  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b) || b.first + row >= b.rows) return;
-  int parts, first;                                          // partial results, and the slot of the first;
+  if (!locate<QB>(a, id % a.tiles, id / a.tiles, b)) return;
+  const bool mine = b.first + row < b.rows;
+  int parts, first;                                          // partial results, and the slot of the first
   if (a.plan) {
     const int tile = id % a.tiles, of_head = uniform_i32(a.plan + a.tiles);
     const int64_t all = (int64_t)of_head * a.hk, x = (int64_t)(id / a.tiles) * of_head + uniform_i32(a.plan + tile);
@@ -373,21 +386,42 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
   auto at = [&](int i) __attribute__((always_inline)) {
     return a.partial + (size_t)(a.plan && i > 0 ? first - 1 + 2 * i : first + i) * (QB * (2 + HD));
   };
+  const int from = mine ? split : parts;
   float m = -INFINITY;
 #pragma unroll 4
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, at(i)[row]);
+  for (int i = from; i < parts; i += SPLIT) m = fmaxf(m, at(i)[row]);
+  if constexpr (SPLIT > 1) {
+    if (c == 0) ms[group] = m;
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < SPLIT; ++s) m = fmaxf(m, ms[group - split + s]);
+  }
   const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f;
   f32x4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
+  for (int i = from; i < parts; i += SPLIT) {
     const float* const p = at(i);
     const float f = __builtin_amdgcn_exp2f(p[row] - ref);
     l += p[QB + row] * f;
     v += *(const f32x4*)(p + 2 * QB + row * HD + c) * f;
   }
-  const float inv = inverse(l);
-  store_four((T*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c, v * inv);
+  if constexpr (SPLIT > 1) {
+    if (c == 0) ls[group] = l;
+    vs[threadIdx.x] = v;
+    __syncthreads();
+    if (split > 0) return;
+#pragma unroll
+    for (int s = 1; s < SPLIT; ++s) {
+      l += ls[group + s];
+      v += vs[threadIdx.x + s * LANES];
+    }
+  }
+  if (mine) store_four((T*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c, v * inverse(l));
+}
+template <typename T, int HD, int QB> void launch_join(const PagedArgs& a, hipStream_t st) {
+  constexpr int SPLIT = QB <= 32 ? 8 : 1;
+  if (a.plan || a.parts > 1) k_paged_join<T, HD, QB, SPLIT><<<(unsigned)((int64_t)a.tiles * a.hk * Joined<HD, SPLIT>::blocks_of_tile(a, QB)), 256, 0, st>>>(a);
 }
 
 // ---- host: what a call takes

@@ -258,7 +258,8 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
 
 // Few rows: NT * 16 of them, W wavefronts that deal the block's keys out in tiles of 32 (wavefront w: tiles w, w + W, ...), each through its own piece of
 // LDS, the next tile on its way in registers; nobody waits for anybody until the results are joined in LDS, in wavefront order.  W = 4: two blocks to a
-// CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory.  W = 8: short sequences, bound by latency, one block each.
+// CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory: 64 sequences of 16 .. 16000 keys, 8 heads of 128 in 8 bits, 201 us, 5.3 TB/s.  W = 8: no more
+// blocks than CUs, bound by a trip's way through LDS, 2 us for 256 keys: one token over 517 keys with 12 heads 11.4 us.
 template <int HD, int NT, int W, bool CODES, bool PLAN>
 __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
   constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
@@ -672,10 +673,22 @@ Route route(const PagedArgs& a, int head_dim) {
   if (rows <= 32) {
     r.qb = rows <= 16 ? 16 : 32;
     r.tiles = tiles_of_call(a, r.qb);
-    // Two blocks to a CU, with equal runs.  Not for sequences up to 2048 keys, whose one block each takes about as long as a plan and a join, nor for
-    // very many; units are counted in 32 bits.
     const int64_t units = (keys + 127) / 128, blocks = r.tiles * a.hk;
-    if (units > 16 && blocks < 8192 && blocks * units < INT_MAX) r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
+    if (a.n_seqs == 1 || units <= 16 || blocks * keys <= 400000) {
+      // Ranges for one block of eight wavefronts a CU, no shorter than one of their trips (256 keys), from three on: one token of 12 heads of 128 over 768 keys 11.5 us
+      // in one, 10.7 in three; over 2000 21.8 and 12.0.
+      int64_t parts = (keys + 255) / 256;
+      if (parts > 256 / blocks) parts = 256 / blocks;
+      if (keys >= 768 && parts > 1) {
+        r.part_keys = (int)(((keys + parts - 1) / parts + 31) / 32 * 32);
+        r.parts = (int)((keys + r.part_keys - 1) / r.part_keys);
+      }
+    } else if (blocks < 8192 && blocks * units < INT_MAX) {
+      // Equal runs of all sequences' keys, two blocks a CU, where there is so much work that lengths below the bound count for more than a plan: 64 sequences of 100 to
+      // 16000 keys 215 us.  Equal lengths lose little: 8 of 16000 keys with 8 heads 51 us, in ranges 47; 4 of 6000 23 and 17.  Not for sequences up to 2048
+      // keys (64 of 2000 52 and 44), nor for very many; units are counted in 32 bits.
+      r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
+    }
   } else {
     // Measured: heads of 128, 6240 x 9360 x 40: 955 us with 256 rows, 986 with 128; 1560 x 20280 x 12: 256 rows in three ranges 206, 128 rows in one 408 (half the
     // chip's blocks), in eight 224; sequences of 2000, 1000, 3000 x 2000, 5000, 3000 x 16, causal: 191 and 163, in two ranges 231 and 191.  Heads of 64, 8192 x
@@ -690,7 +703,7 @@ Route route(const PagedArgs& a, int head_dim) {
 
 template <int HD, int NT, bool CODES> void few(const PagedArgs& a, hipStream_t st) {
   constexpr int QB = NT * 16;
-  const int64_t blocks = (int64_t)a.tiles * a.hk;
+  const int64_t blocks = (int64_t)a.tiles * a.hk * a.parts;
   if (a.plan) {
     k_paged_plan<QB, 128><<<1, 1024, 0, st>>>(a);
     k_paged_few<HD, NT, 4, CODES, true><<<(unsigned)a.runs, 256, 0, st>>>(a);
@@ -707,14 +720,11 @@ template <int HD, bool WIDE, bool CODES> void turns(const PagedArgs& a, hipStrea
   const int64_t total = (int64_t)a.tiles * a.hk * a.parts;
   k_paged_turns<HD, WIDE, CODES><<<(unsigned)((total + 7) / 8 * 8), WIDE ? 512 : 256, lds, st>>>(a);
 }
-template <int HD, int QB> void join(const PagedArgs& a, hipStream_t st) {
-  if (a.plan || a.parts > 1) k_paged_join<bf16_t, HD, QB><<<(unsigned)((int64_t)a.tiles * a.hk * QB * (HD / 4) / 256), 256, 0, st>>>(a);
-}
 template <int HD, bool CODES> void launch(const PagedArgs& a, int qb, hipStream_t st) {
-  if (qb == 16) { few<HD, 1, CODES>(a, st); join<HD, 16>(a, st); }
-  else if (qb == 32) { few<HD, 2, CODES>(a, st); join<HD, 32>(a, st); }
-  else if (qb == 128) { turns<HD, false, CODES>(a, st); join<HD, 128>(a, st); }
-  else { turns<HD, true, CODES>(a, st); join<HD, 256>(a, st); }
+  if (qb == 16) { few<HD, 1, CODES>(a, st); launch_join<bf16_t, HD, 16>(a, st); }
+  else if (qb == 32) { few<HD, 2, CODES>(a, st); launch_join<bf16_t, HD, 32>(a, st); }
+  else if (qb == 128) { turns<HD, false, CODES>(a, st); launch_join<bf16_t, HD, 128>(a, st); }
+  else { turns<HD, true, CODES>(a, st); launch_join<bf16_t, HD, 256>(a, st); }
 }
 
 }  // namespace

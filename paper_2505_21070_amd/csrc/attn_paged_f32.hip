@@ -239,7 +239,7 @@ template <int HD, int QG> void launch(const PagedArgs& a, bool codes, hipStream_
   const int64_t blocks = (int64_t)a.tiles * a.hk;
   const unsigned g = (unsigned)(blocks * a.parts);
   if (codes) k_paged_f32<HD, QG, true><<<g, 256, 0, st>>>(a); else k_paged_f32<HD, QG, false><<<g, 256, 0, st>>>(a);
-  if (a.parts > 1) k_paged_join<float, HD, QB><<<(unsigned)(blocks * QB * (HD / 4) / 256), 256, 0, st>>>(a);
+  launch_join<float, HD, QB>(a, st);
 }
 template <int HD> void launch(const PagedArgs& a, int qb, bool codes, hipStream_t st) {
   if (qb == 16) launch<HD, 1>(a, codes, st); else launch<HD, 4>(a, codes, st);

@@ -63,6 +63,32 @@ def test_padded_batch_of_long_sequences(dtype, fp8, most):
     f = Filled(keys, 2, 128, 16, dtype, fp8)
     for group in (0, 1):
         attend_and_check(f, queries(sum(q_len) + 2, 4, 128, dtype), q_len, group)
+    # the same in a launch made for sequences of 24000 keys
+    f.table = torch.cat([f.table, torch.full((9, 1500 - f.table.shape[1]), -1, dtype=torch.int32, device="cuda")], dim=1).contiguous()
+    for group in (0, 1):
+        attend_and_check(f, queries(sum(q_len) + 2, 4, 128, dtype), q_len, group, max_kv=24000)
+
+
+@pytest.mark.parametrize("q_each", [1, 5])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_sequences_of_very_different_lengths(fp8, q_each, dtype="bf16"):
+    """Tokens of ten sequences of 0 to 21000 keys; then the call captured, and replayed for other lengths, which have to leave the results of eager calls."""
+    keys = [21000, 5, 0, 16000, 129, 9000, 1, 300, 21000, 4000]
+    f = Filled(keys, 2, 64, 64, dtype, fp8)
+    q = queries(10 * q_each, 4, 64, dtype)
+    attend_and_check(f, q, [q_each] * 10, group=1)
+    start = torch.arange(11, dtype=torch.int32, device="cuda") * q_each
+    first = torch.tensor(keys, dtype=torch.int32, device="cuda")
+    lens, out = first.clone(), torch.zeros_like(q)
+    f.cache.attend(q, start, lens, f.table, q_each, 21000, causal_group=1, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        f.cache.attend(q, start, lens, f.table, q_each, 21000, causal_group=1, out=out)
+    for now in (first, first // 2, torch.clamp(first, max=40), first * 0, first):
+        lens.copy_(now)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, f.cache.attend(q, start, now.contiguous(), f.table, q_each, 21000, causal_group=1))
 
 
 @pytest.mark.parametrize("dtype,fp8", STORES)
