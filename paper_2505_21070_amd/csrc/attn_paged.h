@@ -172,9 +172,11 @@ __device__ __forceinline__ int64_t runs_of(const PagedArgs& a, int64_t all) { re
 __device__ __forceinline__ int64_t first_of(const PagedArgs& a, int g, int64_t all) { return g * all / runs_of(a, all); }
 __device__ __forceinline__ int run_of(const PagedArgs& a, int64_t x, int64_t all) { return (int)(((x + 1) * runs_of(a, all) - 1) / all); }
 template <int QB, int UNIT, bool PLAN> struct Walk {
-  int id;                                 // the block's number
+  int id, part;                           // with a plan: the run; else tile and head (tile + head * tiles), and the range
   int64_t x, x1;                          // with a plan: units to do
-  __device__ __forceinline__ Walk(const PagedArgs& a, int block) : id(block), x(0), x1(0) {
+  // of block `block`; all first ranges come first, then the second ones: the last to start are those that only the longest tiles have
+  __device__ __forceinline__ Walk(const PagedArgs& a, int block) : Walk(a, PLAN ? block : block % (a.tiles * a.hk), PLAN ? 0 : block / (a.tiles * a.hk)) {}
+  __device__ __forceinline__ Walk(const PagedArgs& a, int id_, int part_) : id(id_), part(part_), x(0), x1(0) {
     if constexpr (PLAN) {
       const int64_t all = (int64_t)uniform_i32(a.plan + a.tiles) * a.hk;
       if (id < runs_of(a, all)) {
@@ -185,11 +187,11 @@ template <int QB, int UNIT, bool PLAN> struct Walk {
   }
   __device__ __forceinline__ bool next(const PagedArgs& a, Piece& p) {
     if constexpr (!PLAN) {                                    // one piece
-      const int part = __builtin_amdgcn_readfirstlane(id % a.parts), at = id / a.parts;
-      if (!locate<QB>(a, at % a.tiles, at / a.tiles, p.b)) return false;
+      const int part = __builtin_amdgcn_readfirstlane(this->part);
+      if (!locate<QB>(a, id % a.tiles, id / a.tiles, p.b)) return false;
       p.k0 = part * a.part_keys;
       p.k1 = p.b.end < p.k0 + a.part_keys || a.parts == 1 ? p.b.end : p.k0 + a.part_keys;
-      p.slot = a.parts > 1 && p.b.end > a.part_keys ? id : -1;
+      p.slot = a.parts > 1 && p.b.end > a.part_keys ? __builtin_amdgcn_readfirstlane(id) * a.parts + part : -1;
       return p.k0 < p.k1 || part == 0;
     } else {
       if (x >= x1) return false;
@@ -431,8 +433,8 @@ inline int64_t tiles_of_call(const PagedArgs& a, int qb) {
   return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
 }
 // A kind of block: its rows, how many the chip holds, the keys of a step, the steps that a range has at least, and in units of 10 ns a step where all of them are
-// held, a step where no more than half are, and what is done around the steps.
-struct Kind { int qb, slots, keys, least; int64_t full, half, around; };
+// held, a step where no more than half are, a step of the longest of many unequal blocks, and what is done around the steps.
+struct Kind { int qb, slots, keys, least; int64_t full, half, last, around; };
 // The kind and the ranges by an estimate of the time.  One sequence, seen whole: rounds of equal blocks.  Sequences of several lengths and causal borders: all
 // the work, with a little over half of the bound's keys on average, and half of the longest block at the end; at least that block.  Ranges cost a launch
 // and their partial results, written and read at 4.2 TB/s, and a little for each that the estimate does not see.  Where blocks fill the chip many times over there
@@ -451,7 +453,8 @@ inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_
         cost = blocks / k->slots * whole + (last > k->slots / 2 ? whole : last > 0 ? thin : 0);
       } else {
         cost = blocks * (steps * k->full * 11 / 20 + k->around) / k->slots + steps * k->half / 2;
-        cost = cost > thin ? cost : thin;
+        const int64_t longest = steps * (blocks * 2 > k->slots ? k->last : k->half) + k->around;
+        cost = cost > longest ? cost : longest;
       }
       if (parts > 1) cost += 775 + 25 * parts + blocks * k->qb * (head_dim + 2) * 8 / 42000;
       if (cost < best) { best = cost; r.qb = k->qb; r.tiles = n; r.parts = (int)parts; r.part_keys = (int)(steps * k->keys); }

@@ -461,11 +461,11 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   constexpr int W = WIDE ? 8 : 4, QB = W * 32, NS = WIDE ? (CODES ? 3 : 4) : 2;   // wavefronts, rows of a block, LDS stages of keys and of values
   extern __shared__ uint4 smem[];            // NS key tiles, NS value tiles
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // blocks are handed out to the eight XCDs in turn: each gets a run of tiles, whose neighbours share keys in its L2
-  const int total = a.tiles * a.hk * a.parts, per = (total + 7) >> 3;
-  const int pid = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  // blocks are handed out to the eight XCDs in turn: each gets a run of tiles, whose neighbours share keys in its L2, a head's first ranges before its second ones
+  const int of_head = a.tiles * a.parts, total = of_head * a.hk, per = (total + 7) >> 3;
+  const int pid = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3), hk = pid / of_head, part = (pid - hk * of_head) / a.tiles;
   if ((int)(blockIdx.x >> 3) >= per || pid >= total) return;
-  Walk<QB, 64, false> walk(a, pid);
+  Walk<QB, 64, false> walk(a, pid - hk * of_head - part * a.tiles + hk * a.tiles, part);
   Piece p;
   if (!walk.next(a, p)) return;
   const Block& b = p.b;
@@ -693,8 +693,8 @@ Route route(const PagedArgs& a, int head_dim) {
     // Measured: heads of 128, 6240 x 9360 x 40: 955 us with 256 rows, 986 with 128; 1560 x 20280 x 12: 256 rows in three ranges 206, 128 rows in one 408 (half the
     // chip's blocks), in eight 224; sequences of 2000, 1000, 3000 x 2000, 5000, 3000 x 16, causal: 191 and 163, in two ranges 231 and 191.  Heads of 64, 8192 x
     // 8192 x 32: 541 and 504.
-    static const Kind wide[2] = {{256, 256, 64, 8, 157, 157, 800}, {128, 512, 64, 8, 163, 130, 600}},
-                      narrow[2] = {{256, 256, 64, 8, 100, 100, 800}, {128, 512, 64, 8, 94, 80, 600}};
+    static const Kind wide[2] = {{256, 256, 64, 8, 157, 157, 157, 800}, {128, 512, 64, 8, 163, 130, 130, 600}},
+                      narrow[2] = {{256, 256, 64, 8, 100, 100, 100, 800}, {128, 512, 64, 8, 94, 80, 80, 600}};
     choose(a, head_dim == 128 ? wide : narrow, 2, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;

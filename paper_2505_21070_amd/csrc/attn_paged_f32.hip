@@ -228,7 +228,7 @@ Route route(const PagedArgs& a, int head_dim) {
   } else {
     // Measured: 64 x 8192 keys x 16 heads of 128 2.9 us a step; 4096 x 4096 x 12 in rounds of 512 blocks and 256: 966 us.  Blocks of 128 rows (two columns a
     // wavefront) are no faster at any size: 5.2 us a step, and 1026 us.
-    static const Kind wide{64, 512, 32, 4, 450, 290, 800}, narrow{64, 512, 32, 4, 250, 160, 800};
+    static const Kind wide{64, 512, 32, 4, 450, 290, 450, 800}, narrow{64, 512, 32, 4, 250, 160, 250, 800};
     choose(a, head_dim == 128 ? &wide : &narrow, 1, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
