@@ -432,9 +432,9 @@ inline int64_t tiles_of_call(const PagedArgs& a, int qb) {
   const int64_t each = ((int64_t)a.max_q * a.shared + qb - 1) / qb, all = a.n_tokens * a.shared / qb + a.n_seqs;
   return each == 1 ? (int64_t)a.n_seqs : each * a.n_seqs < all ? each * a.n_seqs : all;
 }
-// A kind of block: its rows, how many the chip holds, the keys of a step, the steps that a range has at least, and in units of 10 ns a step where all of them are
-// held, a step where no more than half are, a step of the longest of many unequal blocks, and what is done around the steps.
-struct Kind { int qb, slots, keys, least; int64_t full, half, last, around; };
+// A kind of block: its rows, the keys of a step, the steps that a range has at least, how many a CU holds, beside how many the longest of unequal blocks is taken
+// to run at most, and in units of 10 ns a step with 1, 2 .. of them on a CU, and what is done around the steps.
+struct Kind { int qb, keys, least, per_cu, beside; int64_t step[4], around; };
 // The kind and the ranges by an estimate of the time.  One sequence, seen whole: rounds of equal blocks.  Sequences of several lengths and causal borders: all
 // the work, with a little over half of the bound's keys on average, and half of the longest block at the end; at least that block.  Ranges cost a launch
 // and their partial results, written and read at 4.2 TB/s, and a little for each that the estimate does not see.  Where blocks fill the chip many times over there
@@ -443,17 +443,18 @@ inline void choose(const PagedArgs& a, const Kind* kinds, int n_kinds, int head_
   const bool even = a.n_seqs == 1 && a.group == 0;
   int64_t best = INT64_MAX;
   for (const Kind* k = kinds; k < kinds + n_kinds; ++k) {
-    const int64_t n = tiles_of_call(a, k->qb), key_tiles = (a.max_kv + k->keys - 1) / k->keys;
+    const int64_t n = tiles_of_call(a, k->qb), key_tiles = (a.max_kv + k->keys - 1) / k->keys, slots = k->per_cu * 256;
     for (int64_t parts = 1; parts <= 32; ++parts) {
-      const int64_t blocks = n * a.hk * parts, steps = (key_tiles + parts - 1) / parts, last = blocks % k->slots;
-      if (parts > 1 && (steps < k->least || blocks > 16 * k->slots)) break;
-      const int64_t whole = steps * k->full + k->around, thin = steps * k->half + k->around;
+      const int64_t blocks = n * a.hk * parts, steps = (key_tiles + parts - 1) / parts;
+      if (parts > 1 && (steps < k->least || blocks > 16 * slots)) break;
+      const int64_t full = steps * k->step[k->per_cu - 1] + k->around;
       int64_t cost = 0;
       if (even) {
-        cost = blocks / k->slots * whole + (last > k->slots / 2 ? whole : last > 0 ? thin : 0);
+        const int64_t last = blocks % slots;
+        cost = blocks / slots * full + (last > 0 ? steps * k->step[(last - 1) / 256] + k->around : 0);
       } else {
-        cost = blocks * (steps * k->full * 11 / 20 + k->around) / k->slots + steps * k->half / 2;
-        const int64_t longest = steps * (blocks * 2 > k->slots ? k->last : k->half) + k->around;
+        const int64_t on_cu = (blocks + 255) / 256, longest = steps * k->step[(on_cu < k->beside ? on_cu : k->beside) - 1] + k->around;
+        cost = blocks * (steps * k->step[k->per_cu - 1] * 11 / 20 + k->around) / slots + steps * k->step[0] / 2;
         cost = cost > longest ? cost : longest;
       }
       if (parts > 1) cost += 775 + 25 * parts + blocks * k->qb * (head_dim + 2) * 8 / 42000;

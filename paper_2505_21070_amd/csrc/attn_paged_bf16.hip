@@ -693,8 +693,8 @@ Route route(const PagedArgs& a, int head_dim) {
     // Measured: heads of 128, 6240 x 9360 x 40: 955 us with 256 rows, 986 with 128; 1560 x 20280 x 12: 256 rows in three ranges 206, 128 rows in one 408 (half the
     // chip's blocks), in eight 224; sequences of 2000, 1000, 3000 x 2000, 5000, 3000 x 16, causal: 191 and 163, in two ranges 231 and 191.  Heads of 64, 8192 x
     // 8192 x 32: 541 and 504.
-    static const Kind wide[2] = {{256, 256, 64, 8, 157, 157, 157, 800}, {128, 512, 64, 8, 163, 130, 130, 600}},
-                      narrow[2] = {{256, 256, 64, 8, 100, 100, 100, 800}, {128, 512, 64, 8, 94, 80, 80, 600}};
+    static const Kind wide[2] = {{256, 64, 8, 1, 1, {157}, 800}, {128, 64, 8, 2, 1, {130, 163}, 600}},
+                      narrow[2] = {{256, 64, 8, 1, 1, {100}, 800}, {128, 64, 8, 2, 1, {80, 94}, 600}};
     choose(a, head_dim == 128 ? wide : narrow, 2, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;

@@ -151,7 +151,7 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
 // Four wavefronts.  QG = 4: each has 16 rows of its own, and they share tiles of 32 keys.  QG = 1: all have the same 16 rows and deal the keys
 // out in tiles of 16 (wavefront w: tiles w, w + 4, ...), and meet in LDS at the end.  Either way the next tile is on its way in registers.
 template <int HD, int QG, bool CODES>
-__global__ __launch_bounds__(256) void k_paged_f32(const PagedArgs a) {
+__global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged_f32(const PagedArgs a) {
   constexpr int NT = 1, KG = 4 / QG, TK = QG == 1 ? 16 : 32, KT = TK / 16, RS = HD + 4, QB = QG * NT * 16, TILE = TK * RS;
   constexpr int JOIN = QG == 1 ? 4 * 16 * 2 + 4 * 16 * RS : 0, SIZE = KG * 2 * TILE;
   __shared__ __align__(16) float smem[SIZE > JOIN ? SIZE : JOIN];
@@ -226,9 +226,9 @@ Route route(const PagedArgs& a, int head_dim) {
     r.parts = r.part_keys > 0 ? (int)((keys + r.part_keys - 1) / r.part_keys) : 1;
     if (r.parts < 1) r.parts = 1;
   } else {
-    // Measured: 64 x 8192 keys x 16 heads of 128 2.9 us a step; 4096 x 4096 x 12 in rounds of 512 blocks and 256: 966 us.  Blocks of 128 rows (two columns a
-    // wavefront) are no faster at any size: 5.2 us a step, and 1026 us.
-    static const Kind wide{64, 512, 32, 4, 450, 290, 450, 800}, narrow{64, 512, 32, 4, 250, 160, 250, 800};
+    // Measured: a step of 32 keys takes 2.8, 4.8 and 7.0 us with one, two and three blocks on a CU (heads of 64: 1.6, 2.6, 3.8 and 4.9).  Blocks of 128 rows (two
+    // columns a wavefront) are no faster at any size.
+    static const Kind wide{64, 32, 4, 3, 3, {279, 484, 703}, 800}, narrow{64, 32, 4, 4, 4, {158, 260, 377, 492}, 800};
     choose(a, head_dim == 128 ? &wide : &narrow, 1, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
