@@ -454,7 +454,8 @@ __device__ __forceinline__ void round(State<HD>& s, float scale, const lds_char*
 // The softmax's reference is fixed to a row's maximum over the first 32 keys: weights (bf16) and fp32 sums have 8 exponent bits, so nothing is lost until
 // a sum, of weights or of weighted values, is beyond 2^100; a block with such a row, or one that is not finite, is done again tile by tile, with the reference of those rows raised as in the
 // classical online softmax (the other rows get the same bits).  So are the tiles that hold a border, for all rows.
-// What bounds it: the matrix pipes.
+// What bounds it: the matrix pipes, where blocks fill the chip.  6240 x 9360 x 40 heads of 128 in 8 bits 995 us, 1.20 PFLOP/s; 1560 x 20280 x 12 as they are in
+// three ranges 187 us and 9 of joining, 1.0; heads of 64, 8192 x 8192 x 32, 519 us, 1.06.
 template <int HD, bool WIDE, bool CODES>
 __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const PagedArgs a) {
   constexpr int KS = HD / 32, DT = HD / 16, TILE = 64 * HD * 2;   // bytes

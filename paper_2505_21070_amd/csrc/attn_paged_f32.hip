@@ -5,7 +5,8 @@
 // head dim's order in the first product is free: a lane takes 16 bytes of a key's or query's row and uses their four values in four steps.
 // LDS rows are padded by 16 bytes, so that 16 rows of 16 bytes spread over the 64 banks.  The order of O^T's rows is free as well: a lane reads its
 // channels of a value's row with 16-byte reads.
-// The matrix pipe does 1/16 of bf16's rate, so everything else hides behind it.
+// The matrix pipe does 1/16 of bf16's rate, so everything else hides behind it: 4096 x 4096 x 16 heads of 128 1148 us, 120 TFLOP/s, of 64 585 us, 117; one
+// token's rows are bound by memory: 64 sequences of 2000 keys, 8 heads of 128, 193 us, 5.4 TB/s.
 #include <math.h>
 
 #include "attn_paged.h"
@@ -149,7 +150,8 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
 }
 
 // Four wavefronts.  QG = 4: each has 16 rows of its own, and they share tiles of 32 keys.  QG = 1: all have the same 16 rows and deal the keys
-// out in tiles of 16 (wavefront w: tiles w, w + 4, ...), and meet in LDS at the end.  Either way the next tile is on its way in registers.
+// out in tiles of 16 (wavefront w: tiles w, w + 4, ...), and meet in LDS at the end.  Either way the next tile is on its way in registers.  Registers are bounded for
+// three blocks on a CU (heads of 64: four): 4096 x 4096 x 16 heads 1242 -> 1148 us.
 template <int HD, int QG, bool CODES>
 __global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged_f32(const PagedArgs a) {
   constexpr int NT = 1, KG = 4 / QG, TK = QG == 1 ? 16 : 32, KT = TK / 16, RS = HD + 4, QB = QG * NT * 16, TILE = TK * RS;
