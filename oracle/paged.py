@@ -28,9 +28,8 @@ def fp8_power(x):
     x = np.abs(np.asarray(x, np.float64))
     top = np.where(np.isfinite(x), x, 0.0).max(-1)
     e = np.full(top.shape, MIN_POWER)
-    for i, t in np.ndenumerate(top):
-        while t > FP8_MAX * 2.0 ** e[i]:
-            e[i] += 1
+    while (more := top > FP8_MAX * 2.0 ** e.astype(np.float64)).any():
+        e[more] += 1
     return e
 
 
