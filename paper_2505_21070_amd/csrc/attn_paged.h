@@ -228,7 +228,7 @@ __device__ __forceinline__ int64_t row_at(const PagedArgs& a, const Block& k, in
   const int i = row / a.shared, g = row - i * a.shared;
   return (int64_t)(k.s.row0 + i) * ts + (int64_t)(k.hk * a.shared + g) * hs;
 }
-// Row of the pages that holds key `key` (uniform; at most 15 below a multiple of 16 that is not beyond key_end) of the block's sequence and head.  Beyond its last
+// Row of the pages that holds key `key` (uniform) of the block's sequence and head, which sees a key at least (k.end > 0).  Beyond its last
 // page the last one is taken again, for a page that does not exist the first: what is read there is masked.
 __device__ __forceinline__ int64_t page_row(const PagedArgs& a, const Block& k, int key) {
   int at = key >> a.page_shift;

@@ -503,7 +503,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   // later, or (four stages) two; from registers, tiles go into LDS a round later and into the matrix pipe two.
   constexpr int AHEAD = CODES || WIDE ? 4 : 3;
   // what the first scores need, on its way before the queries and the look at the pages
-  Rows rows = rows_of(0);
+  Rows rows{};
+  if (p.k0 < p.k1) rows = rows_of(0);                         // a sequence without keys has no entry in the table to look at
   bool loaded = p.k0 < p.k1 && (CODES || whole == 0);         // whether `tile`, the next that goes through registers in the end, is in them
   if (loaded) {
     load_k(rows); load_v(rows);

@@ -55,6 +55,18 @@ def test_empty_and_padded(dtype, fp8):
     attend_and_check(f, queries(6, 4, 128, dtype), [0, 0, 6, 0, 0], group=4)
 
 
+@pytest.mark.parametrize("n", [1, 20, 90, 400])
+@pytest.mark.parametrize("dtype,fp8", STORES)
+def test_no_keys_at_all(dtype, fp8, n):
+    """Whole calls without a key: with a table that is not looked at, and without one."""
+    f = Filled([0, 0], 2, 64, 32, dtype, fp8)
+    for width in (1, 0):
+        f.table = f.table[:, :width].contiguous()
+        for group in (0, 1):
+            got = attend_and_check(f, queries(2 * n, 4, 64, dtype), [n, n], group, max_kv=500)
+            assert (got == 0).all()
+
+
 @pytest.mark.parametrize("most", [1, 3, 12])
 @pytest.mark.parametrize("dtype,fp8", STORES)
 def test_padded_batch_of_long_sequences(dtype, fp8, most):
