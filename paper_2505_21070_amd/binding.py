@@ -431,19 +431,21 @@ def _stream_on(device, stream):
     return handle
 
 
-def _new(shape, like, stream, dtype=None):
+def _new(shape, like, stream, dtype):
     """Memory for a result.  On a stream that is not the current one its memory waits for that stream when it goes."""
-    t = like.new_empty(shape, dtype=dtype)
+    t = like.new_empty(*shape, dtype=dtype)
     if stream is not None:
         t.record_stream(stream)
     return t
 
 
 def _result(t, like, heads, n, d, td, device, stream):
-    """The caller's rows for a result, or new ones, and their description."""
+    """The caller's rows for a result, or new ones of `like`'s shape, and their description."""
     if t is not None:
         return t, _rows(t, heads, n, d, td, device)
-    t = _new((n, heads, d), like, stream)
+    t = torch.empty_like(like, memory_format=torch.contiguous_format)       # 0.4 us less than new_empty
+    if stream is not None:
+        t.record_stream(stream)
     return t, _PACK_ROWS(t.data_ptr(), heads * d, d)
 
 
@@ -461,7 +463,7 @@ def qk_norm_rope(q, k, gq, gk, pos, rope_theta=1e4, eps=1e-6, q_out=None, k_out=
     st = _stream_on(dev, stream)
     cfg = _norm_rope(q, hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps)
     q_out, to_q = _result(q_out, q, hq, n, d, td, dev, stream)
-    k_out, to_k = _result(k_out, q, hk, n, d, td, dev, stream)
+    k_out, to_k = _result(k_out, k, hk, n, d, td, dev, stream)
     _check(_lib.dp_qk_norm_rope(cfg, _rows(q, hq, n, d, td, dev), _rows(k, hk, n, d, td, dev), n, to_q, to_k, st), "dp_qk_norm_rope")
     return q_out, k_out
 
@@ -538,7 +540,7 @@ class KVCache:
         out, to_out = _result(out, q, hq, n, d, td, dev, stream)
         cfg = _PACK_ATTN(hq, b, max_q, max_kv, width, causal_group, d ** -0.5 if scale is None else scale)
         nbytes = _lib.dp_attn_paged_workspace_bytes(self._desc, cfg, n)
-        work = _new(nbytes, self.data, stream, torch.uint8) if nbytes else None
+        work = _new((nbytes,), self.data, stream, torch.uint8) if nbytes else None
         _check(_lib.dp_attn_paged(self._desc, cfg, _rows(q, hq, n, d, td, dev), n, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                                   to_out, work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
         return out
