@@ -228,15 +228,32 @@ __device__ __forceinline__ int64_t row_at(const PagedArgs& a, const Block& k, in
   const int i = row / a.shared, g = row - i * a.shared;
   return (int64_t)(k.s.row0 + i) * ts + (int64_t)(k.hk * a.shared + g) * hs;
 }
-// Row of the pages that holds key `key` (uniform) of the block's sequence and head, which sees a key at least (k.end > 0).  Beyond its last
-// page the last one is taken again, for a page that does not exist the first: what is read there is masked.
-__device__ __forceinline__ int64_t page_row(const PagedArgs& a, const Block& k, int key) {
-  int at = key >> a.page_shift;
+// Rows of the pages that hold keys key_of(0), key_of(1) .. (uniform) of the block's sequence and head, which sees a key at least (k.end > 0).  Beyond its last
+// page the last one is taken again, for a page that does not exist the first: what is read there is masked.  All entries of the table are asked for
+// before the first is looked at.
+template <int G, typename KeyOf> __device__ __forceinline__ void page_rows(const PagedArgs& a, const Block& k, int64_t (&at)[G], KeyOf&& key_of) {
   const int last = (k.end - 1) >> a.page_shift;
-  at = at < last ? at : last;
-  const int page = uniform_i32(a.table + (int64_t)k.b * a.table_width + at);
-  return (((int64_t)((uint32_t)page < (uint32_t)a.n_pages ? page : 0) * 2 * a.hk + k.hk) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+  const int32_t* const table = a.table + (int64_t)k.b * a.table_width;
+  int32_t page[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int p = key_of(g) >> a.page_shift;
+    page[g] = uniform_i32(table + (p < last ? p : last));
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+    at[g] = (((int64_t)((uint32_t)page[g] < (uint32_t)a.n_pages ? page[g] : 0) * 2 * a.hk + k.hk) << a.page_shift) + (key_of(g) & ((1 << a.page_shift) - 1));
 }
+// A tile of keys comes in N trips of W wavefronts, RW rows each (powers of two).  Pages hold whole groups of 16 keys, so trips that share such a group share a look
+// at the table: `at` has the first row of each group, or where a trip takes 16 rows and more, this wavefront's first row of each trip.
+template <int N, int W, int RW> struct TileRows {
+  static constexpr int SHARE = W * RW >= 16 ? 1 : 16 / (W * RW) < N ? 16 / (W * RW) : N, G = N / SHARE;
+  int64_t at[G];
+  __device__ __forceinline__ void look(const PagedArgs& a, const Block& b, int key0, int w) {
+    page_rows(a, b, at, [&](int g) __attribute__((always_inline)) { return SHARE == 1 ? key0 + (g * W + w) * RW : key0 + g * 16; });
+  }
+  __device__ __forceinline__ int64_t row(int i, int w) const { return SHARE == 1 ? at[i] : at[i / SHARE] + w * RW + i % SHARE * (W * RW); }
+};
 // whether the page of a key below k.end exists
 __device__ __forceinline__ bool page_exists(const PagedArgs& a, const Block& k, int key) {
   return (uint32_t)a.table[(int64_t)k.b * a.table_width + (key >> a.page_shift)] < (uint32_t)a.n_pages;

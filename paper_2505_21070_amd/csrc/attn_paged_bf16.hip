@@ -79,35 +79,35 @@ template <int HD, int TK, int W, bool CODES> struct Carry {
   Raw raw[N];
   uint32_t byte[CODES ? N : 1];
   // where the trips' rows lie in the pages, for keys key0 .. of the block's sequence: uniform
-  struct Rows { int64_t at[N]; };
+  typedef TileRows<N, W, RW> Rows;
   static __device__ __forceinline__ Rows rows(const PagedArgs& a, const Block& b, int key0, int w) {
     Rows r;
-#pragma unroll
-    for (int i = 0; i < N; ++i) r.at[i] = page_row(a, b, key0 + (i * W + w) * RW);
+    r.look(a, b, key0, w);
     return r;
   }
   // to_values: rows between a head's keys and its values
-  __device__ __forceinline__ void load(const PagedArgs& a, const Rows& rows, int64_t to_values, int lane) {
+  __device__ __forceinline__ void load(const PagedArgs& a, const Rows& rows, int64_t to_values, int w, int lane) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t row = rows.at[i] + to_values;
+      const int64_t row = rows.row(i, w) + to_values;
       raw[i] = *(const Raw*)((const char*)a.data + row * ROW + lane * LB);
       if constexpr (CODES) byte[i] = (a.scales + row)[lane / (ROW / LB)];
     }
   }
   template <bool VALUES> __device__ __forceinline__ void store(uint32_t tile, int w, int lane) const {
+    // rows of a trip differ from the first trip's in higher bits, and the exchange takes each bit by itself: few addresses, the rest in the instructions' offsets
+    const int row = w * RW + lane / (ROW / LB);
+    const uint32_t in_row = lane % (ROW / LB) * LB * (CODES ? 2 : 1) ^ (VALUES ? v_swizzle<HD>(row) : k_swizzle<HD>(row)) * 16, at = tile + row * HD * 2;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int row = (i * W + w) * RW + lane / (ROW / LB), s = (VALUES ? v_swizzle<HD>(row) : k_swizzle<HD>(row)) * 16;
-      const uint32_t at = tile + row * HD * 2;
+      const uint32_t x = (VALUES ? v_swizzle<HD>(i * W * RW) : k_swizzle<HD>(i * W * RW)) * 16, off = i * W * RW * HD * 2;
       if constexpr (!CODES) {
-        lds_put(at + (lane % (ROW / LB) * LB ^ s), raw[i]);
+        lds_put(lds_base((in_row ^ x) + at) + off, raw[i]);
       } else {
         const float f = __uint_as_float(byte[i] << 23);
-        const int c = lane % (ROW / LB) * LB * 2;
 #pragma unroll
         for (int h = 0; h < LB / 8; ++h)
-          lds_put(at + ((c + h * 16) ^ s), __builtin_bit_cast(u32x4, fp8x8_to_bf16(make_uint2(raw[i][2 * h], raw[i][2 * h + 1]), f)));
+          lds_put(lds_base((in_row ^ x ^ h * 16) + at) + off, __builtin_bit_cast(u32x4, fp8x8_to_bf16(make_uint2(raw[i][2 * h], raw[i][2 * h + 1]), f)));
       }
     }
   }
@@ -162,32 +162,29 @@ __device__ __forceinline__ void weighted_sum_checked(uint32_t tile, uint32_t vla
       continue;
     }
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    uint32_t fin[4], pos[4], neg[4], nan[4];
+    // one kind of value after the other: all at once would take registers from the loop around
+    auto operand = [&](auto&& of) __attribute__((always_inline)) {
+      uint32_t x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      fin[i] = w[i]; pos[i] = neg[i] = nan[i] = 0;
+      for (int i = 0; i < 4; ++i) x[i] = of(w[i] & 0xffffu) | of(w[i] >> 16) << 16;
+      __builtin_amdgcn_sched_barrier(0);
+      return __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+    };
+    const bf16x8 finite = operand([](uint32_t x) __attribute__((always_inline)) { return (x & 0x7f80u) == 0x7f80u ? 0u : x; });
 #pragma unroll
-      for (int h = 0; h < 32; h += 16) {
-        const uint32_t x = (w[i] >> h) & 0xffffu;
-        if ((x & 0x7f80u) == 0x7f80u) fin[i] &= ~(0xffffu << h);
-        pos[i] |= (x == 0x7f80u ? 0x3f80u : 0u) << h;
-        neg[i] |= (x == 0xff80u ? 0x3f80u : 0u) << h;
-        nan[i] |= ((x & 0x7fffu) > 0x7f80u ? 0x3f80u : 0u) << h;
+    for (int t = 0; t < NT; ++t) o[d][t] = mfma(finite, __builtin_bit_cast(bf16x8, pf[t]), o[d][t]);
+    auto add = [&](auto&& of, auto&& to) __attribute__((always_inline)) {   // to(value) for rows that see one of the kind that has ones in of(bits)
+      const bf16x8 kind = operand(of);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const f32x4 n = mfma(kind, __builtin_bit_cast(bf16x8, seen[t]), f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[d][t][r] = n[r] > 0.f ? to(o[d][t][r]) : o[d][t][r];
       }
-    }
-    auto vec = [](const uint32_t (&x)[4]) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3])); };
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const f32x4 zero{0.f, 0.f, 0.f, 0.f};
-      const bf16x8 ones = __builtin_bit_cast(bf16x8, seen[t]);
-      const f32x4 np = mfma(vec(pos), ones, zero), nn = mfma(vec(neg), ones, zero), nx = mfma(vec(nan), ones, zero);
-      o[d][t] = mfma(vec(fin), __builtin_bit_cast(bf16x8, pf[t]), o[d][t]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float x = o[d][t][r] + (np[r] > 0.f ? INFINITY : 0.f) - (nn[r] > 0.f ? INFINITY : 0.f);
-        o[d][t][r] = nx[r] > 0.f ? __uint_as_float(0x7fc00000u) : x;
-      }
-    }
+    };
+    add([](uint32_t x) __attribute__((always_inline)) { return x == 0x7f80u ? 0x3f80u : 0u; }, [](float y) __attribute__((always_inline)) { return y + INFINITY; });
+    add([](uint32_t x) __attribute__((always_inline)) { return x == 0xff80u ? 0x3f80u : 0u; }, [](float y) __attribute__((always_inline)) { return y - INFINITY; });
+    add([](uint32_t x) __attribute__((always_inline)) { return (x & 0x7fffu) > 0x7f80u ? 0x3f80u : 0u; }, [](float) __attribute__((always_inline)) { return __uint_as_float(0x7fc00000u); });
   }
 }
 // ones where a score is above -inf
@@ -224,6 +221,7 @@ __device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uin
     } else {
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) {
+        if (NT > 1 && d % 4 == 0) __builtin_amdgcn_sched_barrier(0);         // else all values are read at once, into registers that are not there
         const bf16x8 vf = read_v<HD>(vtile, v_lane<HD>(lane), s, d);
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[d][t] = mfma(vf, __builtin_bit_cast(bf16x8, p[t]), o[d][t]);
@@ -290,8 +288,8 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
     int key = p.k0 + wave * 32;
     auto load = [&](int at) __attribute__((always_inline)) {
       const auto rows = ck.rows(a, b, at, 0);
-      ck.load(a, rows, 0, lane);
-      cv.load(a, rows, to_values, lane);
+      ck.load(a, rows, 0, 0, lane);
+      cv.load(a, rows, to_values, 0, lane);
     };
     if (key < p.k1) load(key);
     const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1));
@@ -353,7 +351,7 @@ template <int HD, int W> struct Direct {
 #ifdef __HIP_DEVICE_COMPILE__
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const char* const from = (const char*)a.data + (rows.at[i] + to_values) * (HD * 2);
+      const char* const from = (const char*)a.data + (rows.row(i, w) + to_values) * (HD * 2);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7fffffff, 0x00020000), (lds_void_t*)(tile + (i * W + w) * 1024), 16, place, 0, 0, 0);
     }
 #endif
@@ -488,8 +486,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   typedef decltype(rows_of(0)) Rows;
   auto direct_k = [&](const Rows& rows, lds_char* to) __attribute__((always_inline)) { Loads::load(a, rows, 0, direct.k, to, wave); };
   auto direct_v = [&](const Rows& rows, lds_char* to) __attribute__((always_inline)) { Loads::load(a, rows, to_values, direct.v, to, wave); };
-  auto load_k = [&](const Rows& rows) __attribute__((always_inline)) { ck.load(a, rows, 0, lane); };
-  auto load_v = [&](const Rows& rows) __attribute__((always_inline)) { cv.load(a, rows, to_values, lane); };
+  auto load_k = [&](const Rows& rows) __attribute__((always_inline)) { ck.load(a, rows, 0, wave, lane); };
+  auto load_v = [&](const Rows& rows) __attribute__((always_inline)) { cv.load(a, rows, to_values, wave, lane); };
   auto store_k = [&](int j) __attribute__((always_inline)) { ck.template store<false>(kst + (j % NS) * TILE, wave, lane); };
   auto store_v = [&](int j) __attribute__((always_inline)) { cv.template store<true>(vst + (j % NS) * TILE, wave, lane); };
   auto load_both = [&](int at) __attribute__((always_inline)) {

@@ -23,10 +23,11 @@ template <int HD, int TK, int W, bool CODES> struct Carry {
   typedef typename std::conditional<CODES, uint32_t, f32x4>::type Raw;
   Raw raw[N];
   uint32_t byte[CODES ? N : 1];
-  __device__ __forceinline__ void load(const PagedArgs& a, const Block& b, int key0, int64_t to_values, int w, int lane) {
+  typedef TileRows<N, W, RW> Rows;
+  __device__ __forceinline__ void load(const PagedArgs& a, const Rows& rows, int64_t to_values, int w, int lane) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t row = page_row(a, b, key0 + (i * W + w) * RW) + to_values;
+      const int64_t row = rows.row(i, w) + to_values;
       raw[i] = *(const Raw*)((const char*)a.data + row * (HD * (CODES ? 1 : 4)) + lane * sizeof(Raw));
       if constexpr (CODES) byte[i] = (a.scales + row)[lane / LANES];
     }
@@ -170,7 +171,12 @@ __global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged
   float* const vt = kt + TILE;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
   Carry<HD, TK, QG, CODES> ck, cv;
-  auto load = [&](int at) __attribute__((always_inline)) { ck.load(a, b, at, 0, qt, lane); cv.load(a, b, at, to_values, qt, lane); };
+  auto load = [&](int at) __attribute__((always_inline)) {
+    typename decltype(ck)::Rows rows;
+    rows.look(a, b, at, qt);
+    ck.load(a, rows, 0, qt, lane);
+    cv.load(a, rows, to_values, qt, lane);
+  };
   const int first = k0 + kg * TK;
   if (first < k1) load(first);
 #pragma unroll
