@@ -257,7 +257,7 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
 // Few rows: NT * 16 of them, W wavefronts that deal the block's keys out in tiles of 32 (wavefront w: tiles w, w + W, ...), each through its own piece of
 // LDS, the next tile on its way in registers; nobody waits for anybody until the results are joined in LDS, in wavefront order.  W = 4: two blocks to a
 // CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory: 64 sequences of 16 .. 16000 keys, 8 heads of 128 in 8 bits, 201 us, 5.3 TB/s.  W = 8: no more
-// blocks than CUs, bound by a trip's way through LDS, 2 us for 256 keys: one token over 517 keys with 12 heads 11.4 us.
+// blocks than CUs, bound by a trip's chain of steps, 1.6 us for 256 keys: one token over 517 keys with 12 heads 10.2 us.
 template <int HD, int NT, int W, bool CODES, bool PLAN>
 __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
   constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
@@ -675,8 +675,8 @@ Route route(const PagedArgs& a, int head_dim) {
     r.tiles = tiles_of_call(a, r.qb);
     const int64_t units = (keys + 127) / 128, blocks = r.tiles * a.hk;
     if (a.n_seqs == 1 || units <= 16 || blocks * keys <= 400000) {
-      // Ranges for one block of eight wavefronts a CU, no shorter than one of their trips (256 keys), from three on: one token of 12 heads of 128 over 768 keys 11.5 us
-      // in one, 10.7 in three; over 2000 21.8 and 12.0.
+      // Ranges for one block of eight wavefronts a CU, no shorter than one of their trips (256 keys), from three on: one token of 12 heads of 128 over 767 keys 11.5 us
+      // in one, over 768 10.2 in three.
       int64_t parts = (keys + 255) / 256;
       if (parts > 256 / blocks) parts = 256 / blocks;
       if (keys >= 768 && parts > 1) {
