@@ -431,11 +431,16 @@ def _stream_on(device, stream):
     return handle
 
 
-def _new(shape, like, stream, dtype):
-    """Memory for a result.  On a stream that is not the current one its memory waits for that stream when it goes."""
-    t = like.new_empty(*shape, dtype=dtype)
-    if stream is not None:
-        t.record_stream(stream)
+def _memory(make, stream, result=True):
+    """make()'s tensor, from the pool of the stream that is going to write it: memory that another stream's pool hands out may still be in use there.
+    A result of a named stream is read on the current one, after a wait: when it goes, its memory waits for what is queued here until then.  A workspace is
+    used by its call alone, and what the pool hands out next comes behind it."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    if result:
+        t.record_stream(torch.cuda.current_stream())
     return t
 
 
@@ -443,9 +448,7 @@ def _result(t, like, heads, n, d, td, device, stream):
     """The caller's rows for a result, or new ones of `like`'s shape, and their description."""
     if t is not None:
         return t, _rows(t, heads, n, d, td, device)
-    t = torch.empty_like(like, memory_format=torch.contiguous_format)       # 0.4 us less than new_empty
-    if stream is not None:
-        t.record_stream(stream)
+    t = _memory(lambda: torch.empty_like(like, memory_format=torch.contiguous_format), stream)     # 0.4 us less than new_empty
     return t, _PACK_ROWS(t.data_ptr(), heads * d, d)
 
 
@@ -472,7 +475,10 @@ class KVCache:
     """Pages of keys and values of many sequences.  data: [n_pages, 2, kv_heads, page_tokens, head_dim], keys at [:, 0] and values at [:, 1], of
     the rows' type, or float8_e4m3fn with scales, uint8 [n_pages, 2, kv_heads, page_tokens]: byte b stands for the factor 2^(b - 127).
     The tensors are the caller's and may be looked at; dtype ("f32", "bf16") is that of the rows, given only with 8-bit data.  Which pages a sequence owns is
-    the caller's page table; a slot is page * page_tokens + place in the page."""
+    the caller's page table; a slot is page * page_tokens + place in the page.
+
+    Calls on a named stream wait for nobody: what they read has to be there, and is the caller's to keep until they have run.  Their results are to be read
+    behind them, and may be dropped by the current stream at any time."""
 
     def __init__(self, data, scales=None, dtype=None):
         td = {"f32": torch.float32, "bf16": torch.bfloat16, None: data.dtype}[dtype]
@@ -523,7 +529,7 @@ class KVCache:
         """The keys and values at the slots, [n, kv_heads, head_dim] each, zeros where a slot is outside the pool."""
         n, (d, td, dev), hk = slot.shape[0], self._like, self.kv_heads
         st = _stream_on(dev, stream)
-        k, v = _new((n, hk, d), self.data, stream, td), _new((n, hk, d), self.data, stream, td)
+        k, v = [_memory(lambda: self.data.new_empty(n, hk, d, dtype=td), stream) for _ in range(2)]
         _check(_lib.dp_kv_read(self._desc, self._slots(slot), n, _PACK_ROWS(k.data_ptr(), hk * d, d), _PACK_ROWS(v.data_ptr(), hk * d, d), st), "dp_kv_read")
         return k, v
 
@@ -540,7 +546,7 @@ class KVCache:
         out, to_out = _result(out, q, hq, n, d, td, dev, stream)
         cfg = _PACK_ATTN(hq, b, max_q, max_kv, width, causal_group, d ** -0.5 if scale is None else scale)
         nbytes = _lib.dp_attn_paged_workspace_bytes(self._desc, cfg, n)
-        work = _new((nbytes,), self.data, stream, torch.uint8) if nbytes else None
+        work = _memory(lambda: torch.empty(nbytes, dtype=torch.uint8, device=dev), stream, result=False) if nbytes else None
         _check(_lib.dp_attn_paged(self._desc, cfg, _rows(q, hq, n, d, td, dev), n, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                                   to_out, work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
         return out
