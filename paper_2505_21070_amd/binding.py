@@ -212,6 +212,19 @@ def _stream_handle(stream):
     return stream.cuda_stream
 
 
+def _memory(make, stream, result=True):
+    """make()'s tensor, from the pool of the stream that is going to write it: memory that another stream's pool hands out may still be in use there.
+    A result of a named stream is read on the current one, after a wait: when it goes, its memory waits for what is queued here until then.  A workspace is
+    used by its call alone, and what the pool hands out next comes behind it."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    if result:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 class Stage:
     """One pipeline stage on the current device.  weights: {"stage": {...}, "layers": [{...}]} of device
     tensors in the stage's dtype (contiguous; matrices [in, out], or as weights_out_in returns them when the
@@ -249,7 +262,7 @@ class Stage:
         nbytes = workspace_bytes(config)
         if nbytes == 0:
             raise DualParalError(DP_EINVAL, "dp_stage_workspace_bytes")
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        self.workspace = _memory(lambda: torch.empty(nbytes, dtype=torch.uint8, device=dev), stream)
         assert self.workspace.data_ptr() % 256 == 0
         h = C.c_void_p()
         self._h = None
@@ -262,7 +275,7 @@ class Stage:
         assert x_in.is_cuda and x_in.dtype == self.torch_dtype and x_in.is_contiguous()
         assert tuple(x_in.shape) == (n_frames * self.tok, self.config.dim), tuple(x_in.shape)
         if out is None:
-            out = torch.empty_like(x_in)
+            out = _memory(lambda: torch.empty_like(x_in), stream)
         assert out.shape == x_in.shape and out.dtype == x_in.dtype and out.is_contiguous() and out.is_cuda
         _check(_lib.dp_stage_forward(self._h, x_in.data_ptr(), out.data_ptr(), n_frames, frame0, float(timestep),
                                      _stream_handle(stream)), "dp_stage_forward")
@@ -273,7 +286,7 @@ class Stage:
 
     def peek(self, what, layer=0, stream=None):
         max_rows = max(self.config.max_block_frames * self.tok, self.config.text_len, 6)
-        buf = torch.empty((max_rows, self.config.dim), dtype=torch.float32, device=self.workspace.device)
+        buf = _memory(lambda: torch.empty((max_rows, self.config.dim), dtype=torch.float32, device=self.workspace.device), stream)
         rows = C.c_int64()
         _check(_lib.dp_stage_peek(self._h, PEEK[what], layer, buf.data_ptr(), buf.numel(), C.byref(rows),
                                   _stream_handle(stream)), "dp_stage_peek")
@@ -346,7 +359,7 @@ class Ends:
         nbytes = _lib.dp_ends_workspace_bytes(C.byref(self.config))
         if nbytes == 0:
             raise DualParalError(DP_EINVAL, "dp_ends_workspace_bytes")
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        self.workspace = _memory(lambda: torch.empty(nbytes, dtype=torch.uint8, device="cuda"), stream)
         h = C.c_void_p()
         self._h = None
         _check(_lib.dp_ends_init(C.byref(self.config), C.byref(ew), self.workspace.data_ptr(), nbytes,
@@ -356,13 +369,13 @@ class Ends:
     def embed(self, latent, stream=None):
         n = latent.shape[0]
         assert latent.is_cuda and latent.dtype == torch.float32 and latent.is_contiguous() and tuple(latent.shape[1:]) == self.frame_shape
-        out = torch.empty((n * self.tok, self.dim), dtype=self.torch_dtype, device=latent.device)
+        out = _memory(lambda: torch.empty((n * self.tok, self.dim), dtype=self.torch_dtype, device=latent.device), stream)
         _check(_lib.dp_embed_forward(self._h, latent.data_ptr(), out.data_ptr(), n, _stream_handle(stream)), "dp_embed_forward")
         return out
 
     def head(self, x, timestep, n_frames, stream=None):
         assert x.is_cuda and x.dtype == self.torch_dtype and x.is_contiguous() and tuple(x.shape) == (n_frames * self.tok, self.dim)
-        v = torch.empty((n_frames,) + self.frame_shape, dtype=torch.float32, device=x.device)
+        v = _memory(lambda: torch.empty((n_frames,) + self.frame_shape, dtype=torch.float32, device=x.device), stream)
         _check(_lib.dp_head_forward(self._h, x.data_ptr(), float(timestep), v.data_ptr(), n_frames, _stream_handle(stream)),
                "dp_head_forward")
         return v
@@ -429,19 +442,6 @@ def _stream_on(device, stream):
     assert device.type == "cuda" and device.index == now, f"tensors on {device}, not on the current device"
     assert stream is None or stream.device == device, f"a stream of {stream.device} for tensors on {device}"
     return handle
-
-
-def _memory(make, stream, result=True):
-    """make()'s tensor, from the pool of the stream that is going to write it: memory that another stream's pool hands out may still be in use there.
-    A result of a named stream is read on the current one, after a wait: when it goes, its memory waits for what is queued here until then.  A workspace is
-    used by its call alone, and what the pool hands out next comes behind it."""
-    if stream is None:
-        return make()
-    with torch.cuda.stream(stream):
-        t = make()
-    if result:
-        t.record_stream(torch.cuda.current_stream())
-    return t
 
 
 def _result(t, like, heads, n, d, td, device, stream):
