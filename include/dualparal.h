@@ -406,7 +406,7 @@ typedef struct {
   int32_t max_kv;             /* 0 .. 2^31 - 1 - 65536                                             */
   int32_t table_width;        /* >= 0                                                              */
   int32_t causal_group;       /* >= 0                                                              */
-  float scale;                /* > 0 and finite, e.g. 1 / sqrt(head_dim)                           */
+  float scale;                /* > 0, and finite times log2(e); e.g. 1 / sqrt(head_dim)            */
 } dp_attn_config;
 size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* cache, const dp_attn_config* cfg, int64_t n_tokens);   /* 0 also if an argument is invalid: dp_attn_paged says why */
 int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_rows* q, int64_t n_tokens, const int32_t* q_start,

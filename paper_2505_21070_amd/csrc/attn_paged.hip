@@ -6,6 +6,8 @@
 
 namespace {
 
+constexpr float LOG2_E = 1.4426950408889634f;
+
 const char* why_not_attn(const dp_kv_cache* c, const dp_attn_config* cfg) {
   if (const char* why = why_not_cache(c)) return why;
   if (!cfg) return "null pointer";
@@ -16,7 +18,7 @@ const char* why_not_attn(const dp_kv_cache* c, const dp_attn_config* cfg) {
   if (cfg->max_kv < 0 || cfg->max_kv > 0x7fffffff - 65536) return "max_kv must be in [0, 2^31 - 1 - 65536]";
   if (cfg->table_width < 0) return "table_width must not be negative";
   if (cfg->causal_group < 0) return "causal_group must not be negative";
-  if (!(cfg->scale > 0.f && cfg->scale < INFINITY)) return "scale must be positive and finite";
+  if (!(cfg->scale > 0.f && cfg->scale * LOG2_E < INFINITY)) return "scale must be positive, and finite times log2(e)";
   return nullptr;
 }
 
@@ -32,7 +34,7 @@ PagedArgs arguments(const dp_kv_cache* c, const dp_attn_config* cfg, int64_t n_t
   a.n_seqs = cfg->n_seqs; a.max_q = cfg->max_q < n_tokens ? cfg->max_q : (int32_t)n_tokens; a.table_width = cfg->table_width; a.group = cfg->causal_group;
   const int64_t most = (int64_t)cfg->table_width << a.page_shift;
   a.max_kv = cfg->max_kv < most ? cfg->max_kv : (int32_t)most;
-  a.scale = cfg->scale * 1.4426950408889634f;
+  a.scale = cfg->scale * LOG2_E;
   return a;
 }
 // 2^29 rows in blocks of at most 4 threads a row, and a block of at most 512 threads begun for each sequence and key head: launches stay below 2^32 threads
