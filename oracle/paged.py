@@ -44,10 +44,13 @@ def fp8_round(y):
 
 
 def fp8_rows(x):
-    """(values that the codes stand for, exponents e): the row as it reads back."""
+    """(values that the codes stand for, exponents e): the row as it reads back.  At e = 120 the codes end at 240: the next one, 256, would stand for 2^128,
+    which fp32 and bf16 do not hold."""
     e = fp8_power(x)
     s = 2.0 ** e.astype(np.float64)[..., None]
-    return fp8_round(np.asarray(x, np.float64) / s) * s, e
+    most = np.where(e == 120, 240.0, FP8_MAX)[..., None]
+    y = fp8_round(np.asarray(x, np.float64) / s)
+    return np.where(np.isnan(y), y, np.clip(y, -most, most)) * s, e
 
 
 def seen_keys(i, n, keys, group):

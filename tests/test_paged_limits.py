@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from oracle import paged as O
 from paper_2505_21070_amd import binding as B
 from test_paged_refusals import attend, attn, cache, refused
 
@@ -13,3 +14,11 @@ def test_scales_that_softmax_in_powers_of_two_does_not_hold(scale):
     assert B._lib.dp_attn_paged_workspace_bytes(cache(), attn(scale=scale), 7) == 0
     assert attend(a=attn(scale=2.3e38, max_q=0)) == B.DP_OK
 
+
+def test_codes_of_the_largest_values_stand_for_finite_ones():
+    for top in (np.finfo(np.float32).max, 1.9375 * 2.0 ** 127, 1.75 * 2.0 ** 127 * (1 + 2.0 ** -20)):
+        x = np.zeros((1, 64))
+        x[0, :3] = top, -top, np.inf
+        back, e = O.fp8_rows(x)
+        assert e[0] == 120 and np.isfinite(np.float32(back[0, :2])).all() and np.isnan(back[0, 2])
+        assert (np.abs(back[0, :2] - x[0, :2]) <= 2.0 ** -4 * top).all()
