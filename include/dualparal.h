@@ -393,7 +393,8 @@ int dp_kv_read(const dp_kv_cache* cache, const int32_t* slot, int64_t n_tokens, 
  * causal_group 0: every query sees every key.  g >= 1: keys come in groups of g (1: tokens, tok_h * tok_w: frames), and a query sees the
  * groups up to its own: with p = kv_len - n + i for the i-th of n new tokens, the keys below (p / g + 1) * g (p >= 0; a query before the
  * first key sees none).  A query that sees no key, or whose scores are all -inf, gets zeros.  What a query does not see does not touch its result, NaN and
- * infinities included.
+ * infinities included.  A value that is not finite reaches the queries that see it, however small its key's weight, unless the score is -inf: such a key weighs
+ * nothing, whatever its value.
  * max_q and max_kv size the launch: rows beyond a sequence's first max_q are left as they are, keys beyond max_kv not read.
  * Scores, softmax and sums are fp32; with DP_BF16 the weights are rounded to bf16 before they meet the values.
  *   workspace  : device, 256-byte aligned, dp_attn_paged_workspace_bytes(cache, cfg, n_tokens) bytes (0 for many calls: then it may be

@@ -84,8 +84,9 @@ def attend(q, k, v, q_start, keys_of, exists, group, scale, out):
                         continue
                     w = np.exp(s - s.max())
                     w = w / w.sum()
-                    live = ~(w == 0) | ~np.isfinite(vv).all(-1)
-                    out[t, h] = (w[live, None] * vv[live]).sum(0)
-                    mean_abs[t, h] = (w[live, None] * np.abs(vv[live])).sum(0)
+                    # a weight is above 0, however small it is in 64 bits, unless the score is -inf: values that are not finite reach the result or do not
+                    finite = np.where(np.isfinite(vv), vv, 0.0)
+                    out[t, h] = w @ finite + (vv - finite)[s != -np.inf].sum(0)
+                    mean_abs[t, h] = w @ np.abs(finite)
                     score_abs[t, h] = (np.abs(kk) @ np.abs(q[t, h])).max() * scale
     return out, mean_abs, score_abs

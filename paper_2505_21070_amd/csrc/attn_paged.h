@@ -292,6 +292,25 @@ __device__ __forceinline__ float raise(Soft& z, float top, float& ref) {
   z.l *= alpha;
   return alpha;
 }
+// What is not finite among the values that a row sees reaches its result, however small the weight: weights are above 0 in exact numbers, unless the score is
+// -inf.  So a sum that is not finite is kept where its factor is 0 in fp32, and where a loop leaves such a sum (0 * infinity is NaN as well) the keys are gone
+// through once more, with the values of every tile looked at, as those of a tile with a border always are.
+__device__ __forceinline__ f32x4 lowered(f32x4 v, float f) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = f == 0.f && !(fabsf(v[r]) < INFINITY) ? v[r] : v[r] * f;
+  return v;
+}
+__device__ __forceinline__ bool finite(f32x4 v) { return fmaf(v[0], 0.f, v[1] * 0.f) + fmaf(v[2], 0.f, v[3] * 0.f) == 0.f; }
+template <int DT, int NT> __device__ __forceinline__ bool finite(const f32x4 (&o)[DT][NT]) {
+  f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = fmaf(o[d][t][r], 0.f, x[r]);
+  return finite(x);
+}
 // Of a lane's four keys in each tile of 16 from key0 on: bit kt where their page does not exist (pages hold whole groups of 16)
 template <int KT> __device__ __forceinline__ uint32_t missing(const PagedArgs& a, const Block& b, int key0, int lane) {
   uint32_t gone = 0;
@@ -359,6 +378,10 @@ __device__ __forceinline__ void join_waves(const PagedArgs& a, const Block& b, f
         l += ml[(w * 16 + r) * 2 + 1] * f;
         v += *(const f32x4*)(os + (w * 16 + r) * OS + c) * f;
       }
+      if (!finite(v)) {
+        v = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < W; ++w) v += lowered(*(const f32x4*)(os + (w * 16 + r) * OS + c), __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - ref));
+      }
       if (slot < 0) {
         store_four((T*)a.out + row_at(a, b, b.first + row, a.o_ts, a.o_hs) + c, v * inverse(l));
       } else {
@@ -425,6 +448,10 @@ __global__ __launch_bounds__(256) void k_paged_join(const PagedArgs a) {
     const float f = __builtin_amdgcn_exp2f(p[row] - ref);
     l += p[QB + row] * f;
     v += *(const f32x4*)(p + 2 * QB + row * HD + c) * f;
+  }
+  if (!finite(v)) {
+    v = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = from; i < parts; i += SPLIT) v += lowered(*(const f32x4*)(at(i) + 2 * QB + row * HD + c), __builtin_amdgcn_exp2f(at(i)[row] - ref));
   }
   if constexpr (SPLIT > 1) {
     if (c == 0) ls[group] = l;

@@ -149,9 +149,10 @@ template <int KT> __device__ __forceinline__ void weigh(const f32x4 (&sc)[KT], f
 __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 // O^T += V^T P^T of 32 keys, NT tiles of 16 rows, where a value that is not finite must not meet the weight 0 of a row that does not see its key (0 *
 // infinity is NaN).  Values are multiplied with what is not finite set to 0; rows that do see +inf, -inf or NaN in a channel are found by
-// products of ones and get it added.  seen: B operand of ones where the row sees the key.
+// products of ones and get it added.  seen: B operand of ones where the row sees the key.  Returns whether there was any such value, seen or not.
 template <int HD, int NT>
-__device__ __forceinline__ void weighted_sum_checked(uint32_t tile, uint32_t vlane, int s, const uint4 (&pf)[NT], const uint4 (&seen)[NT], f32x4 (&o)[HD / 16][NT]) {
+__device__ __forceinline__ bool weighted_sum_checked(uint32_t tile, uint32_t vlane, int s, const uint4 (&pf)[NT], const uint4 (&seen)[NT], f32x4 (&o)[HD / 16][NT]) {
+  bool met = false;
 #pragma unroll
   for (int d = 0; d < HD / 16; ++d) {
     const uint4 v = __builtin_bit_cast(uint4, read_v<HD>(tile, vlane, s, d));
@@ -161,6 +162,7 @@ __device__ __forceinline__ void weighted_sum_checked(uint32_t tile, uint32_t vla
       for (int t = 0; t < NT; ++t) o[d][t] = mfma(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pf[t]), o[d][t]);
       continue;
     }
+    met = true;
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     // one kind of value after the other: all at once would take registers from the loop around
     auto operand = [&](auto&& of) __attribute__((always_inline)) {
@@ -186,6 +188,7 @@ __device__ __forceinline__ void weighted_sum_checked(uint32_t tile, uint32_t vla
     add([](uint32_t x) __attribute__((always_inline)) { return x == 0xff80u ? 0x3f80u : 0u; }, [](float y) __attribute__((always_inline)) { return y - INFINITY; });
     add([](uint32_t x) __attribute__((always_inline)) { return (x & 0x7fffu) > 0x7f80u ? 0x3f80u : 0u; }, [](float) __attribute__((always_inline)) { return __uint_as_float(0x7fc00000u); });
   }
+  return met;
 }
 // ones where a score is above -inf
 __device__ __forceinline__ uint4 ones_of(const f32x4& x, const f32x4& y) {
@@ -193,19 +196,25 @@ __device__ __forceinline__ uint4 ones_of(const f32x4& x, const f32x4& y) {
   return make_uint4(pair(x[0], x[1]), pair(x[2], x[3]), pair(y[0], y[1]), pair(y[2], y[3]));
 }
 // The rest of a tile of KT * 16 keys whose scores are in sc: what a row does not see (border), the classical online softmax (of_row: whether this tile may raise
-// a row's reference), the weighted sum.
-template <int HD, int KT, int NT>
-__device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uint32_t vtile, f32x4 (&sc)[NT][KT], int key0, bool border, const bool (&of_row)[NT], const int (&end)[NT], bool gaps,
+// a row's reference), the weighted sum (checked: with values looked at; KEEP: sums that are not finite are kept).  Returns whether a value looked at was not finite.
+template <int HD, int KT, int NT, bool KEEP>
+__device__ __forceinline__ bool sum_tile(const PagedArgs& a, const Block& b, uint32_t vtile, f32x4 (&sc)[NT][KT], int key0, bool border, bool checked, const bool (&of_row)[NT], const int (&end)[NT], bool gaps,
                                          Soft (&z)[NT], f32x4 (&o)[HD / 16][NT], int lane) {
   uint4 pf[NT][KT / 2];
+  bool met = false;
   const uint32_t gone = gaps ? missing<KT>(a, b, key0, lane) : 0;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (border) hide<KT>(sc[t], key0, end[t], gone, lane);
     float ref;
     const float alpha = raise(z[t], of_row[t] ? maximum<KT>(sc[t], KT) * a.scale : -INFINITY, ref);
+    if (KEEP && __any(alpha == 0.f)) {
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) o[d][t] *= alpha;
+      for (int d = 0; d < HD / 16; ++d) o[d][t] = lowered(o[d][t], alpha);
+    } else {
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) o[d][t] *= alpha;
+    }
     weigh<KT>(sc[t], a.scale, ref, z[t].l, pf[t]);
   }
 #pragma unroll
@@ -213,11 +222,11 @@ __device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uin
     uint4 p[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) p[t] = pf[t][s];
-    if (border) {
+    if (checked) {
       uint4 seen[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) seen[t] = ones_of(sc[t][2 * s], sc[t][2 * s + 1]);
-      weighted_sum_checked<HD, NT>(vtile, v_lane<HD>(lane), s, p, seen, o);
+      met |= weighted_sum_checked<HD, NT>(vtile, v_lane<HD>(lane), s, p, seen, o);
     } else {
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) {
@@ -228,18 +237,28 @@ __device__ __forceinline__ void sum_tile(const PagedArgs& a, const Block& b, uin
       }
     }
   }
+  return met;
 }
 // scores of a tile in plain order
 template <int HD, int KT, int NT>
 __device__ __forceinline__ void score_tile(uint32_t ktile, const bf16x8 (&qf)[NT][HD / 32], f32x4 (&sc)[NT][KT], int lane) {
+  // one column of rows leaves registers for all operands, which are on their way before the first product; else a step's are
+  constexpr int KS = HD / 32, AT_ONCE = NT == 1 ? KS : 1;
+  bf16x8 kf[KS][KT];
 #pragma unroll
-  for (int ks = 0; ks < HD / 32; ++ks)
+  for (int ks = 0; ks < KS; ++ks) {
+    if (ks % AT_ONCE == 0) {
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      const bf16x8 kf = read_k<HD>(ktile, k_lane<HD>(lane), kt, ks);
+      for (int i = ks; i < ks + AT_ONCE; ++i)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) sc[t][kt] = mfma(kf, qf[t][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[t][kt]);
+        for (int kt = 0; kt < KT; ++kt) kf[i][kt] = read_k<HD>(ktile, k_lane<HD>(lane), kt, i);
+      __builtin_amdgcn_sched_barrier(0);
     }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sc[t][kt] = mfma(kf[ks][kt], qf[t][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[t][kt]);
+  }
 }
 
 template <int HD, int NT>
@@ -278,12 +297,15 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
     load_queries<HD, NT>(a, b, b.first, qf, end, lane);
     Soft z[NT];
     f32x4 o[HD / 16][NT];
+    auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      z[t] = Soft{-INFINITY, 0.f};
+      for (int t = 0; t < NT; ++t) {
+        z[t] = Soft{-INFINITY, 0.f};
 #pragma unroll
-      for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+        for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    };
+    clear();
     Carry<HD, 32, 1, CODES> ck, cv;
     int key = p.k0 + wave * 32;
     auto load = [&](int at) __attribute__((always_inline)) {
@@ -293,16 +315,30 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
     };
     if (key < p.k1) load(key);
     const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1));
-    for (; key < p.k1; key += W * 32) {
-      ck.template store<false>(kt, 0, lane);
-      cv.template store<true>(vt, 0, lane);
-      if (key + W * 32 < p.k1) load(key + W * 32);
+    auto tile = [&](auto careful, int lane) __attribute__((always_inline)) {
       f32x4 sc[NT][KT];
       score_tile<HD, KT, NT>(kt, qf, sc, lane);
       bool all[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) all[t] = true;
-      sum_tile<HD, KT, NT>(a, b, vt, sc, key, key + 32 > b.whole || gaps, all, end, gaps, z, o, lane);
+      const bool border = key + 32 > b.whole || gaps;
+      sum_tile<HD, KT, NT, careful>(a, b, vt, sc, key, border, border || careful, all, end, gaps, z, o, lane);
+    };
+    for (; key < p.k1; key += W * 32) {
+      ck.template store<false>(kt, 0, lane);
+      cv.template store<true>(vt, 0, lane);
+      if (key + W * 32 < p.k1) load(key + W * 32);
+      tile(std::false_type{}, lane);
+    }
+    if (!__all(finite(o))) {
+      clear();
+      for (key = p.k0 + wave * 32; key < p.k1; key += W * 32) {
+        const int lane = fresh_lane();
+        load(key);
+        ck.template store<false>(kt, 0, lane);
+        cv.template store<true>(vt, 0, lane);
+        tile(std::true_type{}, lane);
+      }
     }
     join_waves<bf16_t, HD, NT, W, false>(a, b, (float*)smem, z, o, p.slot, wave, lane);
   } while (PLAN && walk.next(a, p));
@@ -526,7 +562,19 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   }
   s.clear();
   int tile = t0;
-  bool over[2] = {};                         // rows whose sums leave no room for their reference
+  bool over[2] = {};                         // rows whose sums leave no room for their reference, or are not finite
+  auto find_over = [&](auto&& is) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      int bad = is(over_lanes(s.z[t].l));
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) bad |= is(s.o[d][t][r]);
+      bad |= __shfl_xor(bad, 16, 64);
+      over[t] = bad | __shfl_xor(bad, 32, 64);
+    }
+  };
   bool scored = false;                       // whether the scores of `tile` are there, and its values in LDS
   if (whole > 0) {
     if constexpr (CODES) {
@@ -591,41 +639,43 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
     loaded = tile + 1 < t1;
     if (loaded) load_both(tile + 1);
     if (WIDE && wave < 4) turn();            // the halves meet again
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      int bad = !(over_lanes(s.z[t].l) <= 0x1p100f);
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) bad |= !(fabsf(s.o[d][t][r]) <= 0x1p100f);
-      bad |= __shfl_xor(bad, 16, 64);
-      over[t] = bad | __shfl_xor(bad, 32, 64);
+    find_over([&](float x) __attribute__((always_inline)) { return !(fabsf(x) <= 0x1p100f); });
+    scored = !__syncthreads_or(over[0] || over[1]);
+  }
+  // tile by tile, the next one on its way, in stages 0 and 1 in turn: what is left, or with `careful` everything once more
+  bool met = false;                          // whether a value in a tile with a border is not finite: all wavefronts go through the same tiles
+  auto tiles = [&](auto careful) __attribute__((always_inline)) {
+    for (int j = 0; tile < t1; ++j, ++tile) {
+      uint32_t values = vst + (whole % NS) * TILE;
+      if (!scored) {
+        if (!loaded) load_both(tile);
+        store_k(j & 1); store_v(j & 1);
+        loaded = tile + 1 < t1;
+        if (loaded) load_both(tile + 1);
+        __syncthreads();
+        score_tile<HD, 4, 2>(kst + (j & 1) * TILE, s.qf, s.sc, lane);
+        values = vst + (j & 1) * TILE;
+      }
+      const bool border = tile >= t0 + whole, of_row[2] = {!careful || border || over[0], !careful || border || over[1]};
+      met |= sum_tile<HD, 4, 2, careful>(a, b, values, s.sc, tile * 64, !careful || border, true, of_row, end, gaps, s.z, s.o, lane);
+      if (scored) { scored = false; __syncthreads(); }        // stages are written again
     }
-    if (__syncthreads_or(over[0] || over[1])) {
-      s.clear();
-#pragma unroll
-      for (int t = 0; t < 2; ++t) s.z[t].m = over[t] ? -INFINITY : s.ref[t];
-      tile = t0;
-      loaded = false;
-    } else {
-      scored = true;
+  };
+  bool once_more = whole > 0 && !scored;
+  if (!once_more) {
+    tiles(std::false_type{});
+    if (met) {
+      find_over([&](float x) __attribute__((always_inline)) { return !(fabsf(x) < INFINITY); });
+      once_more = __syncthreads_or(over[0] || over[1]);
     }
   }
-  // tile by tile: what is left, or everything once more; the next one on its way, in stages 0 and 1 in turn
-  for (int j = 0; tile < t1; ++j, ++tile) {
-    uint32_t values = vst + (whole % NS) * TILE;
-    if (!scored) {
-      if (!loaded) load_both(tile);
-      store_k(j & 1); store_v(j & 1);
-      loaded = tile + 1 < t1;
-      if (loaded) load_both(tile + 1);
-      __syncthreads();
-      score_tile<HD, 4, 2>(kst + (j & 1) * TILE, s.qf, s.sc, lane);
-      values = vst + (j & 1) * TILE;
-    }
-    const bool border = tile >= t0 + whole, of_row[2] = {border || over[0], border || over[1]};
-    sum_tile<HD, 4, 2>(a, b, values, s.sc, tile * 64, border, of_row, end, gaps, s.z, s.o, lane);
-    if (scored) { scored = false; __syncthreads(); }          // stages are written again
+  if (__builtin_expect(once_more, 0)) {
+    s.clear();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) s.z[t].m = over[t] || whole == 0 ? -INFINITY : s.ref[t];
+    tile = t0;
+    loaded = false;
+    tiles(std::true_type{});
   }
   const float l[2] = {over_lanes(s.z[0].l), over_lanes(s.z[1].l)};
   if (p.slot >= 0) {

@@ -42,8 +42,9 @@ template <int HD, int TK, int W, bool CODES> struct Carry {
   }
 };
 
-// One tile of KT * 16 keys: scores, what a row does not see, the online softmax, the weighted sum.
-template <int HD, int KT, int NT>
+// One tile of KT * 16 keys: scores, what a row does not see (border), the online softmax, the weighted sum (at a border and CAREFUL: with values
+// looked at; CAREFUL: and sums that are not finite kept).
+template <int HD, int KT, int NT, bool CAREFUL>
 __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const float* ktile, const float* vtile, const f32x4 (&qf)[NT][HD / 16], int key0,
                                      bool border, const int (&end)[NT], bool gaps, Soft (&z)[NT], f32x4 (&o)[HD / 16][NT], int lane) {
   constexpr int RS = HD + 4;
@@ -101,8 +102,13 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
     if (border) hide<KT>(sc[t], key0, end[t], gone, lane);
     float ref;
     const float alpha = raise(z[t], maximum<KT>(sc[t], KT) * a.scale, ref);
+    if (CAREFUL && __any(alpha == 0.f)) {
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) o[d][t] *= alpha;
+      for (int d = 0; d < HD / 16; ++d) o[d][t] = lowered(o[d][t], alpha);
+    } else {
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) o[d][t] *= alpha;
+    }
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -122,11 +128,11 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
     float x[HD / 16];
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) x[d] = v[i & 1][d];
-    if (border) {
+    if (border || CAREFUL) {
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) bad |= !(fabsf(x[d]) < INFINITY);
     }
-    if (border && __any(bad)) {
+    if ((border || CAREFUL) && __any(bad)) {
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) {
 #pragma unroll
@@ -158,6 +164,7 @@ __global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged
   constexpr int NT = 1, KG = 4 / QG, TK = QG == 1 ? 16 : 32, KT = TK / 16, RS = HD + 4, QB = QG * NT * 16, TILE = TK * RS;
   constexpr int JOIN = QG == 1 ? 4 * 16 * 2 + 4 * 16 * RS : 0, SIZE = KG * 2 * TILE;
   __shared__ __align__(16) float smem[SIZE > JOIN ? SIZE : JOIN];
+  __shared__ int again;                                      // whether a wavefront has sums that are not finite
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qt = wave % QG, kg = wave / QG;
   Walk<QB, KG * TK, false> walk(a, blockIdx.x);
   Piece p;
@@ -171,14 +178,14 @@ __global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged
   float* const vt = kt + TILE;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
   Carry<HD, TK, QG, CODES> ck, cv;
-  auto load = [&](int at) __attribute__((always_inline)) {
+  auto load = [&](int at, int lane) __attribute__((always_inline)) {
     typename decltype(ck)::Rows rows;
     rows.look(a, b, at, qt);
     ck.load(a, rows, 0, qt, lane);
     cv.load(a, rows, to_values, qt, lane);
   };
   const int first = k0 + kg * TK;
-  if (first < k1) load(first);
+  if (first < k1) load(first, lane);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = b.first + (qt * NT + t) * 16 + (lane & 15);
@@ -186,18 +193,43 @@ __global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged
 #pragma unroll
     for (int c = 0; c < HD / 16; ++c) qf[t][c] = *(const f32x4*)(q + c * 16);
     end[t] = row_end(a, b, row);
-    z[t] = Soft{-INFINITY, 0.f};
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
+  auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      z[t] = Soft{-INFINITY, 0.f};
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) o[d][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  clear();
+  if (threadIdx.x == 0) again = 0;                           // seen by all behind the look at the pages
   const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, k0, k1));
-  for (int key = first; key < k1; key += KG * TK) {
+  auto put = [&](int lane) __attribute__((always_inline)) {
     if constexpr (QG > 1) __syncthreads();
     ck.store(kt, qt, lane);
     cv.store(vt, qt, lane);
     if constexpr (QG > 1) __syncthreads();
-    if (key + KG * TK < k1) load(key + KG * TK);
-    step<HD, KT, NT>(a, b, kt, vt, qf, key, key + TK > b.whole || gaps, end, gaps, z, o, lane);
+  };
+  for (int key = first; key < k1; key += KG * TK) {
+    put(lane);
+    if (key + KG * TK < k1) load(key + KG * TK, lane);
+    step<HD, KT, NT, false>(a, b, kt, vt, qf, key, key + TK > b.whole || gaps, end, gaps, z, o, lane);
+  }
+  bool careful = !__all(finite(o));
+  if constexpr (QG > 1) {
+    if (careful) again = 1;
+    __syncthreads();
+    careful = again;
+  }
+  if (__builtin_expect(careful, 0)) {
+    clear();
+    for (int key = first; key < k1; key += KG * TK) {
+      const int lane = fresh_lane();
+      load(key, lane);
+      put(lane);
+      step<HD, KT, NT, true>(a, b, kt, vt, qf, key, key + TK > b.whole || gaps, end, gaps, z, o, lane);
+    }
   }
   if constexpr (QG > 1) {
 #pragma unroll

@@ -22,3 +22,16 @@ def test_codes_of_the_largest_values_stand_for_finite_ones():
         back, e = O.fp8_rows(x)
         assert e[0] == 120 and np.isfinite(np.float32(back[0, :2])).all() and np.isnan(back[0, 2])
         assert (np.abs(back[0, :2] - x[0, :2]) <= 2.0 ** -4 * top).all()
+
+
+def test_infinite_values_and_their_weights():
+    """exp(-2000) is 0 in 64 bits, but no weight is: the value reaches the result unless the score is -inf."""
+    k = np.zeros((3, 1, 64))
+    k[:, 0, 0] = 0.0, -2000.0, -np.inf
+    v = np.ones((3, 1, 64))
+    v[1, 0, 4], v[2, 0, 5] = np.inf, np.inf
+    q = np.zeros((1, 1, 64))
+    q[0, 0, 0] = 1.0
+    for last, want in ((2, np.inf), (3, np.inf)):
+        out, mean, _ = O.attend(q, [k[:last]], [v[:last]], [0, 1], [last], [np.ones(last, bool)], 0, 1.0, np.zeros_like(q))
+        assert out[0, 0, 4] == want and out[0, 0, 5] == 1.0 and np.isfinite(mean).all()
