@@ -52,6 +52,14 @@ extern "C" size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* c, const dp_a
   return workspace_bytes(a, c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim) : route_attn_paged_f32(a, c->head_dim), c->head_dim);
 }
 
+// for the tests, which state the kind of block that each of their calls is meant to reach: its rows, the ranges of the keys and the keys of one, the runs of a plan
+extern "C" void dp_attn_paged_route(const dp_kv_cache* c, const dp_attn_config* cfg, int64_t n_tokens, int32_t* qb_parts_keys_runs) {
+  const PagedArgs a = arguments(c, cfg, n_tokens);
+  const Route r = c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim) : route_attn_paged_f32(a, c->head_dim);
+  const int32_t v[4] = {r.qb, r.parts, r.part_keys, r.runs};
+  for (int i = 0; i < 4; ++i) qb_parts_keys_runs[i] = v[i];
+}
+
 extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, const dp_rows* q, int64_t n_tokens, const int32_t* q_start,
                              const int32_t* kv_len, const int32_t* page_table, const dp_rows* out, void* workspace, size_t have, void* stream) {
   static const char entry[] = "dp_attn_paged";
