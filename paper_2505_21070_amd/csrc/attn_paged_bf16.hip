@@ -740,12 +740,12 @@ Route route(const PagedArgs& a, int head_dim) {
       r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
     }
   } else {
-    // Measured: heads of 128, 6240 x 9360 x 40: 955 us with 256 rows, 986 with 128; 1560 x 20280 x 12: 256 rows in three ranges 206, 128 rows in one 408 (half the
-    // chip's blocks), in eight 224; sequences of 2000, 1000, 3000 x 2000, 5000, 3000 x 16, causal: 191 and 163, in two ranges 231 and 191.  Heads of 64, 8192 x
-    // 8192 x 32: 541 and 504.
-    static const Kind wide[2] = {{256, 64, 8, 1, 1, {157}, 800}, {128, 64, 8, 2, 1, {130, 163}, 600}},
-                      narrow[2] = {{256, 64, 8, 1, 1, {100}, 800}, {128, 64, 8, 2, 1, {80, 94}, 600}};
-    choose(a, head_dim == 128 ? wide : narrow, 2, head_dim, r);
+    // Measured, heads of 128, with 256 and 128 rows: 6240 x 9360 x 40 as they are 997 and 1032 us, in 8 bits 1027 and 1085; 1560 x 20280 x 12 in ranges 199 and 197; 1000,
+    // 3000 and 2000 new tokens over up to 2000 older ones, 16 heads, causal, 214 and 197.  Heads of 64 have 128 rows at every size: two such blocks on a CU take less
+    // a step than one of 256 rows (8192 x 8192 x 32: 532 us, 553).
+    static const Kind wide[2] = {{256, 64, 8, 1, 1, {157}, 800}, {128, 64, 8, 2, 1, {130, 163}, 600}}, narrow{128, 64, 8, 2, 1, {80, 94}, 600};
+    if (head_dim == 128) choose(a, wide, 2, head_dim, r);
+    else choose(a, &narrow, 1, head_dim, r);
   }
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
   return r;
@@ -774,7 +774,7 @@ template <int HD, bool CODES> void launch(const PagedArgs& a, int qb, hipStream_
   if (qb == 16) { few<HD, 1, CODES>(a, st); launch_join<bf16_t, HD, 16>(a, st); }
   else if (qb == 32) { few<HD, 2, CODES>(a, st); launch_join<bf16_t, HD, 32>(a, st); }
   else if (qb == 128) { turns<HD, false, CODES>(a, st); launch_join<bf16_t, HD, 128>(a, st); }
-  else { turns<HD, true, CODES>(a, st); launch_join<bf16_t, HD, 256>(a, st); }
+  else if constexpr (HD == 128) { turns<HD, true, CODES>(a, st); launch_join<bf16_t, HD, 256>(a, st); }
 }
 
 }  // namespace
