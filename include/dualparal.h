@@ -335,9 +335,9 @@ typedef struct {
 
 /* What the pages hold.  DP_KV_PLAIN: the rows as they are (dtype).  DP_KV_FP8: each token's head as head_dim codes of 8 bits
  * (OCP e4m3: 4 exponent and 3 fraction bits, largest value 448) times one power of two, the least 2^e with e >= -100 by which no
- * finite value of the row exceeds 448, held as the byte e + 127.  A power of two loses no bit of a floating-point code's precision, and the value
- * it stands for is exact in bfloat16 and float.  Rounding is to nearest, ties to even, but never beyond the largest of these values, 240 * 2^120; a value that
- * is not finite reads back as NaN. */
+ * finite value of the row exceeds 448, held as the byte e + 127 (27 .. 247; other bytes have no meaning).  A power of two loses no
+ * bit of a floating-point code's precision, and the value it stands for is exact in bfloat16 and float.  Rounding is to nearest,
+ * ties to even, but never beyond the largest of these values, 240 * 2^120; a value that is not finite reads back as NaN. */
 enum { DP_KV_PLAIN = 0, DP_KV_FP8 = 1 };
 typedef struct {
   int32_t kv_heads;           /* 1 .. 1024                                                         */

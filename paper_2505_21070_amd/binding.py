@@ -452,7 +452,7 @@ def _result(t, like, heads, n, d, td, device, stream):
     return t, _PACK_ROWS(t.data_ptr(), heads * d, d)
 
 
-def _norm_rope(q, hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps):
+def _norm_rope(hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps):
     assert td in _KV_DTYPE and gq.shape == gk.shape == (d,) and gq.dtype == gk.dtype == td and gq.is_contiguous() and gk.is_contiguous()
     assert gq.device == gk.device == pos.device == dev and pos.shape == (n, 3) and pos.dtype == torch.int32 and pos.is_contiguous()
     return _PACK_NORM(hq, hk, d, _KV_DTYPE[td], rope_theta, eps, gq.data_ptr(), gk.data_ptr(), pos.data_ptr())
@@ -464,7 +464,7 @@ def qk_norm_rope(q, k, gq, gk, pos, rope_theta=1e4, eps=1e-6, q_out=None, k_out=
     Returns (q_out, k_out)."""
     (n, hq, d), hk, td, dev = q.shape, k.shape[1], q.dtype, q.device
     st = _stream_on(dev, stream)
-    cfg = _norm_rope(q, hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps)
+    cfg = _norm_rope(hq, hk, n, d, td, dev, gq, gk, pos, rope_theta, eps)
     q_out, to_q = _result(q_out, q, hq, n, d, td, dev, stream)
     k_out, to_k = _result(k_out, k, hk, n, d, td, dev, stream)
     _check(_lib.dp_qk_norm_rope(cfg, _rows(q, hq, n, d, td, dev), _rows(k, hk, n, d, td, dev), n, to_q, to_k, st), "dp_qk_norm_rope")
@@ -473,7 +473,7 @@ def qk_norm_rope(q, k, gq, gk, pos, rope_theta=1e4, eps=1e-6, q_out=None, k_out=
 
 class KVCache:
     """Pages of keys and values of many sequences.  data: [n_pages, 2, kv_heads, page_tokens, head_dim], keys at [:, 0] and values at [:, 1], of
-    the rows' type, or float8_e4m3fn with scales, uint8 [n_pages, 2, kv_heads, page_tokens]: byte b stands for the factor 2^(b - 127).
+    the rows' type, or float8_e4m3fn with scales, uint8 [n_pages, 2, kv_heads, page_tokens]: byte b, 27 .. 247, stands for the factor 2^(b - 127).
     The tensors are the caller's and may be looked at; dtype ("f32", "bf16") is that of the rows, given only with 8-bit data.  Which pages a sequence owns is
     the caller's page table; a slot is page * page_tokens + place in the page.
 
@@ -518,7 +518,7 @@ class KVCache:
         """qk_norm_rope of q and k and the write of k and v, in one pass.  Returns q_out (which may be q)."""
         (n, hq, _), (d, td, dev) = q.shape, self._like
         st = _stream_on(dev, stream)
-        cfg = _norm_rope(q, hq, self.kv_heads, n, d, td, dev, gq, gk, pos, rope_theta, eps)
+        cfg = _norm_rope(hq, self.kv_heads, n, d, td, dev, gq, gk, pos, rope_theta, eps)
         assert slot.shape[0] == n
         q_out, to_q = _result(q_out, q, hq, n, d, td, dev, stream)
         _check(_lib.dp_kv_write_qkv(self._desc, cfg, _rows(q, hq, n, d, td, dev), _rows(k, self.kv_heads, n, d, td, dev),

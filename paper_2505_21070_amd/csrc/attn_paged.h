@@ -22,7 +22,7 @@ struct PagedArgs {
   float* partial;                         // of each range, or of the incomplete first [0] and last [1] tile of each run: m[QB], l[QB], O[QB][head_dim]
 };
 
-// read through the scalar cache: uniform addresses of arrays that no kernel here writes
+// read through the scalar cache: uniform addresses of arrays that this launch does not write (the plan is an earlier launch's)
 __device__ __forceinline__ int32_t uniform_i32(const int32_t* p) {
 #ifdef __HIP_DEVICE_COMPILE__
   return *(const __attribute__((address_space(4))) int32_t*)(uintptr_t)p;

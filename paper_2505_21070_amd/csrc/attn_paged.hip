@@ -22,11 +22,6 @@ const char* why_not_attn(const dp_kv_cache* c, const dp_attn_config* cfg) {
   return nullptr;
 }
 
-}  // namespace
-
-#define REFUSE_IF(expr) do { if (const char* why = (expr)) return refuse(entry, why); } while (0)
-
-namespace {
 PagedArgs arguments(const dp_kv_cache* c, const dp_attn_config* cfg, int64_t n_tokens) {
   PagedArgs a{};
   a.data = c->data; a.scales = c->scales; a.n_tokens = n_tokens;

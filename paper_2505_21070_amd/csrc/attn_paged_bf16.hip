@@ -3,8 +3,8 @@
 // Scores are computed transposed, S^T = K Q^T (v_mfma_f32_16x16x32_bf16), so that a lane's accumulators belong to one row and, turned
 // into weights and rounded to bf16, are the B operand of O^T = V^T P^T as they stand.  The rows of a block are (new token, query head)
 // pairs that share a key head: the matrix instructions' columns are filled by shared heads as by tokens, and one read of the keys serves
-// all of them.  Keys and values go from their pages through registers into LDS (codes of 8 bits become bf16 on the way, exactly) in rows as they
-// lie in the page; the operand V^T comes out of LDS by transposing reads (ds_read_b64_tr_b16), whose four consecutive keys a lane are just
+// all of them.  Keys and values go from their pages into LDS in rows as they lie in the page, through registers (codes of 8 bits become bf16 on the way,
+// exactly) or, whole tiles of blocks of many rows that are held as they are, by direct loads; the operand V^T comes out of LDS by transposing reads (ds_read_b64_tr_b16), whose four consecutive keys a lane are just
 // those of four accumulators.
 //
 // A tile of keys is either seen whole by every row of the block, or holds a border (the sequence's end, a causal border, a page that
@@ -130,8 +130,9 @@ template <int HD> __device__ __forceinline__ bf16x8 read_v(uint32_t tile, uint32
   return __builtin_shufflevector(lds_get_transposed(at), lds_get_transposed(at + 16 * HD * 2), 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Weights of KT tiles of 16 keys of a row, from scores in sc, packed for the second product; l grows by the rounded weights.  The reference is m
-// (finite, or 0 while there is none).
+// Weights of KT tiles of 16 keys of a row, from scores in sc, packed for the second product.  They are rounded to bf16 (half a step: 2^-8), the type of the values
+// that they meet, which the fast matrix instructions ask for; l grows by the rounded weights, so that what all have in common cancels (2.2e-3 from 64 bits at
+// 9360 keys, the result's own rounding included; 1.7e-3 with fp32 weights).  The reference is m (finite, or 0 while there is none).
 template <int KT> __device__ __forceinline__ void weigh(const f32x4 (&sc)[KT], float scale, float ref, float& l, uint4 (&pf)[KT / 2]) {
 #pragma unroll
   for (int s = 0; s < KT / 2; ++s) {
@@ -276,7 +277,7 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
 // Few rows: NT * 16 of them, W wavefronts that deal the block's keys out in tiles of 32 (wavefront w: tiles w, w + W, ...), each through its own piece of
 // LDS, the next tile on its way in registers; nobody waits for anybody until the results are joined in LDS, in wavefront order.  W = 4: two blocks to a
 // CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory: 64 sequences of 16 .. 16000 keys, 8 heads of 128 in 8 bits, 201 us, 5.3 TB/s.  W = 8: no more
-// blocks than CUs, bound by a trip's chain of steps, 1.6 us for 256 keys: one token over 517 keys with 12 heads 10.2 us.
+// blocks than CUs, bound by a trip's chain of steps, 1.6 us for 256 keys: one token over 517 keys with 12 heads 10.3 us.
 template <int HD, int NT, int W, bool CODES, bool PLAN>
 __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
   constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
@@ -488,8 +489,8 @@ __device__ __forceinline__ void round(State<HD>& s, float scale, const lds_char*
 // The softmax's reference is fixed to a row's maximum over the first 32 keys: weights (bf16) and fp32 sums have 8 exponent bits, so nothing is lost until
 // a sum, of weights or of weighted values, is beyond 2^100; a block with such a row, or one that is not finite, is done again tile by tile, with the reference of those rows raised as in the
 // classical online softmax (the other rows get the same bits).  So are the tiles that hold a border, for all rows.
-// What bounds it: the matrix pipes, where blocks fill the chip.  6240 x 9360 x 40 heads of 128 in 8 bits 995 us, 1.20 PFLOP/s; 1560 x 20280 x 12 as they are in
-// three ranges 187 us and 9 of joining, 1.0; heads of 64, 8192 x 8192 x 32, 519 us, 1.06.
+// What bounds it: the matrix pipes, where blocks fill the chip.  6240 x 9360 x 40 heads of 128 in 8 bits 1010 us, 1.18 PFLOP/s; 1560 x 20280 x 12 as they are in
+// three ranges 194 us, 9 of them joining, 1.0; heads of 64, 8192 x 8192 x 32, 519 us, 1.06.
 template <int HD, bool WIDE, bool CODES>
 __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const PagedArgs a) {
   constexpr int KS = HD / 32, DT = HD / 16, TILE = 64 * HD * 2;   // bytes

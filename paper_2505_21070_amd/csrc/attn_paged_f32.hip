@@ -6,7 +6,7 @@
 // LDS rows are padded by 16 bytes, so that 16 rows of 16 bytes spread over the 64 banks.  The order of O^T's rows is free as well: a lane reads its
 // channels of a value's row with 16-byte reads.
 // The matrix pipe does 1/16 of bf16's rate, so everything else hides behind it: 4096 x 4096 x 16 heads of 128 1156 us, 119 TFLOP/s, of 64 590 us, 116; one
-// token's rows are bound by memory: 64 sequences of 2000 keys, 8 heads of 128, 193 us, 5.4 TB/s.
+// token's rows are bound by memory: 64 sequences of 2000 keys, 8 heads of 128, 187 us, 5.6 TB/s.
 #include <math.h>
 
 #include "attn_paged.h"

@@ -88,7 +88,7 @@ __device__ __forceinline__ void angles(const RowArgs& a, int64_t t, int lane, in
 }
 
 // One wavefront: the rows of a run, 64 / LANES at a time, U of those trips to memory under way at once.  Measured, bf16 heads of 128, 6240 tokens: norm
-// of 40 + 40 heads 43 us (256 MB, 5.9 TB/s), 40 + 40 heads into codes 36 us (192 MB, 5.3 TB/s), 12 + 12 + 12 with norm into codes 23 us (96 MB,
+// of 40 + 40 heads 43 us (256 MB, 5.9 TB/s), 40 + 40 heads into codes 38 us (192 MB, 5.0 TB/s), 12 + 12 + 12 with norm into codes 23 us (96 MB,
 // 4.1 TB/s); one token 2.9 us.
 template <typename T, int HD, bool NORM, int TO>
 __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
@@ -293,8 +293,6 @@ const char* why_not_norm_arrays(const dp_norm_rope* c) {
 const char* why_not_slots(const int32_t* slot) { return !slot ? "null pointer" : ((uintptr_t)slot & 3) ? "slots must be 4-byte aligned" : nullptr; }
 
 }  // namespace
-
-#define REFUSE_IF(expr) do { if (const char* why = (expr)) return refuse(entry, why); } while (0)
 
 extern "C" int dp_qk_norm_rope(const dp_norm_rope* c, const dp_rows* q, const dp_rows* k, int64_t n, const dp_rows* qo, const dp_rows* ko, void* stream) {
   static const char entry[] = "dp_qk_norm_rope";

@@ -73,3 +73,4 @@ inline int refuse(const char* entry, const char* why) {
   snprintf(text, sizeof text, "%s: %s", entry, why);
   return dp_set_error(DP_EINVAL, text);
 }
+#define REFUSE_IF(expr) do { if (const char* why = (expr)) return refuse(entry, why); } while (0)
