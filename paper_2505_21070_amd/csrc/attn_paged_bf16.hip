@@ -131,7 +131,7 @@ template <int HD> __device__ __forceinline__ bf16x8 read_v(uint32_t tile, uint32
 }
 
 // Weights of KT tiles of 16 keys of a row, from scores in sc, packed for the second product.  They are rounded to bf16 (half a step: 2^-8), the type of the values
-// that they meet, which the fast matrix instructions ask for; l grows by the rounded weights, so that what all have in common cancels (2.2e-3 from 64 bits at
+// that they meet, which the fast matrix instructions ask for; l grows by the rounded weights, so that what all have in common cancels (2.1e-3 from 64 bits at
 // 9360 keys, the result's own rounding included; 1.7e-3 with fp32 weights).  The reference is m (finite, or 0 while there is none).
 template <int KT> __device__ __forceinline__ void weigh(const f32x4 (&sc)[KT], float scale, float ref, float& l, uint4 (&pf)[KT / 2]) {
 #pragma unroll
