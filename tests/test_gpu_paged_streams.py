@@ -112,3 +112,27 @@ def test_a_result_read_here_is_not_handed_out_before(n=3000):
         cache.read(torch.full_like(slot, -1), stream=side)              # zeros into whatever memory is free
     torch.cuda.synchronize()
     assert all(torch.equal(c, want) for c in copies)
+
+
+@pytest.mark.parametrize("dtype,seqs", [("bf16", 1), ("bf16", 48), ("f32", 2)])
+def test_a_named_stream_inside_a_capture(dtype, seqs):
+    """A call on a stream that a capture has branched to: its result and workspace are the graph's, and every replay gives the eager bits."""
+    cache, args = filled(6000, dtype, seqs)
+    q, other = [rows(torch.Generator().manual_seed(i), seqs, HQ, D, dtype).cuda() for i in range(2)]
+    want = cache.attend(q, *args), cache.attend(other, *args)
+    now = q.clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = cache.attend(now, *args, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        kept = out.clone()
+        del out
+    for i in (0, 1, 1, 0):
+        now.copy_((q, other)[i])
+        graph.replay()
+        between = cache.attend(other, *args)                         # eager work behind the replay
+        torch.cuda.synchronize()
+        assert torch.equal(kept, want[i]) and torch.equal(between, want[1])
