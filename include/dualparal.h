@@ -396,7 +396,8 @@ int dp_kv_read(const dp_kv_cache* cache, const int32_t* slot, int64_t n_tokens, 
  * infinities included.  A value that is not finite reaches the queries that see it, however small its key's weight, unless the score is -inf: such a key weighs
  * nothing, whatever its value.
  * max_q and max_kv size the launch: rows beyond a sequence's first max_q are left as they are, keys beyond max_kv not read.
- * Scores, softmax and sums are fp32; with DP_BF16 the weights are rounded to bf16 before they meet the values.
+ * Scores, softmax and sums are fp32, and infinite where they leave its range (a weighted sum is divided by the sum of weights at the end); with DP_BF16
+ * the weights are rounded to bf16 before they meet the values.
  *   workspace  : device, 256-byte aligned, dp_attn_paged_workspace_bytes(cache, cfg, n_tokens) bytes (0 for many calls: then it may be
  *                NULL), used by one call at a time; nothing has to be kept in it between calls.
  * Errors: DP_EINVAL (null pointer, sizes, alignment or strides outside the limits, n_tokens * q_heads above
