@@ -319,7 +319,7 @@ void dp_ends_free(dp_ends_t* ends);
 /*
  * Paged key/value cache, and the operators around it.  A stage keeps ONE block's features of ONE video next to the block being
  * processed (dp_cache_update).  These operators serve what lies beyond that: several videos on one device, histories of many
- * blocks, features held in 8 bits.  A cache is a pool of pages, `page_tokens` consecutive tokens of one sequence each; which pages
+ * blocks, features held in 8 or 4 bits.  A cache is a pool of pages, `page_tokens` consecutive tokens of one sequence each; which pages
  * a sequence owns, in which order, is the caller's table.  They share the stage's readings of RMSNorm, of the 3D rotation and of
  * softmax(q k^T) v, with norms per head instead of over the full width, and key heads that several query heads may share.
  *
@@ -337,8 +337,12 @@ typedef struct {
  * (OCP e4m3: 4 exponent and 3 fraction bits, largest value 448) times one power of two, the least 2^e with e >= -100 by which no
  * finite value of the row exceeds 448, held as the byte e + 127 (27 .. 247; other bytes have no meaning).  A power of two loses no
  * bit of a floating-point code's precision, and the value it stands for is exact in bfloat16 and float.  Rounding is to nearest,
- * ties to even, but never beyond the largest of these values, 240 * 2^120; a value that is not finite reads back as NaN. */
-enum { DP_KV_PLAIN = 0, DP_KV_FP8 = 1 };
+ * ties to even, but never beyond the largest of these values, 240 * 2^120; a value that is not finite reads back as NaN.
+ * DP_KV_FP4: codes of 4 bits, two to a byte, the first one in its low half (OCP e2m1: sign, 0 0.5 1 1.5 2 3 4 6); each group of 32 values of a token's head
+ * has one power of two, the least 2^e with -100 <= e <= 125 by which no finite value of the group exceeds 7, held as the byte e + 127 (27 .. 252).  Rounding
+ * is to nearest, ties to even, and from 5 on to 6: up to 7 by half of the codes' last step at most, as any other code.  The value that a code stands for is exact in bfloat16 and float.  A
+ * group with a value that is not finite has the byte 255 and reads back as NaN, all of it. */
+enum { DP_KV_PLAIN = 0, DP_KV_FP8 = 1, DP_KV_FP4 = 4 };
 typedef struct {
   int32_t kv_heads;           /* 1 .. 1024                                                         */
   int32_t head_dim;           /* 64 or 128                                                         */
@@ -346,8 +350,8 @@ typedef struct {
   int32_t n_pages;            /* n_pages * page_tokens <= 2^31 - 1                                 */
   int32_t dtype;              /* DP_F32 or DP_BF16: rows handed over and read back                 */
   int32_t format;             /* DP_KV_*                                                           */
-  void* data;                 /* device [n_pages, 2 (keys, values), kv_heads, page_tokens, head_dim] of dtype or of codes, 16-byte aligned */
-  uint8_t* scales;            /* device [n_pages, 2, kv_heads, page_tokens], DP_KV_FP8 only        */
+  void* data;                 /* device [n_pages, 2 (keys, values), kv_heads, page_tokens, head_dim] of dtype or of codes (DP_KV_FP4: head_dim / 2 bytes), 16-byte aligned */
+  uint8_t* scales;            /* device [n_pages, 2, kv_heads, page_tokens] with DP_KV_FP8, [.., page_tokens, head_dim / 32] with DP_KV_FP4 */
 } dp_kv_cache;
 
 /* RMSNorm of every head of q and k over its own head_dim values, times the gain, then the stage's 3D rotation of channel pairs

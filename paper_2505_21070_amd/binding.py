@@ -424,6 +424,8 @@ def euler_step(x, v, sigma, sigma_next, stream=None):
 
 
 _KV_DTYPE = {torch.float32: DP_F32, torch.bfloat16: DP_BF16}
+_KV_BITS = {torch.float8_e4m3fn: 8, torch.float4_e2m1fn_x2: 4}
+_KV_FORMAT = {0: 0, 8: 1, 4: 4}         # DP_KV_PLAIN, DP_KV_FP8, DP_KV_FP4
 
 
 def _rows(t, heads, n, d, td, device):
@@ -478,8 +480,9 @@ def qk_norm_rope(q, k, gq, gk, pos, rope_theta=1e4, eps=1e-6, q_out=None, k_out=
 
 class KVCache:
     """Pages of keys and values of many sequences.  data: [n_pages, 2, kv_heads, page_tokens, head_dim], keys at [:, 0] and values at [:, 1], of
-    the rows' type, or float8_e4m3fn with scales, uint8 [n_pages, 2, kv_heads, page_tokens]: byte b, 27 .. 247, stands for the factor 2^(b - 127).
-    The tensors are the caller's and may be looked at; dtype ("f32", "bf16") is that of the rows, given only with 8-bit data.  Which pages a sequence owns is
+    the rows' type, or float8_e4m3fn with scales, uint8 [n_pages, 2, kv_heads, page_tokens]: byte b, 27 .. 247, stands for the factor 2^(b - 127); or
+    float4_e2m1fn_x2, [.., page_tokens, head_dim / 2] bytes of two codes each, with scales [.., page_tokens, head_dim / 32], a byte (27 .. 252, 255: NaN) for 32 values.
+    The tensors are the caller's and may be looked at; dtype ("f32", "bf16") is that of the rows, given only with data of 8 or 4 bits.  Which pages a sequence owns is
     the caller's page table; a slot is page * page_tokens + place in the page.
 
     Calls on a named stream wait for nobody: what they read has to be there, and is the caller's to keep until they have run.  Their results are to be read
@@ -487,23 +490,30 @@ class KVCache:
 
     def __init__(self, data, scales=None, dtype=None):
         td = {"f32": torch.float32, "bf16": torch.bfloat16, None: data.dtype}[dtype]
-        fp8 = data.dtype == torch.float8_e4m3fn
-        assert td in _KV_DTYPE and (fp8 or td == data.dtype), (td, data.dtype)
+        bits = _KV_BITS.get(data.dtype, 0)                   # of a code, 0: rows as they are
+        assert td in _KV_DTYPE and (bits or td == data.dtype), (td, data.dtype)
         assert data.is_cuda and data.dim() == 5 and data.shape[1] == 2 and data.is_contiguous(), tuple(data.shape)
-        assert (scales is not None) == fp8, "scales go with 8-bit data"
-        if fp8:
-            assert scales.dtype == torch.uint8 and scales.shape == data.shape[:4] and scales.is_contiguous() and scales.device == data.device
-        self.data, self.scales, self.torch_dtype = data, scales, td
+        assert (scales is not None) == (bits > 0), "scales go with data of 8 or 4 bits"
         self.n_pages, _, self.kv_heads, self.page_tokens, self.head_dim = data.shape
+        if bits:
+            if bits == 4:
+                self.head_dim *= 2
+            shape = data.shape[:4] + (self.head_dim // 32,) if bits == 4 else data.shape[:4]
+            assert scales.dtype == torch.uint8 and scales.shape == shape and scales.is_contiguous() and scales.device == data.device
+        self.data, self.scales, self.torch_dtype = data, scales, td
         self._like = (self.head_dim, td, data.device)
-        self._desc = bytes(KvCacheDesc(self.kv_heads, self.head_dim, self.page_tokens, self.n_pages, _KV_DTYPE[td], int(fp8), data.data_ptr(),
-                                       scales.data_ptr() if fp8 else None))
+        self._desc = bytes(KvCacheDesc(self.kv_heads, self.head_dim, self.page_tokens, self.n_pages, _KV_DTYPE[td], _KV_FORMAT[bits], data.data_ptr(),
+                                       scales.data_ptr() if bits else None))
 
     @classmethod
-    def empty(cls, n_pages, kv_heads, page_tokens, head_dim, dtype="bf16", fp8=False, device=None):
+    def empty(cls, n_pages, kv_heads, page_tokens, head_dim, dtype="bf16", fp8=False, device=None, fp4=False):
         """A cache of new, zeroed pages."""
+        assert not (fp8 and fp4), "codes of 8 bits or of 4"
         device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         shape = (n_pages, 2, kv_heads, page_tokens)
+        if fp4:
+            return cls(torch.zeros(shape + (head_dim // 2,), dtype=torch.uint8, device=device).view(torch.float4_e2m1fn_x2),
+                       torch.full(shape + (head_dim // 32,), 127, dtype=torch.uint8, device=device), dtype)
         if fp8:
             return cls(torch.zeros(shape + (head_dim,), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn),
                        torch.full(shape, 127, dtype=torch.uint8, device=device), dtype)
@@ -534,7 +544,7 @@ class KVCache:
         """The keys and values at the slots, [n, kv_heads, head_dim] each, zeros where a slot is outside the pool."""
         n, (d, td, dev), hk = slot.shape[0], self._like, self.kv_heads
         st = _stream_on(dev, stream)
-        new, shape = self.data.new_empty, (n, hk, d)
+        new, shape = slot.new_empty, (n, hk, d)
         k, v = (new(shape, dtype=td), new(shape, dtype=td)) if stream is None else [_memory(lambda: new(shape, dtype=td), stream) for _ in range(2)]
         _check(_lib.dp_kv_read(self._desc, self._slots(slot), n, _PACK_ROWS(k.data_ptr(), hk * d, d), _PACK_ROWS(v.data_ptr(), hk * d, d), st), "dp_kv_read")
         return k, v

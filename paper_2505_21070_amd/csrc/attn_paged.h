@@ -517,5 +517,5 @@ inline size_t workspace_bytes(const PagedArgs& a, const Route& r, int head_dim) 
 }
 Route route_attn_paged_bf16(const PagedArgs& a, int head_dim);
 Route route_attn_paged_f32(const PagedArgs& a, int head_dim);
-void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st);
-void launch_attn_paged_f32(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st);
+void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, int format, hipStream_t st);
+void launch_attn_paged_f32(const PagedArgs& a, const Route& r, int head_dim, int format, hipStream_t st);

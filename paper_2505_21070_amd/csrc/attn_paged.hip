@@ -79,7 +79,7 @@ extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, co
     if (r.runs) a.plan = (int32_t*)((char*)workspace + partial_bytes(a, r, c->head_dim));
   }
   (void)hipGetLastError();
-  (c->dtype == DP_BF16 ? launch_attn_paged_bf16 : launch_attn_paged_f32)(a, r, c->head_dim, c->format == DP_KV_FP8, st);
+  (c->dtype == DP_BF16 ? launch_attn_paged_bf16 : launch_attn_paged_f32)(a, r, c->head_dim, c->format, st);
   if (hipGetLastError() != hipSuccess) return dp_set_error(DP_EHIP, "dp_attn_paged: the launch failed");
   return DP_OK;
 }

@@ -3,7 +3,7 @@
 // Scores are computed transposed, S^T = K Q^T (v_mfma_f32_16x16x32_bf16), so that a lane's accumulators belong to one row and, turned
 // into weights and rounded to bf16, are the B operand of O^T = V^T P^T as they stand.  The rows of a block are (new token, query head)
 // pairs that share a key head: the matrix instructions' columns are filled by shared heads as by tokens, and one read of the keys serves
-// all of them.  Keys and values go from their pages into LDS in rows as they lie in the page, through registers (codes of 8 bits become bf16 on the way,
+// all of them.  Keys and values go from their pages into LDS in rows as they lie in the page, through registers (codes of 8 or 4 bits become bf16 on the way,
 // exactly) or, whole tiles of blocks of many rows that are held as they are, by direct loads; the operand V^T comes out of LDS by transposing reads (ds_read_b64_tr_b16), whose four consecutive keys a lane are just
 // those of four accumulators.
 //
@@ -70,9 +70,12 @@ template <int HD> __device__ __forceinline__ int k_swizzle(int row) { return HD 
 template <int HD> __device__ __forceinline__ int v_swizzle(int row) { return HD == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
 
 // A tile of TK keys and values on its way from the pages into LDS, in the registers of W wavefronts, of which this is number w.
-template <int HD, int TK, int W, bool CODES> struct Carry {
-  static constexpr int ROW = CODES ? HD : HD * 2;                            // bytes of a row in the pages
-  static constexpr int LB = TK * ROW / (W * 64) < 16 ? TK * ROW / (W * 64) : 16;   // bytes a lane takes at once
+template <int HD, int TK, int W, int FORMAT> struct Carry {
+  static constexpr bool CODES = FORMAT != DP_KV_PLAIN;
+  static constexpr int ROW = FORMAT == DP_KV_FP4 ? HD / 2 : CODES ? HD : HD * 2;   // bytes of a row in the pages
+  static constexpr int MOST = ROW / 4 < 16 ? ROW / 4 : 16;                   // a trip has 16 rows at most
+  static constexpr int LB = TK * ROW / (W * 64) < MOST ? TK * ROW / (W * 64) : MOST;   // bytes a lane takes at once
+  static constexpr int WIDER = FORMAT == DP_KV_FP4 ? 4 : CODES ? 2 : 1;      // bytes in LDS for one in the pages
   static constexpr int N = TK * ROW / (W * 64 * LB), RW = 64 * LB / ROW;     // trips, rows of a trip of one wavefront
   static_assert(N * W * RW == TK && RW <= 16 && (LB == 16 || LB == 8), "a trip's rows lie in one page");
   typedef typename std::conditional<LB == 16, u32x4, u32x2>::type Raw;
@@ -91,18 +94,23 @@ template <int HD, int TK, int W, bool CODES> struct Carry {
     for (int i = 0; i < N; ++i) {
       const int64_t row = rows.row(i, w) + to_values;
       raw[i] = *(const Raw*)((const char*)a.data + row * ROW + lane * LB);
-      if constexpr (CODES) byte[i] = (a.scales + row)[lane / (ROW / LB)];
+      if constexpr (FORMAT == DP_KV_FP4) byte[i] = (a.scales + row * (HD / FP4_GROUP))[lane * LB / (FP4_GROUP / 2)];
+      else if constexpr (CODES) byte[i] = (a.scales + row)[lane / (ROW / LB)];
     }
   }
   template <bool VALUES> __device__ __forceinline__ void store(uint32_t tile, int w, int lane) const {
     // rows of a trip differ from the first trip's in higher bits, and the exchange takes each bit by itself: few addresses, the rest in the instructions' offsets
     const int row = w * RW + lane / (ROW / LB);
-    const uint32_t in_row = lane % (ROW / LB) * LB * (CODES ? 2 : 1) ^ (VALUES ? v_swizzle<HD>(row) : k_swizzle<HD>(row)) * 16, at = tile + row * HD * 2;
+    const uint32_t in_row = lane % (ROW / LB) * LB * WIDER ^ (VALUES ? v_swizzle<HD>(row) : k_swizzle<HD>(row)) * 16, at = tile + row * HD * 2;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint32_t x = (VALUES ? v_swizzle<HD>(i * W * RW) : k_swizzle<HD>(i * W * RW)) * 16, off = i * W * RW * HD * 2;
       if constexpr (!CODES) {
         lds_put(lds_base((in_row ^ x) + at) + off, raw[i]);
+      } else if constexpr (FORMAT == DP_KV_FP4) {
+        const float f = __uint_as_float(byte[i] << 23);
+#pragma unroll
+        for (int h = 0; h < LB / 4; ++h) lds_put(lds_base((in_row ^ x ^ h * 16) + at) + off, __builtin_bit_cast(u32x4, fp4x8_to_bf16(raw[i][h], f)));
       } else {
         const float f = __uint_as_float(byte[i] << 23);
 #pragma unroll
@@ -278,7 +286,7 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
 // LDS, the next tile on its way in registers; nobody waits for anybody until the results are joined in LDS, in wavefront order.  W = 4: two blocks to a
 // CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory: 64 sequences of 16 .. 16000 keys, 8 heads of 128 in 8 bits, 201 us, 5.3 TB/s.  W = 8: no more
 // blocks than CUs, bound by a trip's chain of steps, 1.6 us for 256 keys: one token over 517 keys with 12 heads 10.3 us.
-template <int HD, int NT, int W, bool CODES, bool PLAN>
+template <int HD, int NT, int W, int FORMAT, bool PLAN>
 __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
   constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
   __shared__ uint4 smem[W * 2 * TILE];
@@ -307,7 +315,7 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
       }
     };
     clear();
-    Carry<HD, 32, 1, CODES> ck, cv;
+    Carry<HD, 32, 1, FORMAT> ck, cv;
     int key = p.k0 + wave * 32;
     auto load = [&](int at) __attribute__((always_inline)) {
       const auto rows = ck.rows(a, b, at, 0);
@@ -491,8 +499,9 @@ __device__ __forceinline__ void round(State<HD>& s, float scale, const lds_char*
 // classical online softmax (the other rows get the same bits).  So are the tiles that hold a border, for all rows.
 // What bounds it: the matrix pipes, where blocks fill the chip.  6240 x 9360 x 40 heads of 128 in 8 bits 1010 us, 1.18 PFLOP/s; 1560 x 20280 x 12 as they are in
 // three ranges 194 us, 9 of them joining, 1.0; heads of 64, 8192 x 8192 x 32, 519 us, 1.06.
-template <int HD, bool WIDE, bool CODES>
+template <int HD, bool WIDE, int FORMAT>
 __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const PagedArgs a) {
+  constexpr bool CODES = FORMAT != DP_KV_PLAIN;
   constexpr int KS = HD / 32, DT = HD / 16, TILE = 64 * HD * 2;   // bytes
   constexpr int W = WIDE ? 8 : 4, QB = W * 32, NS = WIDE ? (CODES ? 3 : 4) : 2;   // wavefronts, rows of a block, LDS stages of keys and of values
   extern __shared__ uint4 smem[];            // NS key tiles, NS value tiles
@@ -514,7 +523,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   lds_char* const kst_ = (lds_char*)(lds_void_t*)smem;
   lds_char* const vst_ = kst_ + NS * TILE;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
-  typedef Carry<HD, 64, W, CODES> Registers;
+  typedef Carry<HD, 64, W, FORMAT> Registers;
   Registers ck, cv;
   typedef Direct<HD, W> Loads;
   const Loads direct(wave, lane);
@@ -752,36 +761,40 @@ Route route(const PagedArgs& a, int head_dim) {
   return r;
 }
 
-template <int HD, int NT, bool CODES> void few(const PagedArgs& a, hipStream_t st) {
+template <int HD, int NT, int FORMAT> void few(const PagedArgs& a, hipStream_t st) {
   constexpr int QB = NT * 16;
   const int64_t blocks = (int64_t)a.tiles * a.hk * a.parts;
   if (a.plan) {
     k_paged_plan<QB, 128><<<1, 1024, 0, st>>>(a);
-    k_paged_few<HD, NT, 4, CODES, true><<<(unsigned)a.runs, 256, 0, st>>>(a);
+    k_paged_few<HD, NT, 4, FORMAT, true><<<(unsigned)a.runs, 256, 0, st>>>(a);
   } else if (blocks <= 256 && a.max_kv > 128) {
-    k_paged_few<HD, NT, 8, CODES, false><<<(unsigned)blocks, 512, 0, st>>>(a);
+    k_paged_few<HD, NT, 8, FORMAT, false><<<(unsigned)blocks, 512, 0, st>>>(a);
   } else {
-    k_paged_few<HD, NT, 4, CODES, false><<<(unsigned)blocks, 256, 0, st>>>(a);
+    k_paged_few<HD, NT, 4, FORMAT, false><<<(unsigned)blocks, 256, 0, st>>>(a);
   }
 }
-template <int HD, bool WIDE, bool CODES> void turns(const PagedArgs& a, hipStream_t st) {
-  constexpr int lds = (WIDE ? (CODES ? 3 : 4) : 2) * 2 * 64 * HD * 2;
+template <int HD, bool WIDE, int FORMAT> void turns(const PagedArgs& a, hipStream_t st) {
+  constexpr int lds = (WIDE ? (FORMAT != DP_KV_PLAIN ? 3 : 4) : 2) * 2 * 64 * HD * 2;
   static std::atomic<uint64_t> done;
-  allow_dynamic_lds((const void*)k_paged_turns<HD, WIDE, CODES>, lds, done);
+  allow_dynamic_lds((const void*)k_paged_turns<HD, WIDE, FORMAT>, lds, done);
   const int64_t total = (int64_t)a.tiles * a.hk * a.parts;
-  k_paged_turns<HD, WIDE, CODES><<<(unsigned)((total + 7) / 8 * 8), WIDE ? 512 : 256, lds, st>>>(a);
+  k_paged_turns<HD, WIDE, FORMAT><<<(unsigned)((total + 7) / 8 * 8), WIDE ? 512 : 256, lds, st>>>(a);
 }
-template <int HD, bool CODES> void launch(const PagedArgs& a, int qb, hipStream_t st) {
-  if (qb == 16) { few<HD, 1, CODES>(a, st); launch_join<bf16_t, HD, 16>(a, st); }
-  else if (qb == 32) { few<HD, 2, CODES>(a, st); launch_join<bf16_t, HD, 32>(a, st); }
-  else if (qb == 128) { turns<HD, false, CODES>(a, st); launch_join<bf16_t, HD, 128>(a, st); }
-  else if constexpr (HD == 128) { turns<HD, true, CODES>(a, st); launch_join<bf16_t, HD, 256>(a, st); }
+template <int HD, int FORMAT> void launch(const PagedArgs& a, int qb, hipStream_t st) {
+  if (qb == 16) { few<HD, 1, FORMAT>(a, st); launch_join<bf16_t, HD, 16>(a, st); }
+  else if (qb == 32) { few<HD, 2, FORMAT>(a, st); launch_join<bf16_t, HD, 32>(a, st); }
+  else if (qb == 128) { turns<HD, false, FORMAT>(a, st); launch_join<bf16_t, HD, 128>(a, st); }
+  else if constexpr (HD == 128) { turns<HD, true, FORMAT>(a, st); launch_join<bf16_t, HD, 256>(a, st); }
 }
 
 }  // namespace
 
 Route route_attn_paged_bf16(const PagedArgs& a, int head_dim) { return route(a, head_dim); }
-void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st) {
-  if (head_dim == 128) { if (codes) launch<128, true>(a, r.qb, st); else launch<128, false>(a, r.qb, st); }
-  else { if (codes) launch<64, true>(a, r.qb, st); else launch<64, false>(a, r.qb, st); }
+void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, int format, hipStream_t st) {
+  auto of = [&](auto f) {
+    if (head_dim == 128) launch<128, decltype(f)::value>(a, r.qb, st); else launch<64, decltype(f)::value>(a, r.qb, st);
+  };
+  if (format == DP_KV_FP4) of(std::integral_constant<int, DP_KV_FP4>{});
+  else if (format == DP_KV_FP8) of(std::integral_constant<int, DP_KV_FP8>{});
+  else of(std::integral_constant<int, DP_KV_PLAIN>{});
 }

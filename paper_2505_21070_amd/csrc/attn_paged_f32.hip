@@ -17,10 +17,12 @@ __device__ __forceinline__ f32x4 mfma(float a, float b, f32x4 c) { return __buil
 
 // A tile of TK keys and values on its way from the pages into LDS, in the registers of W wavefronts, of which this is number w: four
 // channels a lane and trip.
-template <int HD, int TK, int W, bool CODES> struct Carry {
+template <int HD, int TK, int W, int FORMAT> struct Carry {
+  static constexpr bool CODES = FORMAT != DP_KV_PLAIN;
+  static constexpr int ROW = FORMAT == DP_KV_FP4 ? HD / 2 : FORMAT == DP_KV_FP8 ? HD : HD * 4;   // bytes of a row in the pages
   static constexpr int LANES = HD / 4, RW = 64 / LANES, N = TK / (W * RW);   // lanes of a row, rows of a trip of one wavefront, trips
   static_assert(N * W * RW == TK && RW <= 16, "a trip's rows lie in one page");
-  typedef typename std::conditional<CODES, uint32_t, f32x4>::type Raw;
+  typedef typename std::conditional<FORMAT == DP_KV_FP4, uint16_t, typename std::conditional<CODES, uint32_t, f32x4>::type>::type Raw;
   Raw raw[N];
   uint32_t byte[CODES ? N : 1];
   typedef TileRows<N, W, RW> Rows;
@@ -28,15 +30,17 @@ template <int HD, int TK, int W, bool CODES> struct Carry {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int64_t row = rows.row(i, w) + to_values;
-      raw[i] = *(const Raw*)((const char*)a.data + row * (HD * (CODES ? 1 : 4)) + lane * sizeof(Raw));
-      if constexpr (CODES) byte[i] = (a.scales + row)[lane / LANES];
+      raw[i] = *(const Raw*)((const char*)a.data + row * ROW + lane * sizeof(Raw));
+      if constexpr (FORMAT == DP_KV_FP4) byte[i] = (a.scales + row * (HD / FP4_GROUP))[lane / (FP4_GROUP / 4)];
+      else if constexpr (CODES) byte[i] = (a.scales + row)[lane / LANES];
     }
   }
   __device__ __forceinline__ void store(float* tile, int w, int lane) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float* const at = tile + ((i * W + w) * RW + lane / LANES) * (HD + 4) + lane % LANES * 4;
-      if constexpr (CODES) *(float4*)at = fp8x4_to_f32(raw[i], __uint_as_float(byte[i] << 23));
+      if constexpr (FORMAT == DP_KV_FP4) *(float4*)at = fp4x4_to_f32(raw[i], __uint_as_float(byte[i] << 23));
+      else if constexpr (CODES) *(float4*)at = fp8x4_to_f32(raw[i], __uint_as_float(byte[i] << 23));
       else *(f32x4*)at = raw[i];
     }
   }
@@ -159,7 +163,7 @@ __device__ __forceinline__ void step(const PagedArgs& a, const Block& b, const f
 // Four wavefronts.  QG = 4: each has 16 rows of its own, and they share tiles of 32 keys.  QG = 1: all have the same 16 rows and deal the keys
 // out in tiles of 16 (wavefront w: tiles w, w + 4, ...), and meet in LDS at the end.  Either way the next tile is on its way in registers.  Registers are bounded for
 // three blocks on a CU (heads of 64: four): 4096 x 4096 x 16 heads 1242 -> 1148 us.
-template <int HD, int QG, bool CODES>
+template <int HD, int QG, int FORMAT>
 __global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged_f32(const PagedArgs a) {
   constexpr int NT = 1, KG = 4 / QG, TK = QG == 1 ? 16 : 32, KT = TK / 16, RS = HD + 4, QB = QG * NT * 16, TILE = TK * RS;
   constexpr int JOIN = QG == 1 ? 4 * 16 * 2 + 4 * 16 * RS : 0, SIZE = KG * 2 * TILE;
@@ -177,7 +181,7 @@ __global__ __launch_bounds__(256, QG == 4 ? (HD == 64 ? 4 : 3) : 2) void k_paged
   float* const kt = smem + kg * 2 * TILE;
   float* const vt = kt + TILE;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
-  Carry<HD, TK, QG, CODES> ck, cv;
+  Carry<HD, TK, QG, FORMAT> ck, cv;
   auto load = [&](int at, int lane) __attribute__((always_inline)) {
     typename decltype(ck)::Rows rows;
     rows.look(a, b, at, qt);
@@ -274,20 +278,22 @@ Route route(const PagedArgs& a, int head_dim) {
   r.tiles_of_seq = (rows + r.qb - 1) / r.qb;
   return r;
 }
-template <int HD, int QG> void launch(const PagedArgs& a, bool codes, hipStream_t st) {
+template <int HD, int QG> void launch(const PagedArgs& a, int format, hipStream_t st) {
   constexpr int QB = QG * 16;
   const int64_t blocks = (int64_t)a.tiles * a.hk;
   const unsigned g = (unsigned)(blocks * a.parts);
-  if (codes) k_paged_f32<HD, QG, true><<<g, 256, 0, st>>>(a); else k_paged_f32<HD, QG, false><<<g, 256, 0, st>>>(a);
+  if (format == DP_KV_FP4) k_paged_f32<HD, QG, DP_KV_FP4><<<g, 256, 0, st>>>(a);
+  else if (format == DP_KV_FP8) k_paged_f32<HD, QG, DP_KV_FP8><<<g, 256, 0, st>>>(a);
+  else k_paged_f32<HD, QG, DP_KV_PLAIN><<<g, 256, 0, st>>>(a);
   launch_join<float, HD, QB>(a, st);
 }
-template <int HD> void launch(const PagedArgs& a, int qb, bool codes, hipStream_t st) {
-  if (qb == 16) launch<HD, 1>(a, codes, st); else launch<HD, 4>(a, codes, st);
+template <int HD> void launch(const PagedArgs& a, int qb, int format, hipStream_t st) {
+  if (qb == 16) launch<HD, 1>(a, format, st); else launch<HD, 4>(a, format, st);
 }
 
 }  // namespace
 
 Route route_attn_paged_f32(const PagedArgs& a, int head_dim) { return route(a, head_dim); }
-void launch_attn_paged_f32(const PagedArgs& a, const Route& r, int head_dim, bool codes, hipStream_t st) {
-  if (head_dim == 128) launch<128>(a, r.qb, codes, st); else launch<64>(a, r.qb, codes, st);
+void launch_attn_paged_f32(const PagedArgs& a, const Route& r, int head_dim, int format, hipStream_t st) {
+  if (head_dim == 128) launch<128>(a, r.qb, format, st); else launch<64>(a, r.qb, format, st);
 }

@@ -1,8 +1,8 @@
 // Rows of heads on their way into the pages of a key/value cache and out of them: RMSNorm of each head with the 3D rotation
-// (dp_qk_norm_rope), the write with or without codes of 8 bits (dp_kv_write), the two in one pass (dp_kv_write_qkv), the read
+// (dp_qk_norm_rope), the write with or without codes of 8 or 4 bits (dp_kv_write), the two in one pass (dp_kv_write_qkv), the read
 // (dp_kv_read).
 //
-// All are bound by memory: a value is read once and written once, 4 bytes a value in bf16, 3 into codes.  A head's row is 8 to 32 lanes of 16
+// All are bound by memory: a value is read once and written once, 4 bytes a value in bf16, 3 into codes of 8 bits, 2.5 of 4.  A head's row is 8 to 32 lanes of 16
 // bytes, so its sum of squares and its largest value stay within the lanes that hold it, and a channel pair (2i, 2i+1) within one lane.  A wavefront
 // takes a run of one token's heads, all queries, all keys or all values: the token's angles are the same for all of them and are computed once, a
 // pair a lane, in 64 bits up to the turn's fraction.
@@ -32,16 +32,16 @@ struct RowArgs {
   double power[2][6];
 };
 // where the output of keys and values goes
-enum { TO_ROWS = 0, TO_PAGES = 1, TO_CODES = 2 };
+enum { TO_ROWS = 0, TO_PAGES = 1, TO_CODES = 2, TO_FP4 = 3 };
 
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
   return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
 }
-// op over the LANES (8, 16 or 32) lanes of a row, the same in all of them
+// op over the LANES (8, 16 or 32) lanes of a row, or the 4 or 8 of a group of 32 values, the same in all of them
 template <int LANES, typename Op> __device__ __forceinline__ float over_row(float v, Op op) {
   v = op(v, dpp<0xB1>(v));                // quad_perm: lane ^ 1
   v = op(v, dpp<0x4E>(v));                // quad_perm: lane ^ 2
-  v = op(v, dpp<0x141>(v));               // row_half_mirror: the other quad of 8
+  if constexpr (LANES >= 8) v = op(v, dpp<0x141>(v));    // row_half_mirror: the other quad of 8
   if constexpr (LANES >= 16) v = op(v, dpp<0x140>(v));   // row_mirror: the other half of 16
   if constexpr (LANES >= 32) v = op(v, __shfl_xor(v, 16, 64));
   return v;
@@ -161,6 +161,18 @@ __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
         const int64_t row = row0 + ((int64_t)r << a.page_shift);
         if constexpr (TO == TO_PAGES) {
           if (r < last) *(uint4*)((T*)a.data + row * HD + c0) = Vec<T>::pack(x);
+        } else if constexpr (TO == TO_FP4) {
+          float top = 0.f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) top = fmaxf(top, fp4_size(x[i]));
+          const uint32_t byte = fp4_byte(over_row<FP4_GROUP / N>(top, [](float m, float n) { return fmaxf(m, n); }));
+          const float inv = fp4_inverse(byte);
+          if (r < last) {
+            uint8_t* const to = (uint8_t*)a.data + row * (HD / 2) + c0 / 2;
+            if constexpr (N == 8) *(uint32_t*)to = to_fp4x4(x[0], x[1], x[2], x[3], inv) | to_fp4x4(x[4], x[5], x[6], x[7], inv) << 16;
+            else *(uint16_t*)to = (uint16_t)to_fp4x4(x[0], x[1], x[2], x[3], inv);
+            if (c0 % FP4_GROUP == 0) a.scales[row * (HD / FP4_GROUP) + c0 / FP4_GROUP] = (uint8_t)byte;
+          }
         } else {
           float top = 0.f;
 #pragma unroll
@@ -180,7 +192,7 @@ __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
 }
 
 // The way back: one row a lane group, keys and values of a token's heads.  40 + 40 heads of 6240 tokens out of codes 30 us (192 MB, 6.4 TB/s).
-template <typename T, int HD, bool CODES>
+template <typename T, int HD, int FORMAT>
 __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
   constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = 4;
   const int lane = threadIdx.x & 63, c0 = lane % LANES * N;
@@ -198,16 +210,21 @@ __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
   const int64_t hs = is_v ? a.qo_hs : a.ko_hs;                // the values take the place of the queries
   T* const dst = (is_v ? (T*)a.qo + t * a.qo_ts : (T*)a.ko + t * a.ko_ts) + c0;
   for (int r0 = first; r0 < last; r0 += U * ROWS) {
-    typename std::conditional<CODES, typename std::conditional<N == 8, uint2, uint32_t>::type, uint4>::type raw[U];
+    typedef typename std::conditional<N == 8, uint2, uint32_t>::type Fp8;
+    typedef typename std::conditional<N == 8, uint32_t, uint16_t>::type Fp4;
+    typename std::conditional<FORMAT == DP_KV_FP8, Fp8, typename std::conditional<FORMAT == DP_KV_FP4, Fp4, uint4>::type>::type raw[U];
     uint32_t byte[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       int r = r0 + u * ROWS + lane / LANES;
       if (r >= last) r = last - 1;
       const int64_t row = row0 + ((int64_t)r << a.page_shift);
-      if constexpr (CODES) {
-        raw[u] = *(const decltype(&raw[u]))((const uint8_t*)a.data + row * HD + c0);
+      if constexpr (FORMAT == DP_KV_FP8) {
+        raw[u] = *(const Fp8*)((const uint8_t*)a.data + row * HD + c0);
         byte[u] = a.scales[row];
+      } else if constexpr (FORMAT == DP_KV_FP4) {
+        raw[u] = *(const Fp4*)((const uint8_t*)a.data + row * (HD / 2) + c0 / 2);
+        byte[u] = a.scales[row * (HD / FP4_GROUP) + c0 / FP4_GROUP];
       } else {
         raw[u] = *(const uint4*)((const T*)a.data + row * HD + c0);
       }
@@ -217,7 +234,9 @@ __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
       const int r = r0 + u * ROWS + lane / LANES;
       if (r >= last) continue;
       uint4 out;
-      if constexpr (!CODES) out = raw[u];
+      if constexpr (FORMAT == DP_KV_PLAIN) out = raw[u];
+      else if constexpr (FORMAT == DP_KV_FP4 && N == 8) out = fp4x8_to_bf16(raw[u], __uint_as_float(byte[u] << 23));
+      else if constexpr (FORMAT == DP_KV_FP4) { const float4 f = fp4x4_to_f32(raw[u], __uint_as_float(byte[u] << 23)); out = __builtin_bit_cast(uint4, f); }
       else if constexpr (N == 8) out = fp8x8_to_bf16(raw[u], __uint_as_float(byte[u] << 23));
       else { const float4 f = fp8x4_to_f32(raw[u], __uint_as_float(byte[u] << 23)); out = __builtin_bit_cast(uint4, f); }
       if (!kept) out = uint4{};
@@ -258,11 +277,13 @@ void set_cache(RowArgs& a, const dp_kv_cache* c) {
   a.n_slots = (int32_t)((int64_t)c->n_pages * c->page_tokens);
   a.hk = c->kv_heads;
 }
+int to_of(const dp_kv_cache* c) { return c->format == DP_KV_FP4 ? TO_FP4 : c->format == DP_KV_FP8 ? TO_CODES : TO_PAGES; }
 #define SET_ROWS(field, rows) do { a.field = (rows)->data; a.field##_ts = (rows)->token_stride; a.field##_hs = (rows)->head_stride; } while (0)
 
 template <typename T, int HD, bool NORM> void launch_to(const RowArgs& a, int to, hipStream_t st) {
   const unsigned g = blocks_of(a);
-  if (to == TO_CODES) k_head_rows<T, HD, NORM, TO_CODES><<<g, 256, 0, st>>>(a);
+  if (to == TO_FP4) k_head_rows<T, HD, NORM, TO_FP4><<<g, 256, 0, st>>>(a);
+  else if (to == TO_CODES) k_head_rows<T, HD, NORM, TO_CODES><<<g, 256, 0, st>>>(a);
   else if (to == TO_PAGES) k_head_rows<T, HD, NORM, TO_PAGES><<<g, 256, 0, st>>>(a);
   else if constexpr (NORM) k_head_rows<T, HD, NORM, TO_ROWS><<<g, 256, 0, st>>>(a);
 }
@@ -324,7 +345,7 @@ extern "C" int dp_kv_write(const dp_kv_cache* c, const dp_rows* k, const dp_rows
   SET_ROWS(k, k); SET_ROWS(v, v);
   set_cache(a, c);
   a.slot = slot; a.n_tokens = n;
-  return launch_rows<false>(a, c->head_dim, c->dtype, c->format == DP_KV_FP8 ? TO_CODES : TO_PAGES, true, stream, entry);
+  return launch_rows<false>(a, c->head_dim, c->dtype, to_of(c), true, stream, entry);
 }
 
 extern "C" int dp_kv_write_qkv(const dp_kv_cache* c, const dp_norm_rope* m, const dp_rows* q, const dp_rows* k, const dp_rows* v, const int32_t* slot,
@@ -347,7 +368,7 @@ extern "C" int dp_kv_write_qkv(const dp_kv_cache* c, const dp_norm_rope* m, cons
   a.pos = m->pos; a.gq = m->gq; a.gk = m->gk; a.eps = m->eps; a.slot = slot; a.n_tokens = n;
   a.hq = m->q_heads;
   set_powers(a, c->head_dim, m->rope_theta);
-  return launch_rows<true>(a, c->head_dim, c->dtype, c->format == DP_KV_FP8 ? TO_CODES : TO_PAGES, true, stream, entry);
+  return launch_rows<true>(a, c->head_dim, c->dtype, to_of(c), true, stream, entry);
 }
 
 extern "C" int dp_kv_read(const dp_kv_cache* c, const int32_t* slot, int64_t n, const dp_rows* ko, const dp_rows* vo, void* stream) {
@@ -366,9 +387,9 @@ extern "C" int dp_kv_read(const dp_kv_cache* c, const int32_t* slot, int64_t n, 
   const hipStream_t st = (hipStream_t)stream;
   cut(a, 64 / (c->head_dim / (c->dtype == DP_BF16 ? 8 : 4)), true);
   const unsigned g = blocks_of(a);
-  const bool codes = c->format == DP_KV_FP8;
   (void)hipGetLastError();
-#define READ(T, HD) do { if (codes) k_read_rows<T, HD, true><<<g, 256, 0, st>>>(a); else k_read_rows<T, HD, false><<<g, 256, 0, st>>>(a); } while (0)
+#define READ(T, HD) do { if (c->format == DP_KV_FP4) k_read_rows<T, HD, DP_KV_FP4><<<g, 256, 0, st>>>(a); \
+    else if (c->format == DP_KV_FP8) k_read_rows<T, HD, DP_KV_FP8><<<g, 256, 0, st>>>(a); else k_read_rows<T, HD, DP_KV_PLAIN><<<g, 256, 0, st>>>(a); } while (0)
   if (c->dtype == DP_BF16) { if (c->head_dim == 128) READ(bf16_t, 128); else READ(bf16_t, 64); }
   else { if (c->head_dim == 128) READ(float, 128); else READ(float, 64); }
 #undef READ

@@ -1,10 +1,11 @@
-// What the kernels around the paged key/value cache share: where a token's head lies in the pages, codes of 8 bits, and the
+// What the kernels around the paged key/value cache share: where a token's head lies in the pages, codes of 8 and 4 bits, and the
 // checks of rows and caches at the C entries.
 #pragma once
 #include "../../include/dualparal.h"
 #include <stdio.h>
 
 #include "common.h"
+#include "fp4.h"
 
 int dp_set_error(int code, const char* msg);   // defined next to dp_last_error
 
@@ -48,10 +49,10 @@ inline const char* why_not_head(int32_t heads, int32_t head_dim, int32_t dtype) 
 inline const char* why_not_cache(const dp_kv_cache* c) {
   if (!c) return "null pointer";
   if (const char* why = why_not_head(c->kv_heads, c->head_dim, c->dtype)) return why;
-  if (c->format != DP_KV_PLAIN && c->format != DP_KV_FP8) return "the cache's format must be DP_KV_PLAIN or DP_KV_FP8";
+  if (c->format != DP_KV_PLAIN && c->format != DP_KV_FP8 && c->format != DP_KV_FP4) return "the cache's format must be DP_KV_PLAIN, DP_KV_FP8 or DP_KV_FP4";
   if (c->page_tokens < 16 || c->page_tokens > 65536 || (c->page_tokens & (c->page_tokens - 1))) return "page_tokens must be a power of two in [16, 65536]";
   if (c->n_pages < 1 || (int64_t)c->n_pages * c->page_tokens > 0x7fffffff) return "n_pages * page_tokens must be in [1, 2^31 - 1]";
-  if (!c->data || (c->format == DP_KV_FP8 && !c->scales)) return "null pointer";
+  if (!c->data || (c->format != DP_KV_PLAIN && !c->scales)) return "null pointer";
   if ((uintptr_t)c->data & 15) return "the cache must be 16-byte aligned";
   return nullptr;
 }
