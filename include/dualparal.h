@@ -420,6 +420,36 @@ int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_
                   const int32_t* kv_len, const int32_t* page_table, const dp_rows* out, void* workspace, size_t workspace_bytes,
                   void* hip_stream);
 
+/* What lies between two branches of a layer, in one pass: the branch's output y, normalised before or not, gated and added to the residual stream x, and the
+ * stream normalised for the next branch:
+ *   x' = x + res_scale * gate[g] * t,   t = y, or N(y) * post_gain if post_gain is given
+ *   h  = N(x') * gain * (1 + scale[g]) + shift[g]
+ * with N a LayerNorm (biased variance, no affine part) or an RMSNorm over the row's dim values, both with eps, and g the row's group (a video, a block at its own
+ * noise level).  What is not given (NULL) is 1, or 0 for scale and shift.  y NULL: x' = x (before the first branch; then x_out is NULL too).  h NULL: x' alone
+ * (behind the last branch).  x_out NULL: h alone.
+ * Statistics, products and sums are fp32, h comes from x' before it is rounded; one rounding each.  The sum of a row's squares has to be a normal fp32
+ * number (or its mean small next to eps).
+ *   x, x_out   : device [n, dim] of stream_dtype, rows x_stride (x_out_stride) elements apart;  y, h : device [n, dim] of dtype.  Data and strides are
+ *                multiples of 16 bytes (a stride that is never used may be anything), strides not negative, rows that are written do not overlap one another.
+ *                x_out may be x, and h may be y (same data and stride); any other overlap with what is read is not allowed.
+ *   group      : device int32 [n], or NULL: group 0 for all.  A row whose group is outside [0, n_groups) is padding: its x_out and h are left as they are.
+ * n == 0 is a no-op.  Asynchronous on hip_stream; allocates nothing and may be recorded into a HIP graph.
+ * Errors: DP_EINVAL (null pointer, sizes outside the limits, more than 2^24 rows, alignment or strides as above, an option without what it goes with), DP_EHIP. */
+enum { DP_NORM_LAYER = 0, DP_NORM_RMS = 1 };
+typedef struct {
+  int32_t dim;                /* a multiple of 8, 8 .. 16384                                       */
+  int32_t dtype;              /* DP_F32 or DP_BF16: y, h and the gains                             */
+  int32_t stream_dtype;       /* of x and x_out: DP_F32, or dtype                                  */
+  int32_t norm;               /* DP_NORM_*                                                         */
+  int32_t n_groups;           /* >= 1                                                              */
+  float eps, res_scale;
+  const void *gain, *post_gain;        /* device [dim] of dtype, 16-byte aligned, or NULL          */
+  const float *gate, *scale, *shift;   /* device [n_groups, dim], 16-byte aligned, or NULL; scale and shift together */
+  const int32_t* group;
+} dp_gated_norm_config;
+int dp_gated_norm(const dp_gated_norm_config* cfg, const void* x, int64_t x_stride, const void* y, int64_t y_stride, int64_t n, void* x_out,
+                  int64_t x_out_stride, void* h, int64_t h_stride, void* hip_stream);
+
 /* Test hook: copies an internal result to `dst` as float32, token-major [rows, dim].
  *   what : DP_PEEK_*; layer is used by the K / V / cache / modulation peeks, the others refer to the
  *          last layer the last forward ran (they need cfg.debug_taps for X_SELF / X_CROSS).

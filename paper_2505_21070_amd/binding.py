@@ -141,8 +141,14 @@ class AttnConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("q_heads", "n_seqs", "max_q", "max_kv", "table_width", "causal_group")] + [("scale", C.c_float)]
 
 
+class GatedNorm(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dim", "dtype", "stream_dtype", "norm", "n_groups")] + [("eps", C.c_float), ("res_scale", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("gain", "post_gain", "gate", "scale", "shift", "group")]
+
+
 # structs of these calls are passed as bytes packed anew for each call: a third of the time that filling in ctypes' own takes
 _PACK_ROWS, _PACK_NORM, _PACK_ATTN = struct.Struct("Pqq").pack, struct.Struct("4i2f3P").pack, struct.Struct("6if").pack
+_PACK_GATED = struct.Struct("5i2f6P").pack
 _lib.dp_qk_norm_rope.restype = C.c_int
 _lib.dp_qk_norm_rope.argtypes = [C.c_void_p] * 3 + [C.c_int64] + [C.c_void_p] * 3
 _lib.dp_kv_write.restype = C.c_int
@@ -155,6 +161,8 @@ _lib.dp_attn_paged_workspace_bytes.restype = C.c_size_t
 _lib.dp_attn_paged_workspace_bytes.argtypes = [C.c_void_p] * 2 + [C.c_int64]
 _lib.dp_attn_paged.restype = C.c_int
 _lib.dp_attn_paged.argtypes = [C.c_void_p] * 3 + [C.c_int64] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+_lib.dp_gated_norm.restype = C.c_int
+_lib.dp_gated_norm.argtypes = [C.c_void_p] * 2 + [C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
 _lib.dp_stage_free.argtypes = [C.c_void_p]
 _lib.dp_last_error.restype = C.c_char_p
 _lib.dp_last_error.argtypes = []
@@ -566,6 +574,63 @@ class KVCache:
         _check(_lib.dp_attn_paged(self._desc, cfg, _rows(q, hq, n, d, td, dev), n, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                                   to_out, work.data_ptr() if nbytes else None, nbytes, st), "dp_attn_paged")
         return out
+
+
+NORM = {"layer": 0, "rms": 1}
+
+
+def _rows_2d(t, n, d, td, device):
+    """Address and stride of [n, d] rows of a type on a device."""
+    assert t.shape == (n, d) and t.dtype == td and t.device == device, (tuple(t.shape), t.dtype, t.device, (n, d), td, device)
+    s, cs = t.stride()
+    assert cs == 1 or n == 0, t.stride()
+    return t.data_ptr(), s
+
+
+def _result_2d(t, n, d, td, like, stream):
+    """The caller's rows for a result, or new ones, with address and stride."""
+    if t is not None:
+        return (t,) + _rows_2d(t, n, d, td, like.device)
+    t = like.new_empty((n, d), dtype=td) if stream is None else _memory(lambda: like.new_empty((n, d), dtype=td), stream)
+    return t, t.data_ptr(), d
+
+
+def _vector(t, shape, td, device):
+    """Address of an optional contiguous vector, 0 if there is none."""
+    if t is None:
+        return 0
+    assert t.shape == shape and t.dtype == td and t.device == device and t.is_contiguous(), (tuple(t.shape), t.dtype, t.device, shape, td, device)
+    return t.data_ptr()
+
+
+def gated_norm(x, y=None, gain=None, post_gain=None, gate=None, scale=None, shift=None, group=None, norm="layer", res_scale=1.0, eps=1e-6, x_out=None, out=None,
+               dtype=None, next_norm=True, stream=None):
+    """What lies between two branches of a layer, in one pass: x' = x + res_scale * gate * t with t = y, or N(y) * post_gain, and
+    h = N(x') * gain * (1 + scale) + shift, N a LayerNorm ("layer") or an RMSNorm ("rms").  x: [n, dim] residual stream, float32 or of the rows' type; y: [n, dim] of
+    the rows' type; gain, post_gain: [dim] of the rows' type; gate, scale, shift: float32 [n_groups, dim]; group: int32 [n], the rows' groups (outside: padding,
+    left as it is), group 0 if not given.  Without y, h = N(x) ... alone (dtype: the rows' type, x's if not given); next_norm=False: x' alone.  x_out may be x
+    and out may be y.  Returns (x', h), None for what is not computed."""
+    n, d = x.shape
+    dev, ts = x.device, x.dtype
+    td = y.dtype if y is not None else ts if dtype is None else {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    st = _stream_on(dev, stream)
+    assert td in _KV_DTYPE and (ts == torch.float32 or ts == td), (ts, td)
+    assert y is not None or next_norm, "nothing to compute"
+    assert (y is not None or x_out is None) and (next_norm or out is None), "a result that is not computed"
+    groups = next((t.shape[0] for t in (gate, scale, shift) if t is not None), 1 if group is None else 2 ** 31 - 1)
+    vectors, f32 = (groups, d), torch.float32
+    cfg = _PACK_GATED(d, _KV_DTYPE[td], _KV_DTYPE[ts], NORM[norm], groups, eps, res_scale, _vector(gain, (d,), td, dev), _vector(post_gain, (d,), td, dev),
+                      _vector(gate, vectors, f32, dev), _vector(scale, vectors, f32, dev), _vector(shift, vectors, f32, dev),
+                      _vector(group, (n,), torch.int32, dev))
+    x_at, x_s = _rows_2d(x, n, d, ts, dev)
+    y_at, y_s, xo_at, xo_s, h_at, h_s = 0, 0, 0, 0, 0, 0
+    if y is not None:
+        y_at, y_s = _rows_2d(y, n, d, td, dev)
+        x_out, xo_at, xo_s = _result_2d(x_out, n, d, ts, x, stream)
+    if next_norm:
+        out, h_at, h_s = _result_2d(out, n, d, td, x, stream)
+    _check(_lib.dp_gated_norm(cfg, x_at, x_s, y_at, y_s, n, xo_at, xo_s, h_at, h_s, st), "dp_gated_norm")
+    return x_out, out
 
 
 def pipeline_simulate(n_devices, T, block_num, order="reverse"):

@@ -21,3 +21,26 @@ def test_bad_caches(bad):
 
 def test_nothing_to_do():
     assert P.write(c=cache4(), n=0) == P.read(c=cache4(), n=0) == P.qkv(c=cache4(), n=0) == P.attend(c=cache4(), n=0) == B.DP_OK
+
+
+def gated(x=P.AT, xs=128, y=P.AT, ys=128, n=3, xo=P.AT, xos=128, h=P.AT, hs=128, **kw):
+    d = dict(dim=128, dtype=B.DP_BF16, stream_dtype=B.DP_F32, norm=1, n_groups=2, eps=1e-6, res_scale=1.0, gain=P.AT, post_gain=P.AT, gate=P.AT, scale=P.AT, shift=P.AT, group=P.AT)
+    return P.L.dp_gated_norm(bytes(B.GatedNorm(**dict(d, **kw))), x, xs, y, ys, n, xo, xos, h, hs, None)
+
+
+@pytest.mark.parametrize("bad", [dict(dim=0), dict(dim=12), dict(dim=16392), dict(dtype=2), dict(stream_dtype=2), dict(dtype=B.DP_F32, stream_dtype=B.DP_BF16), dict(norm=2), dict(n_groups=0),
+                                 dict(eps=-1.0), dict(eps=float("inf")), dict(res_scale=float("inf")), dict(scale=None), dict(shift=None), dict(gain=P.AT + 4), dict(gate=P.AT + 8),
+                                 dict(group=P.AT + 1), dict(n=-1), dict(n=(1 << 24) + 1), dict(x=None), dict(y=None), dict(h=None), dict(x=P.AT + 8), dict(y=P.AT + 2), dict(xs=130),
+                                 dict(ys=132), dict(hs=-128), dict(xos=0), dict(hs=64), dict(xs=1 << 40), dict(y=None, xo=None, post_gain=None), dict(y=None, xo=None, gate=None),
+                                 dict(h=None, gain=None), dict(h=None, xo=None, gain=None, scale=None, shift=None)], ids=str)
+def test_bad_gated_norms(bad):
+    P.refused(gated(**bad), "dp_gated_norm")
+
+
+def test_gated_norms_of_nothing():
+    assert gated(n=0) == B.DP_OK
+    assert P.L.dp_gated_norm(None, P.AT, 0, P.AT, 0, 0, P.AT, 0, P.AT, 0, None) == B.DP_EINVAL
+
+
+def test_the_binding_packs_what_the_struct_holds():
+    assert B._PACK_GATED(1, 2, 3, 4, 5, 6.0, 7.0, 8, 9, 10, 11, 12, 13) == bytes(B.GatedNorm(1, 2, 3, 4, 5, 6.0, 7.0, 8, 9, 10, 11, 12, 13))
