@@ -44,3 +44,31 @@ def test_gated_norms_of_nothing():
 
 def test_the_binding_packs_what_the_struct_holds():
     assert B._PACK_GATED(1, 2, 3, 4, 5, 6.0, 7.0, 8, 9, 10, 11, 12, 13) == bytes(B.GatedNorm(1, 2, 3, 4, 5, 6.0, 7.0, 8, 9, 10, 11, 12, 13))
+
+
+def linear(w=True, x=P.AT, xs=64, n=3, act=0, y=P.AT, ys=40, **kw):
+    d = dict(out=40, in_=64, dtype=B.DP_BF16, codes=P.AT, scales=P.AT, bias=P.AT)
+    return P.L.dp_linear_fp4(bytes(B.Fp4Matrix(**dict(d, **kw))) if w else None, x, xs, n, act, y, ys, None)
+
+
+def pack(src=P.AT, stride=64, out=40, in_=64, dtype=B.DP_BF16, codes=P.AT, scales=P.AT):
+    return P.L.dp_fp4_pack(src, stride, out, in_, dtype, codes, scales, None)
+
+
+BAD_MATRIX = [dict(out=0), dict(out=(1 << 24) + 1), dict(in_=0), dict(in_=48), dict(in_=(1 << 20) + 32), dict(dtype=2), dict(codes=None), dict(scales=None), dict(codes=P.AT + 8)]
+
+
+@pytest.mark.parametrize("bad", BAD_MATRIX + [dict(w=False), dict(n=-1), dict(n=(1 << 24) + 1), dict(n=1 << 12, out=1 << 24), dict(act=3), dict(act=-1), dict(x=None), dict(y=None), dict(x=P.AT + 8),
+                                              dict(xs=68), dict(xs=-64), dict(xs=1 << 23), dict(y=P.AT + 1), dict(bias=P.AT + 1), dict(ys=39), dict(ys=1 << 39),
+                                              dict(dtype=B.DP_F32, y=P.AT + 2)], ids=str)
+def test_bad_linears(bad):
+    P.refused(linear(**bad), "dp_linear_fp4")
+
+
+@pytest.mark.parametrize("bad", BAD_MATRIX + [dict(src=None), dict(src=P.AT + 1), dict(stride=-1), dict(out=1 << 24, in_=1 << 13)], ids=str)
+def test_bad_packs(bad):
+    P.refused(pack(**bad), "dp_fp4_pack")
+
+
+def test_linears_of_nothing():
+    assert linear(n=0) == linear(n=0, x=None, y=None) == B.DP_OK

@@ -1,0 +1,200 @@
+"""Products with 4-bit weights on the GPU, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import fp4 as F
+from paged import HALF, TD, U, np64
+
+pytestmark = pytest.mark.gpu
+# tokens, out, in: each kernel and its tiles' borders, one group, rows that divide nothing, long sums
+SIZES = [(1, 1, 32), (1, 16, 64), (1, 17, 96), (1, 4608, 1536), (2, 33, 256), (3, 100, 288), (15, 64, 512), (16, 48, 2080), (17, 31, 160), (32, 130, 4128), (33, 129, 544), (48, 80, 1024), (64, 65, 320),
+         (65, 64, 128), (65, 1, 32), (70, 257, 96), (100, 300, 992), (128, 256, 256), (129, 255, 160), (200, 513, 1504), (260, 70, 64), (513, 129, 416), (1000, 24, 2048)]
+
+
+def matrix(out, in_, seed=0, scale_bits=4):
+    """(Linear4's codes and scales, the values they stand for)"""
+    gen = torch.Generator().manual_seed(seed)
+    codes = torch.randint(0, 256, (out, in_ // 2), generator=gen).to(torch.uint8)
+    scales = torch.randint(127 - scale_bits, 128 + scale_bits, (out, in_ // 32), generator=gen).to(torch.uint8)
+    return codes.cuda().view(torch.float4_e2m1fn_x2), scales.cuda(), F.decode(F.unpack(codes.numpy()), scales.numpy())
+
+
+def check(got, x, w, bias, act, dtype):
+    """Sums: one rounding (or a truncation, two halves) for each product of each part and for the wavefronts' sums and the bias; sizes of an input's parts
+    are its own.  The activation's slope is at most 1.13; its own work: the exponent's argument, 4 roundings, moves the result by its size, function, reciprocal, product 6."""
+    ref, y, size = F.linear(np64(x), w, None if bias is None else np64(bias), act)
+    adds = w.shape[1] * (3 if dtype == "f32" else 1) + 12
+    work = 2 * adds * U * size * (1.13 if act else 1.0)
+    if act:
+        arg = np.abs(y) * 1.45 if act == "silu" else 2.31 * np.abs(y + 0.044715 * y ** 3)
+        work = work + np.abs(ref) * U * (6 + 4 * arg)
+    err, tol = np.abs(np64(got) - ref), HALF[dtype] * (np.abs(ref) + work) + work + 1e-37
+    assert got.shape == ref.shape and (err <= tol).all(), (np.argwhere(err > tol)[:4].tolist(), float((err / tol).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,out,in_", SIZES)
+def test_against_the_definition(n, out, in_, dtype):
+    from paper_2505_21070_amd import binding as B
+    codes, scales, w = matrix(out, in_, seed=n + out)
+    gen = torch.Generator().manual_seed(n)
+    x = (torch.randn((n, in_), generator=gen) * 0.3).to(TD[dtype])
+    x[:, ::16] *= 7
+    bias = torch.randn(out, generator=gen).to(TD[dtype]).cuda()
+    for b, act in ((None, None), (bias, "gelu"), (bias, "silu")):
+        m = B.Linear4(codes, scales, b, dtype)
+        check(m.forward(x.cuda(), act=act), x, w, b, act, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,out,in_", SIZES + [(7, 512, 13824), (90, 300, 13824)])
+def test_whole_numbers_are_exact(n, out, in_, dtype):
+    """Small whole numbers: every sum is exact, so every input is there once, and nothing else."""
+    from paper_2505_21070_amd import binding as B
+    codes, scales, w = matrix(out, in_, seed=n, scale_bits=1)
+    x = torch.randint(-3, 4, (n, in_), generator=torch.Generator().manual_seed(out)).to(TD[dtype])
+    got = B.Linear4(codes, scales, None, dtype).forward(x.cuda())
+    want = torch.from_numpy(np64(x) @ w.T)
+    assert want.abs().max() < 2 ** 20
+    assert torch.equal(got.cpu(), want.float().to(TD[dtype]))
+
+
+@pytest.mark.parametrize("n", [1, 20, 64, 65, 130])
+def test_all_bits_of_fp32_inputs(n):
+    """One weight of 1 at a time: the output is the input, bit by bit, as far as bf16's exponents reach."""
+    from paper_2505_21070_amd import binding as B
+    in_ = 160
+    code = np.zeros((in_, in_), int)
+    code[np.arange(in_), np.arange(in_)] = 2
+    codes = torch.from_numpy((code[:, 0::2] | code[:, 1::2] << 4).astype(np.uint8)).cuda().view(torch.float4_e2m1fn_x2)
+    m = B.Linear4(codes, torch.full((in_, in_ // 32), 127, dtype=torch.uint8, device="cuda"), dtype="f32")
+    bits = torch.randint(-2 ** 31, 2 ** 31, (n, in_), generator=torch.Generator().manual_seed(n)).to(torch.int32)
+    bits = bits & ~0x7f800000 | torch.randint(30, 254, (n, in_), generator=torch.Generator().manual_seed(1)).to(torch.int32) << 23
+    x = bits.view(torch.float32)
+    # other inputs of the row are up to 2^97 times as large, and multiplied by 0
+    assert torch.equal(m.forward(x.cuda()).cpu(), x)
+
+
+@pytest.mark.parametrize("n", [1, 17, 64, 65, 140])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_are_not_finite(dtype, n):
+    from paper_2505_21070_amd import binding as B
+    out, in_ = 40, 224
+    codes, scales, w = matrix(out, in_, seed=3)
+    scales[5, 6] = 255
+    w[5, 192:] = np.nan
+    x = torch.randn((n, in_), generator=torch.Generator().manual_seed(2)).to(TD[dtype])
+    at = [0] if n == 1 else [0, n // 2, n - 1]
+    for j, t in enumerate(at):
+        x[t, 200 if j == 0 else 3] = [float("inf"), float("nan"), -float("inf")][j]
+    got = np64(B.Linear4(codes, scales, None, dtype).forward(x.cuda()))
+    with np.errstate(invalid="ignore"):
+        ref = np64(x) @ w.T
+        products = np64(x)[:, None, :] * w[None]
+        ref = np.where(np.isnan(products).any(-1), np.nan, ref)
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    inf = np.isinf(ref)
+    assert np.array_equal(got[inf], ref[inf]) and inf.any() and np.isnan(got[:, 5]).all()
+    fine = np.isfinite(ref)
+    size = (np.abs(np.where(np.isfinite(np64(x)), np64(x), 0)) @ np.abs(np.nan_to_num(w)).T)[fine]          # see check()
+    assert (np.abs(got[fine] - ref[fine]) <= HALF[dtype] * np.abs(ref[fine]) * (1 + 2.0 ** -7) + 2 * (3 * in_ + 12) * U * size).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 5, 40, 65, 300])
+def test_strides_and_what_lies_around(n, dtype):
+    from paper_2505_21070_amd import binding as B
+    out, in_ = 77, 288
+    codes, scales, w = matrix(out, in_, seed=9)
+    m = B.Linear4(codes, scales, None, dtype)
+    gen = torch.Generator().manual_seed(4)
+    wide = torch.full((n + 2, in_ + 64), float("nan"), dtype=TD[dtype], device="cuda")
+    x = wide[1: n + 1, 32: 32 + in_]
+    x.copy_(torch.randn((n, in_), generator=gen))
+    plain = m.forward(x.contiguous())
+    assert torch.equal(m.forward(x), plain)
+    y = torch.full((n + 2, out + 5), 7.0, dtype=TD[dtype], device="cuda")
+    assert m.forward(x, out=y[1: n + 1, 3: 3 + out]) .data_ptr() == y[1:, 3:].data_ptr()
+    assert torch.equal(y[1: n + 1, 3: 3 + out], plain)
+    y[1: n + 1, 3: 3 + out] = 7.0
+    assert (y == 7).all()
+    # one row as every token
+    assert torch.equal(m.forward(x[:1].expand(n, in_)), plain[:1].expand(n, out)) if n > 1 else True
+
+
+def test_pack():
+    from paper_2505_21070_amd import binding as B
+    for dtype in ("bf16", "f32"):
+        for out, in_ in ((1, 32), (7, 96), (300, 1504), (33, 64)):
+            w = torch.randn((out, in_ + 8), generator=torch.Generator().manual_seed(out)) * 2.0 ** torch.randint(-30, 30, (out, 1), generator=torch.Generator().manual_seed(1)).float()
+            w = w.to(TD[dtype])
+            w[0, :3] = torch.tensor([1e38, -0.0, 1e-38])
+            if out > 1:
+                w[1, 31], w[2, 5] = float("nan"), -float("inf")
+            m = B.Linear4.pack(w.cuda()[:, :in_])
+            code, byte = F.encode(np64(w[:, :in_]))
+            assert np.array_equal(F.unpack(m.codes.view(torch.uint8).cpu().numpy()), code) and np.array_equal(m.scales.cpu().numpy(), byte)
+            assert m.torch_dtype == TD[dtype] and (m.out, m.in_) == (out, in_)
+
+
+@pytest.mark.parametrize("n", [1, 30, 200])
+def test_captured_and_replayed_and_repeated(n):
+    from paper_2505_21070_amd import binding as B
+    codes, scales, _ = matrix(700, 1024)
+    m = B.Linear4(codes, scales, None, "bf16")
+    x = torch.randn((n, 1024), device="cuda").bfloat16()
+    y = m.forward(x)
+    assert torch.equal(m.forward(x), y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.forward(x, act="gelu", out=y)
+    for k in range(4):
+        x.mul_(1.25)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(m.forward(x, act="gelu"), y)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    z = m.forward(x, act="gelu", stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(z, y)
+    assert m.forward(x[:0]).shape == (0, 700)
+
+
+def test_codes_beyond_32_bits():
+    """A matrix of more than 2^32 bytes of codes: its last outputs."""
+    from paper_2505_21070_amd import binding as B
+    in_, out = 1 << 16, (1 << 17) + 300
+    codes = torch.zeros((out, in_ // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.full((out, in_ // 32), 127, dtype=torch.uint8, device="cuda")
+    codes[-1, -1], codes[-2, 0] = 0x20, 0x02
+    m = B.Linear4(codes.view(torch.float4_e2m1fn_x2), scales)
+    for n in (1, 70):
+        x = torch.zeros((n, in_), dtype=torch.bfloat16, device="cuda")
+        x[:, -1], x[:, 0] = 3.0, 5.0
+        y = m.forward(x)
+        assert (y[:, -1] == 3).all() and (y[:, -2] == 5).all() and (y[:, :-2] == 0).all()
+
+
+def test_refused_by_the_binding():
+    from paper_2505_21070_amd import binding as B
+    codes, scales, _ = matrix(8, 64)
+    m = B.Linear4(codes, scales)
+    x = torch.zeros((3, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in ((codes.view(torch.uint8), scales), (codes, scales[:, :1].contiguous()), (codes, scales.float()), (codes.cpu(), scales), (codes, scales, torch.zeros(7, device="cuda").bfloat16()),
+                (codes, scales, torch.zeros(8, device="cuda"))):
+        with pytest.raises(AssertionError):
+            B.Linear4(*bad)
+    for bad in (x.float(), x[:, :32], x.cpu(), x.t().contiguous().t()):
+        with pytest.raises(AssertionError):
+            m.forward(bad)
+    with pytest.raises(AssertionError):
+        m.forward(x, out=torch.zeros((3, 9), dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(KeyError):
+        m.forward(x, act="relu")
+    with pytest.raises(B.DualParalError) as e:
+        m.forward(torch.zeros((3, 68), dtype=torch.bfloat16, device="cuda")[:, 4:])
+    assert e.value.code == B.DP_EINVAL and "16-byte" in str(e.value)
+    with pytest.raises(AssertionError):
+        B.Linear4.pack(torch.zeros((4, 40), device="cuda"))
