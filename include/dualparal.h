@@ -421,28 +421,35 @@ int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_
                   void* hip_stream);
 
 /* Products with weights held in 4 bits: y = act(x W^T + bias) for n tokens, one to many.  W [out, in] is held as DP_KV_FP4 holds rows: codes e2m1, two to a byte,
- * the first one in its low half, and a byte for each 32 values of a row.  dp_fp4_pack makes codes and bytes of a matrix (out * in <= 2^36); the bytes 27 .. 252 and 255 (NaN) are
- * those it writes, 1 .. 254 are read as 2^(b - 127).
- *   codes  : device [out, in / 2], 16-byte aligned;  scales : device [out, in / 32];  bias : device [out] of dtype, or NULL
+ * the first one in its low half, and a byte for each 32 values of a row.  dp_fp4_pack makes codes and bytes of a matrix; the bytes 27 .. 252 and 255 (NaN) are those it
+ * writes, 1 .. 254 are read as 2^(b - 127).  dp_fp4_lay puts both, once, into the order that the products read them in: out and in are filled up to multiples of 16 and
+ * 128, which is all that is known of that order; it takes 0.53 bytes a weight as the codes do, which are not needed any more.
+ *   codes  : device [out, in / 2], 16-byte aligned;  scales : device [out, in / 32]
+ *   laid   : device, dp_fp4_laid_bytes(out, in) bytes, 64-byte aligned;  bias : device [out] of dtype, or NULL
  *   src    : device, row o at src + o * stride elements, of dtype
- *   x      : device, token t's in values at x + t * x_stride elements, of dtype, 16-byte aligned in its stride too, x_stride in [0, 2^22]
+ *   x      : device, token t's in values at x + t * x_stride elements, of dtype, 16-byte aligned in its stride too, x_stride in [0, 2^21]
  *   y      : device, token t's out values at y + t * y_stride, of dtype; must not overlap anything that is read
  * Sums are fp32: an input of 32 bits is multiplied in three exact parts of 8 bits (parts below 2^-126 may count as 0, as inputs of 16 bits below it may), a weight is exact, the
- * activation is fp32; one rounding at the end.  A token's result does not depend on the tokens beside it, but for the order of its sum, which is the kernel's that the number
- * of tokens selects; a call repeats its bits.  What is not finite in x reaches that token's outputs as in exact arithmetic (infinity times 0 is NaN), a NaN byte its row's.
+ * activation is fp32; one rounding at the end.  A token's result does not depend on the tokens beside it, but for the order of its sum, which goes by the number of tokens; a call
+ * repeats its bits.  What is not finite in x reaches that token's outputs as in exact arithmetic (infinity times 0 is NaN), a NaN byte its row's.
+ *   workspace  : device, 256-byte aligned, dp_linear_fp4_workspace_bytes(w, n) bytes (0 for many calls: then it may be NULL), used by one call at a time; nothing has to be
+ *                kept in it between calls.
  * n == 0 is a no-op.  Asynchronous on hip_stream; allocates nothing and may be recorded into a HIP graph.
- * Errors: DP_EINVAL (null pointer, sizes outside the limits, n * out above 2^35, alignment or strides as above), DP_EHIP. */
+ * Errors: DP_EINVAL (null pointer, sizes outside the limits, n * out above 2^35, alignment or strides as above), DP_ENOMEM (workspace too small), DP_EHIP. */
 enum { DP_ACT_NONE = 0, DP_ACT_GELU = 1 /* tanh approximation, the stage's */, DP_ACT_SILU = 2 };
 typedef struct {
   int32_t out;                /* 1 .. 2^24                                                         */
-  int32_t in;                 /* a multiple of 32, 32 .. 2^20                                      */
+  int32_t in;                 /* a multiple of 32, 32 .. 2^20; out * in <= 2^36                    */
   int32_t dtype;              /* DP_F32 or DP_BF16: x, y and the bias                              */
-  const void* codes;
-  const uint8_t* scales;
+  const void* laid;
   const void* bias;
 } dp_fp4_matrix;
+size_t dp_fp4_laid_bytes(int32_t out, int32_t in);             /* 0 if the sizes are invalid */
 int dp_fp4_pack(const void* src, int64_t stride, int32_t out, int32_t in, int32_t dtype, void* codes, uint8_t* scales, void* hip_stream);
-int dp_linear_fp4(const dp_fp4_matrix* w, const void* x, int64_t x_stride, int64_t n, int32_t act, void* y, int64_t y_stride, void* hip_stream);
+int dp_fp4_lay(const void* codes, const uint8_t* scales, int32_t out, int32_t in, void* laid, void* hip_stream);
+size_t dp_linear_fp4_workspace_bytes(const dp_fp4_matrix* w, int64_t n);   /* 0 also if an argument is invalid: dp_linear_fp4 says why */
+int dp_linear_fp4(const dp_fp4_matrix* w, const void* x, int64_t x_stride, int64_t n, int32_t act, void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,
+                  void* hip_stream);
 
 /* What lies between two branches of a layer, in one pass: the branch's output y, normalised before or not, gated and added to the residual stream x, and the
  * stream normalised for the next branch:

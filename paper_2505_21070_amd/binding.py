@@ -142,7 +142,7 @@ class AttnConfig(C.Structure):
 
 
 class Fp4Matrix(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("out", "in_", "dtype")] + [(n, C.c_void_p) for n in ("codes", "scales", "bias")]
+    _fields_ = [(n, C.c_int32) for n in ("out", "in_", "dtype")] + [(n, C.c_void_p) for n in ("laid", "bias")]
 
 
 class GatedNorm(C.Structure):
@@ -167,8 +167,14 @@ _lib.dp_attn_paged.restype = C.c_int
 _lib.dp_attn_paged.argtypes = [C.c_void_p] * 3 + [C.c_int64] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
 _lib.dp_fp4_pack.restype = C.c_int
 _lib.dp_fp4_pack.argtypes = [C.c_void_p, C.c_int64] + [C.c_int32] * 3 + [C.c_void_p] * 3
+_lib.dp_fp4_laid_bytes.restype = C.c_size_t
+_lib.dp_fp4_laid_bytes.argtypes = [C.c_int32] * 2
+_lib.dp_fp4_lay.restype = C.c_int
+_lib.dp_fp4_lay.argtypes = [C.c_void_p] * 2 + [C.c_int32] * 2 + [C.c_void_p] * 2
+_lib.dp_linear_fp4_workspace_bytes.restype = C.c_size_t
+_lib.dp_linear_fp4_workspace_bytes.argtypes = [C.c_void_p, C.c_int64]
 _lib.dp_linear_fp4.restype = C.c_int
-_lib.dp_linear_fp4.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+_lib.dp_linear_fp4.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.dp_gated_norm.restype = C.c_int
 _lib.dp_gated_norm.argtypes = [C.c_void_p] * 2 + [C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
 _lib.dp_stage_free.argtypes = [C.c_void_p]
@@ -614,32 +620,40 @@ def _vector(t, shape, td, device):
 ACT = {None: 0, "gelu": 1, "silu": 2}
 
 
+def pack_fp4(w, stream=None):
+    """A matrix w [out, in], in a multiple of 32, rounded to 4 bits: codes float4_e2m1fn_x2 [out, in / 2] and scales uint8 [out, in / 32], as KVCache holds rows."""
+    o, i = w.shape
+    st = _stream_on(w.device, stream)
+    assert w.dtype in _KV_DTYPE and w.stride(1) == 1 and i % 32 == 0, (w.dtype, w.stride(), w.shape)
+    new = lambda *shape: w.new_empty(shape, dtype=torch.uint8)   # noqa: E731
+    codes, scales = (new(o, i // 2), new(o, i // 32)) if stream is None else [_memory(lambda: new(o, k), stream) for k in (i // 2, i // 32)]
+    _check(_lib.dp_fp4_pack(w.data_ptr(), w.stride(0), o, i, _KV_DTYPE[w.dtype], codes.data_ptr(), scales.data_ptr(), st), "dp_fp4_pack")
+    return codes.view(torch.float4_e2m1fn_x2), scales
+
+
 class Linear4:
     """y = act(x W^T + bias) with weights in 4 bits.  codes: float4_e2m1fn_x2 [out, in / 2], scales: uint8 [out, in / 32], a byte b for 32 values that stands for
-    the factor 2^(b - 127) (255: NaN), as in KVCache; bias: [out] of the tokens' type, or None.  dtype ("f32", "bf16") is that of the tokens.  The tensors are the caller's
-    and may be looked at.  Calls on a named stream wait for nobody, as KVCache's."""
+    the factor 2^(b - 127) (255: NaN), as pack_fp4 makes them; bias: [out] of the tokens' type, or None.  dtype ("f32", "bf16") is that of the tokens.  Codes and
+    scales are read once, here, into the order that the products want (`laid`, of the same size), and not kept.  Calls on a named stream wait for nobody, as
+    KVCache's."""
 
-    def __init__(self, codes, scales, bias=None, dtype="bf16"):
-        td = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    def __init__(self, codes, scales, bias=None, dtype="bf16", stream=None):
+        td, dev = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype], codes.device
         assert codes.is_cuda and codes.dtype == torch.float4_e2m1fn_x2 and codes.dim() == 2 and codes.is_contiguous(), (tuple(codes.shape), codes.dtype)
         self.out, self.in_ = codes.shape[0], 2 * codes.shape[1]
-        assert scales.dtype == torch.uint8 and scales.shape == (self.out, self.in_ // 32) and scales.is_contiguous() and scales.device == codes.device
-        self.codes, self.scales, self.bias, self.torch_dtype, self._dev = codes, scales, bias, td, codes.device
-        self._desc = bytes(Fp4Matrix(self.out, self.in_, _KV_DTYPE[td], codes.data_ptr(), scales.data_ptr(), _vector(bias, (self.out,), td, codes.device) or None))
+        assert scales.dtype == torch.uint8 and scales.shape == (self.out, self.in_ // 32) and scales.is_contiguous() and scales.device == dev
+        st, nbytes = _stream_on(dev, stream), _lib.dp_fp4_laid_bytes(self.out, self.in_)
+        if nbytes == 0:
+            raise DualParalError(DP_EINVAL, "dp_fp4_laid_bytes")
+        self.laid = _memory(lambda: torch.empty(nbytes, dtype=torch.uint8, device=dev), stream)
+        _check(_lib.dp_fp4_lay(codes.data_ptr(), scales.data_ptr(), self.out, self.in_, self.laid.data_ptr(), st), "dp_fp4_lay")
+        self.bias, self.torch_dtype, self._dev, self._need = bias, td, dev, (0, 0)
+        self._desc = bytes(Fp4Matrix(self.out, self.in_, _KV_DTYPE[td], self.laid.data_ptr(), _vector(bias, (self.out,), td, dev) or None))
 
     @classmethod
     def pack(cls, w, bias=None, stream=None):
         """The same of a matrix w [out, in] of the tokens' type, rounded to 4 bits."""
-        o, i = w.shape
-        st = _stream_on(w.device, stream)
-        assert w.dtype in _KV_DTYPE and (w.stride(1) == 1 or i == 1) and i % 32 == 0, (w.dtype, w.stride(), w.shape)
-
-        def new(*shape):
-            make = lambda: w.new_empty(shape, dtype=torch.uint8)   # noqa: E731
-            return make() if stream is None else _memory(make, stream)
-        codes, scales = new(o, i // 2), new(o, i // 32)
-        _check(_lib.dp_fp4_pack(w.data_ptr(), w.stride(0), o, i, _KV_DTYPE[w.dtype], codes.data_ptr(), scales.data_ptr(), st), "dp_fp4_pack")
-        return cls(codes.view(torch.float4_e2m1fn_x2), scales, bias, "bf16" if w.dtype == torch.bfloat16 else "f32")
+        return cls(*pack_fp4(w, stream), bias, "bf16" if w.dtype == torch.bfloat16 else "f32", stream)
 
     def forward(self, x, act=None, out=None, stream=None):
         """x: [n, in], which may be a view of wider rows; act: None, "gelu" (tanh) or "silu".  Returns [n, out]."""
@@ -647,7 +661,12 @@ class Linear4:
         st = _stream_on(dev, stream)
         x_at, x_s = _rows_2d(x, n, self.in_, td, dev)
         out, o_at, o_s = _result_2d(out, n, self.out, td, x, stream)
-        _check(_lib.dp_linear_fp4(self._desc, x_at, x_s, n, ACT[act], o_at, o_s, st), "dp_linear_fp4")
+        need = self._need                       # (tokens, bytes) of the call before: the size of the workspace goes by the tokens alone
+        if need[0] != n:
+            self._need = need = (n, _lib.dp_linear_fp4_workspace_bytes(self._desc, n))
+        nbytes = need[1]
+        work = _memory(lambda: torch.empty(nbytes, dtype=torch.uint8, device=dev), stream, result=False) if nbytes else None
+        _check(_lib.dp_linear_fp4(self._desc, x_at, x_s, n, ACT[act], o_at, o_s, work.data_ptr() if nbytes else None, nbytes, st), "dp_linear_fp4")
         return out
 
 

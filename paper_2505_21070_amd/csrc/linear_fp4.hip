@@ -4,8 +4,8 @@
 // v_mfma_f32_16x16x32_bf16: 16 outputs of a row tile against 16 tokens.  fp32 inputs are split into three bf16 parts of 8 bits each, which together are
 // the input exactly (as far as bf16 reaches down: a part below 2^-126 may be lost), so that fp32 takes the same instructions three times instead of ones of 1/16 the rate; all sums are fp32.
 //
-// The order of the products' k is free, as long as both operands have the same: a lane takes consecutive codes of one row, whole groups, and the values of the
-// token that meet them.
+// What bounds it: few tokens, the codes' way from memory (5120 -> 13824, one token 9.4 us, 4.0 TB/s); many, the matrix pipes (6240 tokens 5120 -> 5120 264 us, 1.24
+// PFLOP/s; fp32 1560 tokens 1536 -> 8960 154 us, 280 TFLOP/s, beside the parts' arithmetic).
 #include <math.h>
 #include <stdio.h>
 
@@ -25,13 +25,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 struct LinearArgs {
-  const uint8_t *codes, *scales;
+  const uint8_t* laid;
   const void *bias, *x;
   void* y;
   int64_t x_s, y_s, n;
   int32_t in, out, act;
-  int32_t row_tiles, token_tiles;          // k_many: of a block's rows and tokens
-  int32_t by_four;                         // outputs may be stored four at a time
+  int32_t row_tiles, token_tiles;          // of a block's rows and tokens
+  int32_t parts;                           // ranges of the inputs, whose sums go into partial [parts][n][out]
+  float* partial;
+  int32_t by_four, by_eight;               // outputs may be stored four at a time, eight (rows end with a whole eight)
 };
 
 __device__ __forceinline__ float activated(float v, int act) {
@@ -75,200 +77,176 @@ __device__ __forceinline__ void zero(uint4& v) { v = uint4{}; }
 __device__ __forceinline__ void zero(Raw8& v) { v.a = v.b = f32x4{0.f, 0.f, 0.f, 0.f}; }
 __device__ __forceinline__ bool finite(f32x4 v) { return fmaf(v[0], 0.f, v[1] * 0.f) + fmaf(v[2], 0.f, v[3] * 0.f) == 0.f; }
 
-// Few tokens: R * 16 outputs, NT * 16 tokens, W wavefronts that deal the inputs out in steps of 256 (wavefront w: steps w, w + W, ..) and add up in LDS in
-// wavefront order.  A lane takes 64 consecutive codes of a row, two groups, a step.  Bound by the codes' way from memory: two steps are on their way.
-template <typename T, int R, int NT, int W>
-__global__ __launch_bounds__(W * 64) void k_few(const LinearArgs a) {
-  typedef Parts<T> P;
-  __shared__ f32x4 sums[W][R * NT][64];
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row0 = blockIdx.x * (R * 16), groups = a.in / FP4_GROUP, steps = (a.in + 255) / 256;
-  const uint8_t* codes[R];
-  const uint8_t* scales[R];
+// Weights as dp_fp4_lay leaves them: for each tile of 16 rows and step of 128 inputs, one behind the other, 1024 bytes of codes and 64 of group bytes.  Codes lie as
+// the operands want them: lane l takes 16 bytes, whose word i has the eight codes of row l % 16 that product i (inputs 32 i ..) takes from it (8 (l / 16) ..), and the
+// row's four group bytes.  Rows and inputs that fill the last tile and step up are zeros.  Read row by row, the group bytes alone took as long as the codes
+// (13824 x 5120, one token: 16 us), since a wavefront's 64 bytes lay in 16 places.
+constexpr int CHUNK = 1088;
+template <int R> struct Step {
+  uint4 c[R];
+  uint32_t s[R];
+  // laid: the tiles' first chunks (uniform); codes, bytes: the lane's places in a chunk
+  __device__ __forceinline__ void load(const uint8_t* const (&laid)[R], int step, uint32_t codes, uint32_t bytes) {
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int row = row0 + r * 16 + lr < a.out ? row0 + r * 16 + lr : a.out - 1;
-    codes[r] = a.codes + (int64_t)row * (a.in / 2) + lg * 32;
-    scales[r] = a.scales + (int64_t)row * groups + lg * 2;
-  }
-  const T* x[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int64_t token = t * 16 + lr < a.n ? t * 16 + lr : a.n - 1;
-    x[t] = (const T*)a.x + token * a.x_s + lg * 64;
-  }
-  struct Step { uint4 c[R][2]; uint32_t s[R][2]; };
-  auto load = [&](Step& s, int step) __attribute__((always_inline)) {
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bool in = step * 8 + lg * 2 + h < groups;
-        s.c[r][h] = in ? *(const uint4*)(codes[r] + (int64_t)step * 128 + h * 16) : uint4{};
-        s.s[r][h] = in ? scales[r][step * 8 + h] : 127u;
-      }
-  };
-  f32x4 acc[R][NT];
-  auto multiply = [&](const Step& s, int step, auto careful) __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool in = step * 8 + lg * 2 + h < groups;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bf16x8 w[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const uint32_t c = i == 0 ? s.c[r][h].x : i == 1 ? s.c[r][h].y : i == 2 ? s.c[r][h].z : s.c[r][h].w;
-          w[r] = __builtin_bit_cast(bf16x8, fp4x8_to_bf16(c, __uint_as_float(s.s[r][h] << 23)));
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          typename P::Raw raw;
-          if (in) raw = *(const typename P::Raw*)(x[t] + step * 256 + h * 32 + i * 8); else zero(raw);
-          bf16x8 p[P::N];
-          P::template split<decltype(careful)::value>(raw, p);
-#pragma unroll
-          for (int j = 0; j < P::N; ++j)
-#pragma unroll
-            for (int r = 0; r < R; ++r) acc[r][t] = mfma(w[r], p[j], acc[r][t]);
-        }
-      }
+    for (int r = 0; r < R; ++r) {
+      const uint8_t* const at = laid[r] + (int64_t)step * CHUNK;
+      c[r] = *(const uint4*)(at + codes);
+      s[r] = *(const uint32_t*)(at + bytes);
     }
-  };
-  auto all = [&](auto careful) __attribute__((always_inline)) {
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    Step s0, s1;
-    int step = wave;
-    if (step < steps) load(s0, step);
-    if (step + W < steps) load(s1, step + W);
-    while (step < steps) {
-      const Step now = s0;
-      s0 = s1;
-      if (step + 2 * W < steps) load(s1, step + 2 * W);
-      multiply(now, step, careful);
-      step += W;
-    }
-  };
-  all(std::false_type{});
-  if constexpr (P::N > 1) {                // what is not finite has parts that are not: once more with a look at each value
-    bool fine = true;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) fine &= finite(acc[r][t]);
-    if (!__all(fine)) all(std::true_type{});
   }
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) sums[wave][r * NT + t][lane] = acc[r][t];
-  __syncthreads();
-  for (int i = threadIdx.x; i < R * NT * 256; i += W * 64) {
-    const int token = i / (R * 16), of = i % (R * 16), tile = of / 16 * NT + token / 16, at = (of % 16 / 4) * 16 + token % 16;
-    if (token >= a.n || row0 + of >= a.out) continue;
-    float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) v += sums[w][tile][at][of & 3];
-    if (a.bias) v += Elem<T>::ld((const T*)a.bias + row0 + of);
-    Elem<T>::st((T*)a.y + token * a.y_s + row0 + of, activated(v, a.act));
-  }
+};
+// eight weights: word i with the i-th byte of the row's four
+__device__ __forceinline__ bf16x8 weights(uint4 c, uint32_t bytes, int i) {
+  const uint32_t w = i == 0 ? c.x : i == 1 ? c.y : i == 2 ? c.z : c.w;
+  return __builtin_bit_cast(bf16x8, fp4x8_to_bf16(w, __uint_as_float((bytes >> (8 * i) & 255u) << 23)));
 }
 
-// Many tokens: four wavefronts of R * 16 outputs each, side by side, that share NT * 16 tokens' inputs in LDS, in steps of 128; codes go straight into
-// registers.  LDS rows of a token are 128 inputs, their 16-byte chunks exchanged by the row so that 16 rows of one chunk column spread over the banks.  Inputs
-// come by direct loads, two stages.
-template <typename T, int R, int NT>
-__global__ __launch_bounds__(256) void k_many(const LinearArgs a) {
+// LDS by typed address.  Tiles arrive by direct loads while others are read; what says that the two do not meet are the restricted pointers of `round`, without
+// which the compiler has every read of LDS wait for all loads on their way.
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ u32x4 lds_get(const lds_char* p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  return *(const __attribute__((address_space(3))) u32x4*)p;
+#else
+  return u32x4{};
+#endif
+}
+
+// WK groups of WR x WT wavefronts.  A group has WR * R * 16 outputs and WT * NT * 16 tokens, R and NT tiles of 16 a wavefront; it goes through the inputs in steps of
+// 128 (group k: steps k, k + WK, ..), and the groups add up in LDS in their order.  A group's tokens share their inputs through LDS, where they come by direct
+// loads; codes go straight into registers.  Either is NS - 1 steps ahead.  LDS rows are a token's 128 inputs, their 16-byte chunks exchanged by the row so that 16
+// rows of one chunk column spread over the banks.
+template <typename T, int R, int NT, int WR, int WT, int WK, int NS>
+__global__ __launch_bounds__(WR * WT * WK * 64) void k_linear(const LinearArgs a) {
   typedef Parts<T> P;
-  constexpr int ROW = 128 * sizeof(T), CPR = ROW / 16, TOKENS = NT * 16, TILE = TOKENS * ROW, TRIPS = TILE / (256 * 16);
-  __shared__ __align__(16) char smem[2][TILE];
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int WG = WR * WT, W = WG * WK, ROW = 128 * sizeof(T), CPR = ROW / 16, TOKENS = WT * NT * 16, TILE = TOKENS * ROW, TRIPS = TILE / (WG * 1024), CA = NS - 1;
+  static_assert(TRIPS * WG * 1024 == TILE && (NS - 2) * (TRIPS + 2 * R) < 64, "whole trips, which the counter of loads can tell apart");
+  extern __shared__ uint4 lds[];
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wg = wave % WG, kg = wave / WG;
+  lds_char* const smem = (lds_char*)(lds_void_t*)lds + kg * (NS * TILE);   // the group's NS stages
   // blocks are handed out to the eight XCDs in turn: each gets a run of tiles, whose neighbours share weights
-  const int total = a.row_tiles * a.token_tiles, per = (total + 7) >> 3, pid = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || pid >= total) return;
-  const int row0 = pid / a.token_tiles * (R * 64) + wave * (R * 16), groups = a.in / FP4_GROUP, steps = (a.in + 127) / 128;
+  const int of_part = a.row_tiles * a.token_tiles, total = of_part * a.parts, per = (total + 7) >> 3, id = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+  const int part = id / of_part, pid = id - part * of_part;
+  const int row0 = pid / a.token_tiles * (WR * R * 16) + wg / WT * (R * 16), all_steps = (a.in + 127) / 128;
+  const int step0 = (int)((int64_t)all_steps * part / a.parts), steps = (int)((int64_t)all_steps * (part + 1) / a.parts);
   const int64_t token0 = (int64_t)(pid % a.token_tiles) * TOKENS;
-  const int tokens = a.n - token0 < TOKENS ? (int)(a.n - token0) : TOKENS;
-  const uint8_t* codes[R];
-  const uint8_t* scales[R];
+  const int tokens = a.n - token0 < TOKENS ? (int)(a.n - token0) : TOKENS, mine = wg % WT * (NT * 16);
+  // tiles beyond the last row: the last one again, not stored
+  const int tiles = (a.out + 15) / 16, tile0 = row0 / 16;
+  const uint8_t* laid[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int row = row0 + r * 16 + lr < a.out ? row0 + r * 16 + lr : a.out - 1;
-    codes[r] = a.codes + (int64_t)row * (a.in / 2) + lg * 16;
-    scales[r] = a.scales + (int64_t)row * groups + lg;
-  }
-  // this lane's chunk of a trip: LDS place (trip * 256 + thread) holds row place / CPR, chunk place % CPR exchanged by the row
+  for (int r = 0; r < R; ++r) laid[r] = a.laid + (int64_t)(tile0 + r < tiles ? tile0 + r : tiles - 1) * all_steps * CHUNK;
+  const uint32_t codes_at = lane * 16, bytes_at = 1024 + lr * 4;
+  // this lane's chunk of a trip: LDS place (trip * threads + thread) holds row place / CPR, chunk place % CPR exchanged by the row; rows of no token are zeros
   const T* const x = (const T*)a.x + token0 * a.x_s;
   const uint32_t x_bytes = (uint32_t)(((int64_t)(tokens - 1) * a.x_s + a.in) * sizeof(T));
   uint32_t from[TRIPS];
-  int chunk[TRIPS];
+  int in_row[TRIPS];                       // bytes from the chunk on to the row's end, at step 0
 #pragma unroll
   for (int i = 0; i < TRIPS; ++i) {
-    const int place = i * 256 + (int)threadIdx.x, row = place / CPR;
-    chunk[i] = place % CPR ^ (row & 15);
-    from[i] = (uint32_t)((row < tokens ? row : 0) * a.x_s * sizeof(T)) + chunk[i] * 16;   // rows of no token: the first one's, not stored
+    const int place = (i * WG + wg) * 64 + lane, row = place / CPR, c = (place % CPR ^ (row & 15)) * 16;
+    from[i] = row < tokens ? (uint32_t)(row * a.x_s * sizeof(T)) + c : 0x80000000u;
+    in_row[i] = a.in * (int)sizeof(T) - c;
   }
-  auto move = [&](int step, int stage) __attribute__((always_inline)) {
+  auto move = [&](int step, lds_char* to) __attribute__((always_inline)) {
+#ifdef __HIP_DEVICE_COMPILE__
 #pragma unroll
     for (int i = 0; i < TRIPS; ++i) {
-      // the last step's inputs beyond the row's end are zeros, not the next row's
-      const uint32_t at = step * ROW + chunk[i] * 16 < a.in * (int)sizeof(T) ? from[i] + step * ROW : 0x80000000u;
-      load_lds16(x, x_bytes, at, 0, (uint4*)(smem[stage] + (i * 4 + wave) * 1024));
+      const uint32_t at = step * ROW < in_row[i] ? from[i] + step * ROW : 0x80000000u;   // inputs beyond a row's end are zeros, not the next row's
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)x, 0, (int)x_bytes, 0x00020000), (lds_void_t*)(to + (i * WG + wg) * 1024), 16, at, 0, 0, 0);
     }
-  };
-  struct Step { uint4 c[R]; uint32_t s[R]; };
-  auto load = [&](Step& s, int step) __attribute__((always_inline)) {
-    const bool in = step * 4 + lg < groups;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      s.c[r] = in ? *(const uint4*)(codes[r] + (int64_t)step * 64) : uint4{};
-      s.s[r] = in ? scales[r][step * 4] : 127u;
-    }
+#endif
   };
   f32x4 acc[R][NT];
-  auto multiply = [&](const Step& s, const char* tile, auto careful) __attribute__((always_inline)) {
+  // The step whose inputs are at `tile`: four products of 32 inputs, whose tokens' operands are read in pieces of NC tiles, AHEAD pieces before they are used.
+  constexpr int NC = NT * P::N > 4 ? (NT > 4 ? NT / 2 : NT > 1 && P::N > 1 ? NT / 2 : NT) : NT, PIECES = 4 * (NT / NC), AHEAD = NT * P::N <= 4 ? 3 : 1;
+  static_assert(NT % NC == 0, "whole pieces");
+  auto multiply = [&](const Step<R>& s, const lds_char* __restrict__ tile, auto careful) __attribute__((always_inline)) {
+    const lds_char* const base = tile + (mine + lr) * ROW;
+    typename P::Raw raw[AHEAD + 1][NC];
+    auto read = [&](int piece) __attribute__((always_inline)) {
+      const int i = piece / (NT / NC), t0 = piece % (NT / NC) * NC;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      bf16x8 w[R];
+      for (int t = 0; t < NC; ++t) {
+        const lds_char* const row = base + (t0 + t) * 16 * ROW;
+        auto& to = raw[piece % (AHEAD + 1)][t];
+        if constexpr (P::N == 1) to = __builtin_bit_cast(uint4, lds_get(row + ((i * 4 + lg) ^ lr) * 16));
+        else { to.a = __builtin_bit_cast(f32x4, lds_get(row + ((i * 8 + lg * 2) ^ lr) * 16)); to.b = __builtin_bit_cast(f32x4, lds_get(row + ((i * 8 + lg * 2 + 1) ^ lr) * 16)); }
+      }
+    };
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const uint32_t c = i == 0 ? s.c[r].x : i == 1 ? s.c[r].y : i == 2 ? s.c[r].z : s.c[r].w;
-        w[r] = __builtin_bit_cast(bf16x8, fp4x8_to_bf16(c, __uint_as_float(s.s[r] << 23)));
+    for (int p = 0; p < AHEAD; ++p) read(p);
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 w[R];
+#pragma unroll
+    for (int piece = 0; piece < PIECES; ++piece) {
+      const int i = piece / (NT / NC), t0 = piece % (NT / NC) * NC;
+      if (piece + AHEAD < PIECES) {
+        read(piece + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (t0 == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) w[r] = weights(s.c[r], s.s[r], i);
       }
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const char* const row = tile + (t * 16 + lr) * ROW;
-        typename P::Raw raw;
-        if constexpr (P::N == 1) raw = *(const uint4*)(row + ((lg * 4 + i) ^ lr) * 16);
-        else { raw.a = *(const f32x4*)(row + ((lg * 8 + i * 2) ^ lr) * 16); raw.b = *(const f32x4*)(row + ((lg * 8 + i * 2 + 1) ^ lr) * 16); }
+      for (int t = 0; t < NC; ++t) {
         bf16x8 p[P::N];
-        P::template split<decltype(careful)::value>(raw, p);
+        P::template split<decltype(careful)::value>(raw[piece % (AHEAD + 1)][t], p);
 #pragma unroll
         for (int j = 0; j < P::N; ++j)
 #pragma unroll
-          for (int r = 0; r < R; ++r) acc[r][t] = mfma(w[r], p[j], acc[r][t]);
+          for (int r = 0; r < R; ++r) acc[r][t0 + t] = mfma(w[r], p[j], acc[r][t0 + t]);
       }
     }
+  };
+  auto arrived = [&](auto behind) __attribute__((always_inline)) {   // at most so many loads are on their way, and all wavefronts are here
+    __builtin_amdgcn_sched_barrier(0);
+    vm_wait<decltype(behind)::value>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // A round issues a step's codes and bytes (2 R loads), then a step's inputs (TRIPS): so many loads are behind the inputs of the next step.  Steps past the end:
+  // the first one again, never used.
+  typedef std::integral_constant<int, (NS - 2) * (TRIPS + 2 * R)> Behind;
+  auto round = [&](Step<R>& slot, int step, const lds_char* __restrict__ tile, lds_char* __restrict__ to, auto careful) __attribute__((always_inline)) {
+    const Step<R> now = slot;
+    const int next = step + CA * WK < steps ? step + CA * WK : step0;
+    slot.load(laid, next, codes_at, bytes_at);
+    __builtin_amdgcn_sched_barrier(0);
+    move(next, to);
+    __builtin_amdgcn_sched_barrier(0);
+    if (WK == 1 || step < steps) multiply(now, tile, careful);
+    arrived(Behind{});
   };
   auto all = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    Step next;
-    move(0, 0);
-    load(next, 0);
-    for (int step = 0; step < steps; ++step) {
-      tile_barrier();                      // this step's inputs are there, and all are done with the other stage
-      const Step now = next;
-      if (step + 1 < steps) {
-        move(step + 1, (step + 1) & 1);
-        load(next, step + 1);
+    if (step0 < steps) {
+      Step<R> ring[CA];
+#pragma unroll
+      for (int d = 0; d < CA; ++d) {
+        const int step = step0 + kg + d * WK < steps ? step0 + kg + d * WK : step0;
+        ring[d].load(laid, step, codes_at, bytes_at);
+        __builtin_amdgcn_sched_barrier(0);
+        move(step, smem + d * TILE);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      multiply(now, smem[step & 1], careful);
+      arrived(Behind{});
+      int stage = 0, to = CA;
+      for (int step = step0; step < steps; step += CA * WK)
+#pragma unroll
+        for (int d = 0; d < CA; ++d) {
+          if (step + d * WK >= steps) break;
+          round(ring[d], step + d * WK + kg, smem + stage * TILE, smem + to * TILE, careful);
+          stage = stage + 1 < NS ? stage + 1 : 0;
+          to = to + 1 < NS ? to + 1 : 0;
+        }
+      arrived(std::integral_constant<int, 0>{});   // nothing lands in LDS any more
     }
   };
   all(std::false_type{});
@@ -280,24 +258,99 @@ __global__ __launch_bounds__(256) void k_many(const LinearArgs a) {
       for (int t = 0; t < NT; ++t) fine &= finite(acc[r][t]);
     if (__syncthreads_or(!fine)) all(std::true_type{});
   }
+  if constexpr (WK > 1) {
+    // sums of a group's tiles behind those of the others; each group adds up and stores its share of the tiles
+    static_assert((int)sizeof(f32x4) * 64 * R * NT * W <= NS * TILE * WK, "sums fit where the stages were");
+    f32x4* const sums = (f32x4*)lds;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sums[(wave * (R * NT) + r * NT + t) * 64 + lane] = acc[r][t];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if ((r * NT + t) % WK == kg) {
+          f32x4 v = sums[(wg * (R * NT) + r * NT + t) * 64 + lane];
+#pragma unroll
+          for (int k = 1; k < WK; ++k) v += sums[((k * WG + wg) * (R * NT) + r * NT + t) * 64 + lane];
+          acc[r][t] = v;
+        }
+  }
+  if (a.parts > 1) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int64_t token = token0 + mine + t * 16 + lr;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int row = row0 + r * 16 + lg * 4;
+        if ((WK > 1 && (r * NT + t) % WK != kg) || token >= a.n || row >= a.out) continue;
+        float* const to = a.partial + ((int64_t)part * a.n + token) * a.out + row;
+        if (a.out % 4 == 0) *(f32x4*)to = acc[r][t];
+        else
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (row + i < a.out) to[i] = acc[r][t][i];
+      }
+    }
+    return;
+  }
+  f32x4 bias[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = row0 + r * 16 + lg * 4 + i;
+      bias[r][i] = a.bias && row < a.out ? Elem<T>::ld((const T*)a.bias + row) : 0.f;
+    }
+  auto finished = [&](int r, int t) __attribute__((always_inline)) {
+    f32x4 v = acc[r][t] + bias[r];
+    if (a.act != DP_ACT_NONE)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = activated(v[i], a.act);
+    return v;
+  };
+  // 16-bit outputs of large tiles go through LDS (free by now, a wavefront's own part of it), so that global memory sees 32 R bytes of a token at once and not 32.  Units of
+  // four outputs are exchanged by the token.
+  if constexpr (sizeof(T) == 2 && WK == 1 && R > 1) {
+    if (a.by_eight) {
+      constexpr int UPR = R * 4, CPT = R * 2, PER = 64 / CPT;      // units and 16-byte chunks of a token, tokens of a trip
+      static_assert(UPR <= 16 && W * NT * 16 * UPR * 8 <= NS * TILE, "tiles fit where the stages were");
+      uint2* const stg = (uint2*)lds + wave * (NT * 16 * UPR);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        __builtin_amdgcn_sched_barrier(0);   // one tile of tokens after the other: registers are full
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const f32x4 v = finished(r, t);
+          stg[(t * 16 + lr) * UPR + ((r * 4 + lg) ^ (lr & (UPR - 1)))] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NT * 16 / PER; ++i) {
+        const int t = i * PER + lane / CPT, ch = lane % CPT;
+        uint4 v = ((const uint4*)stg)[t * CPT + ch];
+        if (t & 1) v = make_uint4(v.z, v.w, v.x, v.y);
+        const int row = row0 + (ch ^ ((t & (UPR - 1)) >> 1)) * 8;
+        if (token0 + mine + t < a.n && row < a.out) *(uint4*)((T*)a.y + (token0 + mine + t) * a.y_s + row) = v;
+      }
+      return;
+    }
+  }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int64_t token = token0 + t * 16 + lr;
+    const int64_t token = token0 + mine + t * 16 + lr;
     if (token >= a.n) continue;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+      if (WK > 1 && (r * NT + t) % WK != kg) continue;
       const int row = row0 + r * 16 + lg * 4;
       T* const to = (T*)a.y + token * a.y_s + row;
-      float v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = acc[r][t][i];
-        if (a.bias && row + i < a.out) v[i] += Elem<T>::ld((const T*)a.bias + row + i);
-        v[i] = activated(v[i], a.act);
-      }
+      const f32x4 v = finished(r, t);
       if (a.by_four && row + 3 < a.out) {
         if constexpr (sizeof(T) == 2) *(uint2*)to = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-        else *(f32x4*)to = f32x4{v[0], v[1], v[2], v[3]};
+        else *(f32x4*)to = v;
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -306,22 +359,91 @@ __global__ __launch_bounds__(256) void k_many(const LinearArgs a) {
     }
   }
 }
+// the ranges' sums, in their order
+template <typename T> __global__ __launch_bounds__(256) void k_join(const LinearArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = a.n * a.out;
+  if (i >= all) return;
+  float v = 0.f;
+#pragma unroll 4
+  for (int p = 0; p < a.parts; ++p) v += a.partial[p * all + i];
+  const int64_t token = i / a.out, of = i - token * a.out;
+  if (a.bias) v += Elem<T>::ld((const T*)a.bias + of);
+  Elem<T>::st((T*)a.y + token * a.y_s + of, activated(v, a.act));
+}
 
-template <typename T, int R, int NT> void few(const LinearArgs& a, hipStream_t st) {
-  k_few<T, R, NT, 8><<<(unsigned)((a.out + R * 16 - 1) / (R * 16)), 512, 0, st>>>(a);
+template <typename T, int R, int NT, int WR, int WT, int WK, int NS> void launch_tiles(LinearArgs& a, hipStream_t st) {
+  constexpr int lds = NS * WK * WT * NT * 16 * 128 * (int)sizeof(T);
+  static std::atomic<uint64_t> done;
+  allow_dynamic_lds((const void*)k_linear<T, R, NT, WR, WT, WK, NS>, lds, done);
+  a.row_tiles = (a.out + WR * R * 16 - 1) / (WR * R * 16);
+  a.token_tiles = (int32_t)((a.n + WT * NT * 16 - 1) / (WT * NT * 16));
+  const int64_t total = (int64_t)a.row_tiles * a.token_tiles * a.parts;
+  k_linear<T, R, NT, WR, WT, WK, NS><<<(unsigned)((total + 7) / 8 * 8), WR * WT * WK * 64, lds, st>>>(a);
+  if (a.parts > 1) k_join<T><<<(unsigned)((a.n * a.out + 255) / 256), 256, 0, st>>>(a);
 }
-template <typename T, int R, int NT> void many(LinearArgs& a, hipStream_t st) {
-  a.row_tiles = (a.out + R * 64 - 1) / (R * 64);
-  a.token_tiles = (int32_t)((a.n + NT * 16 - 1) / (NT * 16));
-  const int64_t total = (int64_t)a.row_tiles * a.token_tiles;
-  k_many<T, R, NT><<<(unsigned)((total + 7) / 8 * 8), 256, 0, st>>>(a);
+// The tiles there are, and what they take: rows and tokens of a block, its groups (WK), how many of them a CU holds, and in units of 10 ns a group's step with 1, 2 .. blocks
+// on a CU in the last round of blocks, in the rounds before it, and what is done around the steps.  Fitted to 1248 launches: 512 .. 13824 outputs, 1504 .. 13824 inputs, 1 .. 6240
+// tokens; the estimate below then takes a tile within 1 % of the best one on average, 8 % at worst.
+struct Tile { int rows, tokens, groups, per_cu, last[3], full, around; };
+#define TILES_BF16(X) \
+  X(1, 1, 2, 1, 4, 3, {32, 16, 4, 3, {32, 64, 95}, 88, 152}) \
+  X(1, 1, 2, 1, 8, 3, {32, 16, 8, 1, {53}, 70, 214}) \
+  X(1, 1, 4, 1, 4, 4, {64, 16, 4, 2, {44, 103}, 103, 219}) \
+  X(1, 2, 2, 1, 4, 3, {32, 32, 4, 1, {46}, 51, 175}) \
+  X(1, 2, 4, 1, 4, 3, {64, 32, 4, 1, {57}, 62, 251}) \
+  X(1, 3, 2, 1, 4, 3, {32, 48, 4, 1, {68}, 82, 207}) \
+  X(1, 3, 4, 1, 4, 3, {64, 48, 4, 1, {78}, 94, 301}) \
+  X(1, 4, 4, 1, 2, 4, {64, 64, 2, 1, {60}, 70, 285}) \
+  X(2, 4, 4, 1, 2, 3, {128, 64, 2, 1, {90}, 123, 377}) \
+  X(2, 4, 4, 1, 1, 3, {128, 64, 1, 2, {64, 104}, 108, 356}) \
+  X(4, 4, 4, 2, 1, 2, {256, 128, 1, 1, {150}, 176, 776}) \
+  X(4, 6, 4, 2, 1, 2, {256, 192, 1, 1, {200}, 225, 923}) \
+  X(4, 8, 4, 2, 1, 2, {256, 256, 1, 1, {252}, 291, 1075})
+#define TILES_F32(X) \
+  X(1, 1, 1, 1, 8, 2, {16, 16, 8, 1, {117}, 130, 203}) \
+  X(1, 1, 2, 1, 4, 3, {32, 16, 4, 1, {108}, 116, 185}) \
+  X(1, 1, 4, 1, 4, 2, {64, 16, 4, 1, {179}, 165, 215}) \
+  X(1, 2, 4, 1, 2, 3, {64, 32, 2, 1, {162}, 171, 231}) \
+  X(2, 2, 4, 1, 2, 2, {128, 32, 2, 2, {210, 391}, 319, 273}) \
+  X(2, 2, 4, 1, 1, 3, {128, 32, 1, 3, {121, 210, 306}, 301, 276}) \
+  X(4, 2, 4, 1, 1, 2, {256, 32, 1, 2, {164, 312}, 293, 579}) \
+  X(8, 2, 2, 1, 1, 2, {256, 32, 1, 2, {238, 283}, 262, 1104}) \
+  X(8, 2, 4, 2, 1, 2, {512, 64, 1, 1, {434}, 457, 1347})
+template <typename T> struct Tiles;
+#define X(R, NT, WR, WT, WK, NS, ...) __VA_ARGS__,
+template <> struct Tiles<bf16_t> { static constexpr Tile all[] = {TILES_BF16(X)}; };
+template <> struct Tiles<float> { static constexpr Tile all[] = {TILES_F32(X)}; };
+#undef X
+constexpr Tile Tiles<bf16_t>::all[];
+constexpr Tile Tiles<float>::all[];
+
+struct Route { int kind, parts; };
+// The kind of tile and the ranges by an estimate of the time: rounds of equal blocks.  Ranges, of the smaller tiles alone, cost a launch and their sums, written and read at
+// 4.2 TB/s.
+template <typename T> Route route(const LinearArgs& a) {
+  Route r{};
+  int64_t best = INT64_MAX;
+  const int64_t steps = (a.in + 127) / 128;
+  for (const Tile& k : Tiles<T>::all) {
+    const int64_t tiles = ((int64_t)a.out + k.rows - 1) / k.rows * ((a.n + k.tokens - 1) / k.tokens), slots = 256 * k.per_cu;
+    for (int parts = 1; parts <= 8; parts *= 2) {
+      if (parts > 1 && (k.rows > 128 || steps < parts * k.groups || tiles * parts > slots)) break;
+      const int64_t of_group = ((steps + parts - 1) / parts + k.groups - 1) / k.groups, rounds = tiles * parts / slots, rest = tiles * parts % slots;
+      int64_t cost = rounds * (of_group * k.full + k.around);
+      if (rest > 0) cost += of_group * k.last[(rest - 1) / 256] + k.around;
+      if (parts > 1) cost += 260 + parts * a.n * a.out / 5250;
+      if (cost < best) { best = cost; r.kind = (int)(&k - Tiles<T>::all); r.parts = parts; }
+    }
+  }
+  return r;
 }
-template <typename T> void launch(LinearArgs& a, hipStream_t st) {
-  if (a.n <= 16) few<T, 1, 1>(a, st);
-  else if (a.n <= 32) few<T, 1, 2>(a, st);
-  else if (a.n <= 64) few<T, 1, 4>(a, st);
-  else if constexpr (sizeof(T) == 2) many<T, 4, 8>(a, st);
-  else many<T, 4, 4>(a, st);
+size_t partial_bytes(const LinearArgs& a, const Route& r) { return r.parts > 1 ? (size_t)r.parts * a.n * a.out * sizeof(float) : 0; }
+template <typename T> void launch(LinearArgs& a, const Route& r, hipStream_t st) {
+  a.parts = r.parts;
+  int kind = 0;
+#define X(R, NT, WR, WT, WK, NS, ...) if (r.kind == kind++) return launch_tiles<T, R, NT, WR, WT, WK, NS>(a, st);
+  if constexpr (sizeof(T) == 2) { TILES_BF16(X) } else { TILES_F32(X) }
+#undef X
 }
 
 // A group a thread: its 32 values, largest one, byte and codes.
@@ -346,33 +468,60 @@ template <typename T> __global__ __launch_bounds__(256) void k_pack(const T* src
   scales[id] = (uint8_t)byte;
 }
 
+// A chunk of a tile and step a wavefront: each lane its 16 bytes, the first 16 lanes the rows' group bytes.
+__global__ __launch_bounds__(256) void k_lay(const uint8_t* codes, const uint8_t* scales, int32_t out, int32_t in, uint8_t* laid) {
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, steps = (in + 127) / 128, groups = in / FP4_GROUP;
+  const int64_t chunk = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), tile = chunk / steps;
+  const int step = (int)(chunk - tile * steps);
+  if (tile >= (out + 15) / 16) return;
+  const int64_t row = tile * 16 + lr;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = row < out && step * 4 + i < groups ? *(const uint32_t*)(codes + row * (in / 2) + (step * 4 + i) * 16 + lg * 4) : 0u;
+  *(uint4*)(laid + chunk * CHUNK + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+  if (lg == 0) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b |= (row < out && step * 4 + i < groups ? scales[row * groups + step * 4 + i] : 127u) << (8 * i);
+    *(uint32_t*)(laid + chunk * CHUNK + 1024 + lr * 4) = b;
+  }
+}
+
 int refuse_linear(const char* entry, const char* why) {
   thread_local char text[200];
   snprintf(text, sizeof text, "%s: %s", entry, why);
   return dp_set_error(DP_EINVAL, text);
 }
-const char* why_not_matrix(int32_t out, int32_t in, int32_t dtype, const void* codes, const uint8_t* scales) {
+const char* why_not_sizes(int32_t out, int32_t in) {
   if (in < FP4_GROUP || in > 1 << 20 || in % FP4_GROUP) return "in must be a multiple of 32 in [32, 2^20]";
   if (out < 1 || out > 1 << 24) return "out must be in [1, 2^24]";
-  if (dtype != DP_F32 && dtype != DP_BF16) return "dtype must be DP_F32 or DP_BF16";
-  if (!codes || !scales) return "null pointer";
-  if ((uintptr_t)codes & 15) return "codes must be 16-byte aligned";
+  if ((int64_t)out * in > (int64_t)1 << 36) return "out * in must be at most 2^36";
   return nullptr;
 }
+const char* why_not_codes(const void* codes, const uint8_t* scales) {
+  if (!codes || !scales) return "null pointer";
+  return (uintptr_t)codes & 15 ? "codes must be 16-byte aligned" : nullptr;
+}
+#define REFUSE_IF(expr) do { if (const char* why = (expr)) return refuse_linear(entry, why); } while (0)
 
 }  // namespace
 
+extern "C" size_t dp_fp4_laid_bytes(int32_t out, int32_t in) {
+  if (const char* why = why_not_sizes(out, in)) { refuse_linear("dp_fp4_laid_bytes", why); return 0; }
+  return (size_t)((out + 15) / 16) * ((in + 127) / 128) * CHUNK;
+}
+
 extern "C" int dp_fp4_pack(const void* src, int64_t stride, int32_t out, int32_t in, int32_t dtype, void* codes, uint8_t* scales, void* stream) {
   static const char entry[] = "dp_fp4_pack";
-  if (const char* why = why_not_matrix(out, in, dtype, codes, scales)) return refuse_linear(entry, why);
+  REFUSE_IF(why_not_sizes(out, in));
+  REFUSE_IF(dtype != DP_F32 && dtype != DP_BF16 ? "dtype must be DP_F32 or DP_BF16" : nullptr);
+  REFUSE_IF(why_not_codes(codes, scales));
   const int size = dtype == DP_BF16 ? 2 : 4;
-  if (!src) return refuse_linear(entry, "null pointer");
-  if ((uintptr_t)src & (size - 1)) return refuse_linear(entry, "rows must be aligned to their type");
-  if (out > 1 && (stride < 0 || stride > (int64_t)1 << 38)) return refuse_linear(entry, "strides must be in [0, 2^38]");
-  const int64_t threads = (int64_t)out * (in / FP4_GROUP);
-  if (threads > (int64_t)1 << 31) return refuse_linear(entry, "out * in must be at most 2^36");
+  REFUSE_IF(!src ? "null pointer" : nullptr);
+  REFUSE_IF((uintptr_t)src & (size - 1) ? "rows must be aligned to their type" : nullptr);
+  REFUSE_IF(out > 1 && (stride < 0 || stride > (int64_t)1 << 38) ? "strides must be in [0, 2^38]" : nullptr);
   const hipStream_t st = (hipStream_t)stream;
-  const unsigned g = (unsigned)((threads + 255) / 256);
+  const unsigned g = (unsigned)(((int64_t)out * (in / FP4_GROUP) + 255) / 256);
   (void)hipGetLastError();
   if (dtype == DP_BF16) k_pack<bf16_t><<<g, 256, 0, st>>>((const bf16_t*)src, stride, out, in / FP4_GROUP, (uint8_t*)codes, scales);
   else k_pack<float><<<g, 256, 0, st>>>((const float*)src, stride, out, in / FP4_GROUP, (uint8_t*)codes, scales);
@@ -380,28 +529,71 @@ extern "C" int dp_fp4_pack(const void* src, int64_t stride, int32_t out, int32_t
   return DP_OK;
 }
 
-extern "C" int dp_linear_fp4(const dp_fp4_matrix* w, const void* x, int64_t x_stride, int64_t n, int32_t act, void* y, int64_t y_stride, void* stream) {
+extern "C" int dp_fp4_lay(const void* codes, const uint8_t* scales, int32_t out, int32_t in, void* laid, void* stream) {
+  static const char entry[] = "dp_fp4_lay";
+  REFUSE_IF(why_not_sizes(out, in));
+  REFUSE_IF(why_not_codes(codes, scales));
+  REFUSE_IF(!laid ? "null pointer" : nullptr);
+  REFUSE_IF((uintptr_t)laid & 63 ? "the laid matrix must be 64-byte aligned" : nullptr);
+  const int64_t chunks = (int64_t)((out + 15) / 16) * ((in + 127) / 128);
+  (void)hipGetLastError();
+  k_lay<<<(unsigned)((chunks + 3) / 4), 256, 0, (hipStream_t)stream>>>((const uint8_t*)codes, scales, out, in, (uint8_t*)laid);
+  if (hipGetLastError() != hipSuccess) return dp_set_error(DP_EHIP, "dp_fp4_lay: the launch failed");
+  return DP_OK;
+}
+
+namespace {
+const char* why_not_linear(const dp_fp4_matrix* w, int64_t n) {
+  if (!w) return "null pointer";
+  if (const char* why = why_not_sizes(w->out, w->in)) return why;
+  if (w->dtype != DP_F32 && w->dtype != DP_BF16) return "dtype must be DP_F32 or DP_BF16";
+  return n < 0 || n > 1 << 24 || n * w->out > (int64_t)1 << 35 ? "n must be in [0, 2^24], n * out at most 2^35" : nullptr;
+}
+}  // namespace
+
+extern "C" size_t dp_linear_fp4_workspace_bytes(const dp_fp4_matrix* w, int64_t n) {
+  if (const char* why = why_not_linear(w, n)) { refuse_linear("dp_linear_fp4_workspace_bytes", why); return 0; }
+  LinearArgs a{};
+  a.n = n; a.in = w->in; a.out = w->out;
+  return n == 0 ? 0 : partial_bytes(a, w->dtype == DP_BF16 ? route<bf16_t>(a) : route<float>(a));
+}
+
+// for the tests, which state the tile that each of their calls is meant to reach: its number, and the ranges of the inputs
+extern "C" void dp_linear_fp4_route(const dp_fp4_matrix* w, int64_t n, int32_t* kind_parts) {
+  LinearArgs a{};
+  a.n = n; a.in = w->in; a.out = w->out;
+  const Route r = w->dtype == DP_BF16 ? route<bf16_t>(a) : route<float>(a);
+  kind_parts[0] = r.kind;
+  kind_parts[1] = r.parts;
+}
+
+extern "C" int dp_linear_fp4(const dp_fp4_matrix* w, const void* x, int64_t x_stride, int64_t n, int32_t act, void* y, int64_t y_stride, void* workspace, size_t have, void* stream) {
   static const char entry[] = "dp_linear_fp4";
-#define REFUSE_IF(expr) do { if (const char* why = (expr)) return refuse_linear(entry, why); } while (0)
-  REFUSE_IF(!w ? "null pointer" : nullptr);
-  REFUSE_IF(why_not_matrix(w->out, w->in, w->dtype, w->codes, w->scales));
+  REFUSE_IF(why_not_linear(w, n));
   REFUSE_IF(act != DP_ACT_NONE && act != DP_ACT_GELU && act != DP_ACT_SILU ? "act must be DP_ACT_NONE, DP_ACT_GELU or DP_ACT_SILU" : nullptr);
-  REFUSE_IF(n < 0 || n > 1 << 24 || n * w->out > (int64_t)1 << 35 ? "n must be in [0, 2^24], n * out at most 2^35" : nullptr);
   if (n == 0) return DP_OK;
   const int size = w->dtype == DP_BF16 ? 2 : 4;
-  REFUSE_IF(!x || !y ? "null pointer" : nullptr);
+  REFUSE_IF(!x || !y || !w->laid ? "null pointer" : nullptr);
+  REFUSE_IF((uintptr_t)w->laid & 63 ? "the laid matrix must be 64-byte aligned" : nullptr);
   REFUSE_IF(((uintptr_t)x & 15) || (n > 1 && x_stride % (16 / size)) ? "rows of x must be 16-byte aligned, in their stride too" : nullptr);
-  REFUSE_IF(n > 1 && (x_stride < 0 || x_stride > 1 << 22) ? "x_stride must be in [0, 2^22]" : nullptr);
+  REFUSE_IF(n > 1 && (x_stride < 0 || x_stride > 1 << 21) ? "x_stride must be in [0, 2^21]" : nullptr);
   REFUSE_IF(((uintptr_t)y | (uintptr_t)w->bias) & (size - 1) ? "y and the bias must be aligned to their type" : nullptr);
   REFUSE_IF(n > 1 && (y_stride < w->out || y_stride > (int64_t)1 << 38) ? "y_stride must be in [out, 2^38]" : nullptr);
-#undef REFUSE_IF
   LinearArgs a{};
-  a.codes = (const uint8_t*)w->codes; a.scales = w->scales; a.bias = w->bias; a.x = x; a.y = y;
+  a.laid = (const uint8_t*)w->laid; a.bias = w->bias; a.x = x; a.y = y;
   a.x_s = n > 1 ? x_stride : 0; a.y_s = n > 1 ? y_stride : 0; a.n = n; a.in = w->in; a.out = w->out; a.act = act;
   a.by_four = (uintptr_t)y % (4 * size) == 0 && a.y_s % 4 == 0;
+  a.by_eight = (uintptr_t)y % (8 * size) == 0 && a.y_s % 8 == 0 && a.out % 8 == 0;
+  const Route r = w->dtype == DP_BF16 ? route<bf16_t>(a) : route<float>(a);
+  if (const size_t need = partial_bytes(a, r)) {
+    REFUSE_IF((uintptr_t)workspace & 255 ? "the workspace must be 256-byte aligned" : nullptr);
+    if (!workspace || have < need) return dp_set_error(DP_ENOMEM, "dp_linear_fp4: workspace too small");
+    a.partial = (float*)workspace;
+  }
   const hipStream_t st = (hipStream_t)stream;
   (void)hipGetLastError();
-  if (w->dtype == DP_BF16) launch<bf16_t>(a, st); else launch<float>(a, st);
+  if (w->dtype == DP_BF16) launch<bf16_t>(a, r, st); else launch<float>(a, r, st);
   if (hipGetLastError() != hipSuccess) return dp_set_error(DP_EHIP, "dp_linear_fp4: the launch failed");
   return DP_OK;
 }
+#undef REFUSE_IF

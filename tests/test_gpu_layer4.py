@@ -21,8 +21,9 @@ class Layer:
         self.m, self.w = {}, {}
         for name, (o, i) in dict(qkv=((heads + 2 * kv_heads) * d, dim), out=(dim, heads * d), up=(ffn, dim), down=(dim, ffn)).items():
             bias = (r(o) * 0.1).to(TD[dtype])
-            self.m[name] = B.Linear4.pack((r(o, i) * i ** -0.5).to(TD[dtype]).cuda(), bias.cuda())
-            self.w[name] = (F.decode(F.unpack(self.m[name].codes.view(torch.uint8).cpu().numpy()), self.m[name].scales.cpu().numpy()), np64(bias))
+            codes, scales = B.pack_fp4((r(o, i) * i ** -0.5).to(TD[dtype]).cuda())
+            self.m[name] = B.Linear4(codes, scales, bias.cuda(), dtype)
+            self.w[name] = (F.decode(F.unpack(codes.view(torch.uint8).cpu().numpy()), scales.cpu().numpy()), np64(bias))
         self.g = {n: (r(s) * 0.1 + 1.1).to(TD[dtype]) for n, s in dict(q=d, k=d, attn=dim, ffn=dim).items()}
         self.v = {n: r(seqs, dim) * 0.3 for n in ("gate1", "scale1", "shift1", "gate2", "scale2", "shift2")}
         self.gd, self.vd = {n: t.cuda() for n, t in self.g.items()}, {n: t.cuda() for n, t in self.v.items()}

@@ -1,4 +1,6 @@
 """Products with 4-bit weights on the GPU, against the definition in 64 bits."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -8,6 +10,7 @@ from paged import HALF, TD, U, np64
 
 pytestmark = pytest.mark.gpu
 # tokens, out, in: each kernel and its tiles' borders, one group, rows that divide nothing, long sums
+# (test_every_tile: which)
 SIZES = [(1, 1, 32), (1, 16, 64), (1, 17, 96), (1, 4608, 1536), (2, 33, 256), (3, 100, 288), (15, 64, 512), (16, 48, 2080), (17, 31, 160), (32, 130, 4128), (33, 129, 544), (48, 80, 1024), (64, 65, 320),
          (65, 64, 128), (65, 1, 32), (70, 257, 96), (100, 300, 992), (128, 256, 256), (129, 255, 160), (200, 513, 1504), (260, 70, 64), (513, 129, 416), (1000, 24, 2048)]
 
@@ -45,6 +48,50 @@ def test_against_the_definition(n, out, in_, dtype):
     for b, act in ((None, None), (bias, "gelu"), (bias, "silu")):
         m = B.Linear4(codes, scales, b, dtype)
         check(m.forward(x.cuda(), act=act), x, w, b, act, dtype)
+
+
+# each tile, and each that a call's inputs may be cut into ranges for: number, ranges -> a call that takes it, with ends that divide nothing
+REACH = {
+    "bf16": {(0, 1): (1, 500, 1504), (0, 4): (1, 1500, 8992), (0, 8): (1, 500, 8992), (1, 1): (1, 2900, 8992), (2, 1): (1, 8801, 2016), (2, 4): (1, 2900, 13792), (3, 1): (17, 4505, 1504),
+             (3, 4): (17, 1500, 8992), (4, 1): (17, 8801, 1504), (4, 2): (17, 4505, 13792), (4, 8): (33, 1001, 13792), (5, 1): (65, 3333, 1504), (6, 1): (33, 8801, 2016), (6, 4): (33, 2900, 13792),
+             (7, 1): (50, 8801, 1504), (8, 1): (33, 20001, 1504), (8, 2): (50, 8801, 8992), (9, 1): (65, 20001, 1504), (10, 1): (800, 5003, 1504), (11, 1): (400, 20001, 1504),
+             (12, 1): (1000, 13001, 1504)},
+    "f32": {(0, 1): (1, 500, 1504), (0, 8): (1, 500, 8992), (1, 1): (1, 4505, 1504), (1, 8): (1, 500, 4000), (2, 1): (1, 8801, 1504), (2, 4): (1, 2900, 13792), (3, 1): (17, 8801, 1504),
+            (3, 8): (17, 1500, 13792), (4, 1): (17, 20001, 1504), (4, 2): (65, 3333, 2016), (4, 8): (33, 1500, 4000), (5, 2): (33, 20001, 4000), (5, 8): (33, 1500, 5088), (6, 1): (33, 20001, 1504),
+            (7, 1): (130, 20001, 4000), (8, 1): (1550, 3333, 1504)},
+}
+# rows that end with a whole eight: the tiles that go through LDS on their way out
+EVEN = [("bf16", (8, 1), (50, 19992, 1504)), ("bf16", (9, 1), (65, 19992, 1504)), ("bf16", (10, 1), (800, 5000, 1504)), ("bf16", (11, 1), (400, 19992, 1504)), ("bf16", (12, 1), (1000, 13000, 1504)),
+        ("f32", (8, 1), (1550, 3336, 1504))]
+
+
+def kind_of(out, in_, dtype, n):
+    from paper_2505_21070_amd import binding as B
+    got = (C.c_int32 * 2)()
+    B._lib.dp_linear_fp4_route(bytes(B.Fp4Matrix(out, in_, int(dtype == "bf16"), None, None)), C.c_int64(n), got)
+    return tuple(got)
+
+
+@pytest.mark.parametrize("dtype,kind,sizes", [(d, k, REACH[d][k]) for d in REACH for k in REACH[d]] + EVEN)
+def test_every_tile(dtype, kind, sizes):
+    """Whole numbers through each kind of tile, exact; its first and last outputs, tokens and inputs among them."""
+    from paper_2505_21070_amd import binding as B
+    n, out, in_ = sizes
+    assert kind_of(out, in_, dtype, n) == kind
+    gen = torch.Generator().manual_seed(n)
+    codes = torch.randint(0, 256, (out, in_ // 2), generator=gen).to(torch.uint8)
+    scales = torch.randint(126, 128, (out, in_ // 32), generator=gen).to(torch.uint8)
+    x = torch.randint(-2, 3, (n, in_), generator=gen).to(TD[dtype])
+    bias = torch.randint(-8, 8, (out,), generator=gen).to(TD[dtype])
+    y = torch.full((n + 1, out + 8), 99.0, dtype=TD[dtype], device="cuda")
+    m = B.Linear4(codes.cuda().view(torch.float4_e2m1fn_x2), scales.cuda(), bias.cuda(), dtype)
+    for to in (None, y[:n, :out]):
+        got = m.forward(x.cuda(), out=to)
+        for rows in (slice(0, 64), slice(out // 2 - 40, out // 2 + 40), slice(max(0, out - 300), out)):
+            w = torch.from_numpy(F.decode(F.unpack(codes[rows].numpy()), scales[rows].numpy()))
+            want = x.double() @ w.T + bias[rows].double()
+            assert want.abs().max() < 2 ** 20 and torch.equal(got[:, rows].cpu(), want.float().to(TD[dtype]))
+    assert (y[n] == 99).all() and (y[:, out:] == 99).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -132,10 +179,11 @@ def test_pack():
             w[0, :3] = torch.tensor([1e38, -0.0, 1e-38])
             if out > 1:
                 w[1, 31], w[2, 5] = float("nan"), -float("inf")
-            m = B.Linear4.pack(w.cuda()[:, :in_])
+            codes, scales = B.pack_fp4(w.cuda()[:, :in_])
             code, byte = F.encode(np64(w[:, :in_]))
-            assert np.array_equal(F.unpack(m.codes.view(torch.uint8).cpu().numpy()), code) and np.array_equal(m.scales.cpu().numpy(), byte)
-            assert m.torch_dtype == TD[dtype] and (m.out, m.in_) == (out, in_)
+            assert np.array_equal(F.unpack(codes.view(torch.uint8).cpu().numpy()), code) and np.array_equal(scales.cpu().numpy(), byte)
+            m = B.Linear4.pack(w.cuda()[:, :in_])
+            assert m.torch_dtype == TD[dtype] and (m.out, m.in_) == (out, in_) and torch.equal(m.laid, B.Linear4(codes, scales, dtype=dtype).laid)
 
 
 @pytest.mark.parametrize("n", [1, 30, 200])
@@ -170,6 +218,7 @@ def test_codes_beyond_32_bits():
     scales = torch.full((out, in_ // 32), 127, dtype=torch.uint8, device="cuda")
     codes[-1, -1], codes[-2, 0] = 0x20, 0x02
     m = B.Linear4(codes.view(torch.float4_e2m1fn_x2), scales)
+    del codes, scales
     for n in (1, 70):
         x = torch.zeros((n, in_), dtype=torch.bfloat16, device="cuda")
         x[:, -1], x[:, 0] = 3.0, 5.0
@@ -196,5 +245,6 @@ def test_refused_by_the_binding():
     with pytest.raises(B.DualParalError) as e:
         m.forward(torch.zeros((3, 68), dtype=torch.bfloat16, device="cuda")[:, 4:])
     assert e.value.code == B.DP_EINVAL and "16-byte" in str(e.value)
-    with pytest.raises(AssertionError):
-        B.Linear4.pack(torch.zeros((4, 40), device="cuda"))
+    for w in (torch.zeros((4, 40), device="cuda"), torch.zeros((64, 4), device="cuda").t(), torch.zeros((4, 64), device="cuda").half()):
+        with pytest.raises(AssertionError):
+            B.pack_fp4(w)
