@@ -515,7 +515,7 @@ inline size_t partial_bytes(const PagedArgs& a, const Route& r, int head_dim) {
 inline size_t workspace_bytes(const PagedArgs& a, const Route& r, int head_dim) {
   return partial_bytes(a, r, head_dim) + (r.runs ? ((size_t)r.tiles + 1) * sizeof(int32_t) : 0);
 }
-Route route_attn_paged_bf16(const PagedArgs& a, int head_dim);
+Route route_attn_paged_bf16(const PagedArgs& a, int head_dim, int format);
 Route route_attn_paged_f32(const PagedArgs& a, int head_dim);
 void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, int format, hipStream_t st);
 void launch_attn_paged_f32(const PagedArgs& a, const Route& r, int head_dim, int format, hipStream_t st);

@@ -44,13 +44,13 @@ extern "C" size_t dp_attn_paged_workspace_bytes(const dp_kv_cache* c, const dp_a
   if (why) { refuse("dp_attn_paged_workspace_bytes", why); return 0; }
   if (n_tokens == 0 || cfg->n_seqs == 0 || cfg->max_q == 0) return 0;
   const PagedArgs a = arguments(c, cfg, n_tokens);
-  return workspace_bytes(a, c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim) : route_attn_paged_f32(a, c->head_dim), c->head_dim);
+  return workspace_bytes(a, c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim, c->format) : route_attn_paged_f32(a, c->head_dim), c->head_dim);
 }
 
 // for the tests, which state the kind of block that each of their calls is meant to reach: its rows, the ranges of the keys and the keys of one, the runs of a plan
 extern "C" void dp_attn_paged_route(const dp_kv_cache* c, const dp_attn_config* cfg, int64_t n_tokens, int32_t* qb_parts_keys_runs) {
   const PagedArgs a = arguments(c, cfg, n_tokens);
-  const Route r = c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim) : route_attn_paged_f32(a, c->head_dim);
+  const Route r = c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim, c->format) : route_attn_paged_f32(a, c->head_dim);
   const int32_t v[4] = {r.qb, r.parts, r.part_keys, r.runs};
   for (int i = 0; i < 4; ++i) qb_parts_keys_runs[i] = v[i];
 }
@@ -70,7 +70,7 @@ extern "C" int dp_attn_paged(const dp_kv_cache* c, const dp_attn_config* cfg, co
   a.q_ts = q->token_stride; a.q_hs = q->head_stride; a.o_ts = out->token_stride; a.o_hs = out->head_stride;
   a.q_start = q_start; a.kv_len = kv_len; a.table = page_table;
   const hipStream_t st = (hipStream_t)stream;
-  const Route r = c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim) : route_attn_paged_f32(a, c->head_dim);
+  const Route r = c->dtype == DP_BF16 ? route_attn_paged_bf16(a, c->head_dim, c->format) : route_attn_paged_f32(a, c->head_dim);
   a.tiles = (int32_t)r.tiles; a.tiles_of_seq = (int32_t)r.tiles_of_seq; a.parts = r.parts; a.part_keys = r.part_keys; a.runs = r.runs;
   if (const size_t need = workspace_bytes(a, r, c->head_dim)) {
     REFUSE_IF((uintptr_t)workspace & 255 ? "the workspace must be 256-byte aligned" : nullptr);

@@ -220,7 +220,7 @@ __device__ __forceinline__ bool sum_tile(const PagedArgs& a, const Block& b, uin
     if (KEEP && __any(alpha == 0.f)) {
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) o[d][t] = lowered(o[d][t], alpha);
-    } else {
+    } else if (!__all(alpha == 1.f)) {                       // most tiles raise no row's reference
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) o[d][t] *= alpha;
     }
@@ -270,14 +270,41 @@ __device__ __forceinline__ void score_tile(uint32_t ktile, const bf16x8 (&qf)[NT
   }
 }
 
-template <int HD, int NT>
+// Codes of 4 bits of 32 keys straight from the pages into operands: a lane takes a quarter of a key's row, whole groups or half of one, as it lies there, and the
+// channels of its quarter in the products' order, 8 in each: which channels meet in a product is free, as long as the queries' are the same ones (SPREAD).
+template <int HD> struct KeyCodes {
+  static constexpr int ROW = HD / 2;         // bytes of a row in the pages
+  typedef typename std::conditional<HD == 128, u32x4, u32x2>::type Raw;
+  Raw raw[2];
+  uint32_t byte[2];
+  __device__ __forceinline__ void load(const PagedArgs& a, const int64_t (&at)[2], int lane) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      raw[kt] = *(const Raw*)((const char*)a.data + at[kt] * ROW + (lane & 15) * ROW + (lane >> 4) * (ROW / 4));
+      byte[kt] = (a.scales + at[kt] * (HD / FP4_GROUP))[(lane & 15) * (HD / FP4_GROUP) + (lane >> 4) * (HD / 4) / FP4_GROUP];
+    }
+  }
+  template <int NT> __device__ __forceinline__ void score(const bf16x8 (&qf)[NT][HD / 32], f32x4 (&sc)[NT][2]) const {
+#pragma unroll
+    for (int ks = 0; ks < HD / 32; ++ks)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const bf16x8 k = __builtin_bit_cast(bf16x8, fp4x8_to_bf16(raw[kt][ks], __uint_as_float(byte[kt] << 23)));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sc[t][kt] = mfma(k, qf[t][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[t][kt]);
+      }
+  }
+};
+
+// SPREAD: lane group g has channels g * (HD / 4) .., as KeyCodes
+template <int HD, int NT, bool SPREAD = false>
 __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b, int row0, bf16x8 (&qf)[NT][HD / 32], int (&end)[NT], int lane) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = row0 + t * 16 + (lane & 15);
-    const bf16_t* const q = (const bf16_t*)a.q + row_at(a, b, row < b.rows ? row : b.rows - 1, a.q_ts, a.q_hs) + (lane >> 4) * 8;
+    const bf16_t* const q = (const bf16_t*)a.q + row_at(a, b, row < b.rows ? row : b.rows - 1, a.q_ts, a.q_hs) + (lane >> 4) * (SPREAD ? HD / 4 : 8);
 #pragma unroll
-    for (int ks = 0; ks < HD / 32; ++ks) qf[t][ks] = __builtin_bit_cast(bf16x8, *(const uint4*)(q + ks * 32));
+    for (int ks = 0; ks < HD / 32; ++ks) qf[t][ks] = __builtin_bit_cast(bf16x8, *(const uint4*)(q + ks * (SPREAD ? 8 : 32)));
     end[t] = row_end(a, b, row);
   }
 }
@@ -286,13 +313,17 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
 // LDS, the next tile on its way in registers; nobody waits for anybody until the results are joined in LDS, in wavefront order.  W = 4: two blocks to a
 // CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory: 64 sequences of 16 .. 16000 keys, 8 heads of 128 in 8 bits, 201 us, 5.3 TB/s.  W = 8: no more
 // blocks than CUs, bound by a trip's chain of steps, 1.6 us for 256 keys: one token over 517 keys with 12 heads 10.3 us.
+// blocks of four wavefronts to a CU
+constexpr int few_per_cu(int head_dim, int nt, int format) { return format == DP_KV_FP4 && nt == 1 ? (head_dim == 64 ? 4 : 3) : 2; }
 template <int HD, int NT, int W, int FORMAT, bool PLAN>
-__global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
-  constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR;
-  __shared__ uint4 smem[W * 2 * TILE];
+__global__ __launch_bounds__(W * 64, (W == 4 ? few_per_cu(HD, NT, FORMAT) : 2)) void k_paged_few(const PagedArgs a) {
+  constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR, JOIN = (W * 16 * (2 + HD + 4) * 4 + 15) / 16;
+  constexpr bool DIRECT = FORMAT == DP_KV_FP4;               // keys do not go through LDS
+  constexpr int TILES = W * (DIRECT ? 1 : 2) * TILE;
+  __shared__ uint4 smem[TILES > JOIN ? TILES : JOIN];
   static_assert(sizeof(smem) >= sizeof(float) * W * 16 * (2 + HD + 4), "join_waves");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t kt = lds_address(smem) + wave * 2 * TILE * 16, vt = kt + TILE * 16;
+  const uint32_t kt = lds_address(smem) + wave * (DIRECT ? 1 : 2) * TILE * 16, vt = DIRECT ? kt : kt + TILE * 16;
   const int64_t to_values = (int64_t)a.hk << a.page_shift;
   Walk<QB, 128, PLAN> walk(a, blockIdx.x);
   Piece p;
@@ -303,7 +334,7 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
     const Block& b = p.b;
     bf16x8 qf[NT][HD / 32];
     int end[NT];
-    load_queries<HD, NT>(a, b, b.first, qf, end, lane);
+    load_queries<HD, NT, DIRECT>(a, b, b.first, qf, end, lane);
     Soft z[NT];
     f32x4 o[HD / 16][NT];
     auto clear = [&]() __attribute__((always_inline)) {
@@ -315,38 +346,48 @@ __global__ __launch_bounds__(W * 64, 2) void k_paged_few(const PagedArgs a) {
       }
     };
     clear();
-    Carry<HD, 32, 1, FORMAT> ck, cv;
+    typedef Carry<HD, 32, 1, FORMAT> Tile;
+    typename std::conditional<DIRECT, KeyCodes<HD>, Tile>::type ck;
+    Tile cv;
     int key = p.k0 + wave * 32;
-    auto load = [&](int at) __attribute__((always_inline)) {
-      const auto rows = ck.rows(a, b, at, 0);
-      ck.load(a, rows, 0, 0, lane);
+    auto load = [&](int at, int lane) __attribute__((always_inline)) {
+      const auto rows = Tile::rows(a, b, at, 0);
+      if constexpr (DIRECT) {
+        static_assert(sizeof(rows.at) == 16, "two groups of 16 keys");
+        ck.load(a, rows.at, lane);
+      } else {
+        ck.load(a, rows, 0, 0, lane);
+      }
       cv.load(a, rows, to_values, 0, lane);
     };
-    if (key < p.k1) load(key);
+    if (key < p.k1) load(key, lane);
     const bool gaps = __builtin_amdgcn_readfirstlane((int)pages_missing(a, b, p.k0, p.k1));
-    auto tile = [&](auto careful, int lane) __attribute__((always_inline)) {
+    // the tile in the registers; `next` sends the one after it on its way
+    auto tile = [&](auto careful, int lane, auto&& next) __attribute__((always_inline)) {
       f32x4 sc[NT][KT];
-      score_tile<HD, KT, NT>(kt, qf, sc, lane);
+      if constexpr (DIRECT) {
+        ck.score(qf, sc);
+        cv.template store<true>(vt, 0, lane);
+        next();
+      } else {
+        ck.template store<false>(kt, 0, lane);
+        cv.template store<true>(vt, 0, lane);
+        next();
+        score_tile<HD, KT, NT>(kt, qf, sc, lane);
+      }
       bool all[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) all[t] = true;
       const bool border = key + 32 > b.whole || gaps;
       sum_tile<HD, KT, NT, careful>(a, b, vt, sc, key, border, border || careful, all, end, gaps, z, o, lane);
     };
-    for (; key < p.k1; key += W * 32) {
-      ck.template store<false>(kt, 0, lane);
-      cv.template store<true>(vt, 0, lane);
-      if (key + W * 32 < p.k1) load(key + W * 32);
-      tile(std::false_type{}, lane);
-    }
+    for (; key < p.k1; key += W * 32) tile(std::false_type{}, lane, [&]() __attribute__((always_inline)) { if (key + W * 32 < p.k1) load(key + W * 32, lane); });
     if (!__all(finite(o))) {
       clear();
       for (key = p.k0 + wave * 32; key < p.k1; key += W * 32) {
         const int lane = fresh_lane();
-        load(key);
-        ck.template store<false>(kt, 0, lane);
-        cv.template store<true>(vt, 0, lane);
-        tile(std::true_type{}, lane);
+        load(key, lane);
+        tile(std::true_type{}, lane, []() {});
       }
     }
     join_waves<bf16_t, HD, NT, W, false>(a, b, (float*)smem, z, o, p.slot, wave, lane);
@@ -725,7 +766,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, 2) void k_paged_turns(const Paged
   }
 }
 
-Route route(const PagedArgs& a, int head_dim) {
+Route route(const PagedArgs& a, int head_dim, int format) {
   Route r{};
   const int64_t rows = (int64_t)a.max_q * a.shared, keys = a.max_kv;          // of a sequence, at most
   r.parts = 1;
@@ -747,7 +788,8 @@ Route route(const PagedArgs& a, int head_dim) {
       // Equal runs of all sequences' keys, two blocks a CU, where there is so much work that lengths below the bound count for more than a plan: 64 sequences of 100 to
       // 16000 keys 215 us.  Equal lengths lose little: 8 of 16000 keys with 8 heads 51 us, in ranges 47; 4 of 6000 23 and 17.  Not for sequences up to 2048
       // keys (64 of 2000 52 and 44), nor for very many; units are counted in 32 bits.
-      r.runs = (int)(blocks * units < 512 ? blocks * units : 512);
+      const int64_t most = 256 * few_per_cu(head_dim, rows <= 16 ? 1 : 2, format);
+      r.runs = (int)(blocks * units < most ? blocks * units : most);
     }
   } else {
     // Measured, heads of 128, with 256 and 128 rows: 6240 x 9360 x 40 as they are 997 and 1032 us, in 8 bits 1027 and 1085; 1560 x 20280 x 12 in ranges 199 and 197; 1000,
@@ -789,7 +831,7 @@ template <int HD, int FORMAT> void launch(const PagedArgs& a, int qb, hipStream_
 
 }  // namespace
 
-Route route_attn_paged_bf16(const PagedArgs& a, int head_dim) { return route(a, head_dim); }
+Route route_attn_paged_bf16(const PagedArgs& a, int head_dim, int format) { return route(a, head_dim, format); }
 void launch_attn_paged_bf16(const PagedArgs& a, const Route& r, int head_dim, int format, hipStream_t st) {
   auto of = [&](auto f) {
     if (head_dim == 128) launch<128, decltype(f)::value>(a, r.qb, st); else launch<64, decltype(f)::value>(a, r.qb, st);
