@@ -602,10 +602,14 @@ def _rows_2d(t, n, d, td, device):
 
 
 def _result_2d(t, n, d, td, like, stream):
-    """The caller's rows for a result, or new ones, with address and stride."""
+    """The caller's rows for a result, or new ones (of `like`'s shape where it has one and the type), with address and stride."""
     if t is not None:
         return (t,) + _rows_2d(t, n, d, td, like.device)
-    t = like.new_empty((n, d), dtype=td) if stream is None else _memory(lambda: like.new_empty((n, d), dtype=td), stream)
+    if like.dtype == td and like.shape[1] == d:      # 0.3 us less than new_empty
+        make = lambda: torch.empty_like(like, memory_format=torch.contiguous_format)   # noqa: E731
+    else:
+        make = lambda: like.new_empty((n, d), dtype=td)   # noqa: E731
+    t = make() if stream is None else _memory(make, stream)
     return t, t.data_ptr(), d
 
 
@@ -677,25 +681,26 @@ def gated_norm(x, y=None, gain=None, post_gain=None, gate=None, scale=None, shif
     the rows' type; gain, post_gain: [dim] of the rows' type; gate, scale, shift: float32 [n_groups, dim]; group: int32 [n], the rows' groups (outside: padding,
     left as it is), group 0 if not given.  Without y, h = N(x) ... alone (dtype: the rows' type, x's if not given); next_norm=False: x' alone.  x_out may be x
     and out may be y.  Returns (x', h), None for what is not computed."""
-    n, d = x.shape
-    dev, ts = x.device, x.dtype
+    (n, d), dev, ts = x.shape, x.device, x.dtype
     td = y.dtype if y is not None else ts if dtype is None else {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
     st = _stream_on(dev, stream)
     assert td in _KV_DTYPE and (ts == torch.float32 or ts == td), (ts, td)
-    assert y is not None or next_norm, "nothing to compute"
-    assert (y is not None or x_out is None) and (next_norm or out is None), "a result that is not computed"
-    groups = next((t.shape[0] for t in (gate, scale, shift) if t is not None), 1 if group is None else 2 ** 31 - 1)
-    vectors, f32 = (groups, d), torch.float32
-    cfg = _PACK_GATED(d, _KV_DTYPE[td], _KV_DTYPE[ts], NORM[norm], groups, eps, res_scale, _vector(gain, (d,), td, dev), _vector(post_gain, (d,), td, dev),
-                      _vector(gate, vectors, f32, dev), _vector(scale, vectors, f32, dev), _vector(shift, vectors, f32, dev),
-                      _vector(group, (n,), torch.int32, dev))
+    assert y is not None or (next_norm and x_out is None), "nothing to compute, or a result of it"
+    assert next_norm or out is None, "a result that is not computed"
+    by_group = gate if gate is not None else scale if scale is not None else shift
+    groups = by_group.shape[0] if by_group is not None else 1 if group is None else 2 ** 31 - 1
+    vectors = (groups, d)
+    cfg = _PACK_GATED(d, _KV_DTYPE[td], _KV_DTYPE[ts], NORM[norm], groups, eps, res_scale, 0 if gain is None else _vector(gain, (d,), td, dev),
+                      0 if post_gain is None else _vector(post_gain, (d,), td, dev), 0 if gate is None else _vector(gate, vectors, torch.float32, dev),
+                      0 if scale is None else _vector(scale, vectors, torch.float32, dev), 0 if shift is None else _vector(shift, vectors, torch.float32, dev),
+                      0 if group is None else _vector(group, (n,), torch.int32, dev))
     x_at, x_s = _rows_2d(x, n, d, ts, dev)
-    y_at, y_s, xo_at, xo_s, h_at, h_s = 0, 0, 0, 0, 0, 0
+    y_at = y_s = xo_at = xo_s = h_at = h_s = 0
     if y is not None:
         y_at, y_s = _rows_2d(y, n, d, td, dev)
         x_out, xo_at, xo_s = _result_2d(x_out, n, d, ts, x, stream)
     if next_norm:
-        out, h_at, h_s = _result_2d(out, n, d, td, x, stream)
+        out, h_at, h_s = _result_2d(out, n, d, td, y if y is not None else x, stream)
     _check(_lib.dp_gated_norm(cfg, x_at, x_s, y_at, y_s, n, xo_at, xo_s, h_at, h_s, st), "dp_gated_norm")
     return x_out, out
 
