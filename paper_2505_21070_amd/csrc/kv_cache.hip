@@ -87,6 +87,12 @@ __device__ __forceinline__ void angles(const RowArgs& a, int64_t t, int lane, in
   for (int i = 0; i < NP; ++i) { cs[i] = __shfl(c, pair0 + i, 64); sn[i] = __shfl(s, pair0 + i, 64); }
 }
 
+// The number of a block.  Blocks are handed out to the eight XCDs in turn; with RUNS each XCD gets a run of them, so that tokens that share lines of codes and of
+// scale bytes (32 or 128 of them a line) meet in its L2.
+template <bool RUNS> __device__ __forceinline__ uint32_t block_of() {
+  return RUNS ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x;
+}
+
 // One wavefront: the rows of a run, 64 / LANES at a time, U of those trips to memory under way at once.  Measured, bf16 heads of 128, 6240 tokens: norm
 // of 40 + 40 heads 43 us (256 MB, 5.9 TB/s), 40 + 40 heads into codes 38 us (192 MB, 5.0 TB/s), 12 + 12 + 12 with norm into codes 23 us (96 MB,
 // 4.1 TB/s); one token 2.9 us.
@@ -94,7 +100,7 @@ template <typename T, int HD, bool NORM, int TO>
 __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
   constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = 4;
   const int lane = threadIdx.x & 63, in_row = lane % LANES, c0 = in_row * N;
-  const uint32_t task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^26, see cut()
+  const uint32_t task = block_of<TO == TO_CODES || TO == TO_FP4>() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^26, see cut()
   const int64_t t = task / (uint32_t)a.runs;
   if (t >= a.n_tokens) return;
   int run = (int)(task % (uint32_t)a.runs);
@@ -194,9 +200,9 @@ __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
 // The way back: one row a lane group, keys and values of a token's heads.  40 + 40 heads of 6240 tokens out of codes 30 us (192 MB, 6.4 TB/s).
 template <typename T, int HD, int FORMAT>
 __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
-  constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = 4;
+  constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = FORMAT == DP_KV_FP4 ? 8 : 4;
   const int lane = threadIdx.x & 63, c0 = lane % LANES * N;
-  const uint32_t task = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^26, see cut()
+  const uint32_t task = block_of<FORMAT != DP_KV_PLAIN>() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // below 2^26, see cut()
   const int64_t t = task / (uint32_t)a.runs;
   if (t >= a.n_tokens) return;
   int run = (int)(task % (uint32_t)a.runs);
@@ -216,6 +222,7 @@ __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
     uint32_t byte[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (FORMAT == DP_KV_FP4 && r0 + u * ROWS >= last) break;
       int r = r0 + u * ROWS + lane / LANES;
       if (r >= last) r = last - 1;
       const int64_t row = row0 + ((int64_t)r << a.page_shift);
@@ -262,7 +269,7 @@ void cut(RowArgs& a, int rows, bool values) {
   a.runs_k = runs(a.hk, a.per_k);
   a.runs = a.runs_q + (values ? 2 : 1) * a.runs_k;
 }
-unsigned blocks_of(const RowArgs& a) { return (unsigned)((a.n_tokens * a.runs + 3) / 4); }
+unsigned blocks_of(const RowArgs& a) { return (unsigned)((a.n_tokens * a.runs + 31) / 32 * 8); }   // whole eights, see block_of()
 
 void set_powers(RowArgs& a, int hd, float theta) {
   const int cs = hd / 6, cf = hd / 2 - 2 * cs;
