@@ -313,7 +313,9 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
 // LDS, the next tile on its way in registers; nobody waits for anybody until the results are joined in LDS, in wavefront order.  W = 4: two blocks to a
 // CU keep 128 KB (codes: 64 KB) under way, and what bounds it is memory: 64 sequences of 16 .. 16000 keys, 8 heads of 128 in 8 bits, 201 us, 5.3 TB/s.  W = 8: no more
 // blocks than CUs, bound by a trip's chain of steps, 1.6 us for 256 keys: one token over 517 keys with 12 heads 10.3 us.
-// blocks of four wavefronts to a CU
+// Codes of 4 bits take so little memory that two blocks on a CU are bound by their own work: keys go from the pages straight into operands (KeyCodes), which frees
+// half of the LDS, and three blocks fit, four with heads of 64: the same 64 sequences, 32 heads on 8, 156 us, 143 with keys straight into operands, 127 with three blocks (4.9 TB/s beside
+// plan and join).
 constexpr int few_per_cu(int head_dim, int nt, int format) { return format == DP_KV_FP4 && nt == 1 ? (head_dim == 64 ? 4 : 3) : 2; }
 template <int HD, int NT, int W, int FORMAT, bool PLAN>
 __global__ __launch_bounds__(W * 64, (W == 4 ? few_per_cu(HD, NT, FORMAT) : 2)) void k_paged_few(const PagedArgs a) {

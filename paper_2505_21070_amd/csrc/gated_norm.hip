@@ -5,7 +5,8 @@
 // rounded once.
 //
 // Bound by memory: x, y, x' and h once each, 12 bytes a value with an fp32 stream and bf16 rows.  A row stays in the registers of the wavefronts that own it, 8
-// consecutive values a lane and trip; gate, scale and shift come out of the caches.
+// consecutive values a lane and trip; gate, scale and shift come out of the caches.  6240 rows of 5120, fp32 stream, LayerNorm, modulated 82 us (384 MB, 4.7 TB/s; a copy 5.1); with
+// vectors kept in registers over several rows 2 % less at twice the registers, with non-temporal loads 2 % more.  48 rows of 1536 6 us.
 #include <math.h>
 #include <stdio.h>
 

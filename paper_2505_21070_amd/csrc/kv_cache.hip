@@ -94,8 +94,8 @@ template <bool RUNS> __device__ __forceinline__ uint32_t block_of() {
 }
 
 // One wavefront: the rows of a run, 64 / LANES at a time, U of those trips to memory under way at once.  Measured, bf16 heads of 128, 6240 tokens: norm
-// of 40 + 40 heads 43 us (256 MB, 5.9 TB/s), 40 + 40 heads into codes 38 us (192 MB, 5.0 TB/s), 12 + 12 + 12 with norm into codes 23 us (96 MB,
-// 4.1 TB/s); one token 2.9 us.
+// of 40 + 40 heads 43 us (256 MB, 5.9 TB/s), 40 + 40 heads into codes of 8 bits 37 us (192 MB, 5.2 TB/s), of 4 bits 31 us (162 MB, 5.3 TB/s; 37 with blocks as they come), 12 + 12 + 12
+// with norm into codes of 8 bits 22 us (96 MB, 4.4 TB/s); one token 2.9 us.
 template <typename T, int HD, bool NORM, int TO>
 __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
   constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = 4;
@@ -197,7 +197,8 @@ __global__ __launch_bounds__(256) void k_head_rows(const RowArgs a) {
   }
 }
 
-// The way back: one row a lane group, keys and values of a token's heads.  40 + 40 heads of 6240 tokens out of codes 30 us (192 MB, 6.4 TB/s).
+// The way back: one row a lane group, keys and values of a token's heads.  40 + 40 heads of 6240 tokens out of codes of 8 bits 29 us (192
+// MB, 6.6 TB/s), of 4 bits 27 us (162 MB, 6.0 TB/s), for which eight trips are under way; codes are in the last-level cache after their write.
 template <typename T, int HD, int FORMAT>
 __global__ __launch_bounds__(256) void k_read_rows(const RowArgs a) {
   constexpr int N = Vec<T>::N, LANES = HD / N, ROWS = 64 / LANES, U = FORMAT == DP_KV_FP4 ? 8 : 4;
