@@ -43,7 +43,7 @@ __device__ __forceinline__ float activated(float v, int act) {
 }
 
 // Eight values of a token as B operands: one for bf16, the three parts of fp32 values, each the upper 16 bits of what is left.  CAREFUL: of a value that is not
-// finite there is no rest.
+// finite there is no rest, and NaN is one that its upper 16 bits show.
 template <typename T> struct Parts;
 template <> struct Parts<bf16_t> {
   static constexpr int N = 1;
@@ -59,6 +59,9 @@ template <> struct Parts<float> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v[2] = {i < 2 ? r.a[2 * i] : r.b[2 * i - 4], i < 2 ? r.a[2 * i + 1] : r.b[2 * i - 3]};
+      if (CAREFUL)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h] = v[h] != v[h] ? __uint_as_float(0x7fc00000u) : v[h];
 #pragma unroll
       for (int j = 0; j < 3; ++j) {
         w[j][i] = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302u);
@@ -73,8 +76,6 @@ template <> struct Parts<float> {
     for (int j = 0; j < 3; ++j) p[j] = __builtin_bit_cast(bf16x8, make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]));
   }
 };
-__device__ __forceinline__ void zero(uint4& v) { v = uint4{}; }
-__device__ __forceinline__ void zero(Raw8& v) { v.a = v.b = f32x4{0.f, 0.f, 0.f, 0.f}; }
 __device__ __forceinline__ bool finite(f32x4 v) { return fmaf(v[0], 0.f, v[1] * 0.f) + fmaf(v[2], 0.f, v[3] * 0.f) == 0.f; }
 
 // Weights as dp_fp4_lay leaves them: for each tile of 16 rows and step of 128 inputs, one behind the other, 1024 bytes of codes and 64 of group bytes.  Codes lie as

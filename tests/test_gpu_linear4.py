@@ -148,6 +148,19 @@ def test_values_that_are_not_finite(dtype, n):
     assert (np.abs(got[fine] - ref[fine]) <= HALF[dtype] * np.abs(ref[fine]) * (1 + 2.0 ** -7) + 2 * (3 * in_ + 12) * U * size).all()
 
 
+@pytest.mark.parametrize("n", [1, 40, 300])
+def test_every_nan_is_one(n):
+    """fp32 NaNs that only their lower bits tell from infinity, beside a weight of 1 and one of 0."""
+    from paper_2505_21070_amd import binding as B
+    codes = torch.zeros((2, 64), dtype=torch.uint8, device="cuda")
+    codes[0, 10] = 0x02                                    # output 0 takes input 20, output 1 nothing
+    m = B.Linear4(codes.view(torch.float4_e2m1fn_x2), torch.full((2, 4), 127, dtype=torch.uint8, device="cuda"), dtype="f32")
+    x = torch.zeros((n, 128))
+    x.view(torch.int32)[0, 20], x.view(torch.int32)[n - 1, 21] = 0x7f800001, -0x7fffff
+    y = m.forward(x.cuda())
+    assert torch.isnan(y[0]).all() and torch.isnan(y[n - 1]).all() and (y[1: n - 1] == 0).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [1, 5, 40, 65, 300])
 def test_strides_and_what_lies_around(n, dtype):
