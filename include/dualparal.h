@@ -435,7 +435,7 @@ int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_
  *   workspace  : device, 256-byte aligned, dp_linear_fp4_workspace_bytes(w, n) bytes (0 for many calls: then it may be NULL), used by one call at a time; nothing has to be
  *                kept in it between calls.
  * n == 0 is a no-op.  Asynchronous on hip_stream; allocates nothing and may be recorded into a HIP graph.
- * Errors: DP_EINVAL (null pointer, sizes outside the limits, n * out above 2^35, alignment or strides as above), DP_ENOMEM (workspace too small), DP_EHIP. */
+ * Errors: DP_EINVAL (null pointer, sizes outside the limits, n * out above 2^35, alignment or strides as above, y at x), DP_ENOMEM (workspace too small), DP_EHIP. */
 enum { DP_ACT_NONE = 0, DP_ACT_GELU = 1 /* tanh approximation, the stage's */, DP_ACT_SILU = 2 };
 typedef struct {
   int32_t out;                /* 1 .. 2^24                                                         */
@@ -465,7 +465,8 @@ int dp_linear_fp4(const dp_fp4_matrix* w, const void* x, int64_t x_stride, int64
  *                x_out may be x, and h may be y (same data and stride); any other overlap with what is read is not allowed.
  *   group      : device int32 [n], or NULL: group 0 for all.  A row whose group is outside [0, n_groups) is padding: its x_out and h are left as they are.
  * n == 0 is a no-op.  Asynchronous on hip_stream; allocates nothing and may be recorded into a HIP graph.
- * Errors: DP_EINVAL (null pointer, sizes outside the limits, more than 2^24 rows, alignment or strides as above, an option without what it goes with), DP_EHIP. */
+ * Errors: DP_EINVAL (null pointer, sizes outside the limits, more than 2^24 rows, n * dim above 2^35, alignment or strides as above, an option without what it goes with,
+ *         one memory for both results), DP_EHIP. */
 enum { DP_NORM_LAYER = 0, DP_NORM_RMS = 1 };
 typedef struct {
   int32_t dim;                /* a multiple of 8, 8 .. 16384                                       */

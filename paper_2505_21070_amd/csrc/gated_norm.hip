@@ -232,12 +232,14 @@ extern "C" int dp_gated_norm(const dp_gated_norm_config* c, const void* x, int64
   REFUSE_IF((c->scale != nullptr) != (c->shift != nullptr) ? "scale and shift go together" : nullptr);
   REFUSE_IF(((uintptr_t)c->gain | (uintptr_t)c->post_gain | (uintptr_t)c->gate | (uintptr_t)c->scale | (uintptr_t)c->shift) & 15 ? "gains, gates, scales and shifts must be 16-byte aligned" : nullptr);
   REFUSE_IF((uintptr_t)c->group & 3 ? "group must be 4-byte aligned" : nullptr);
-  REFUSE_IF(n < 0 || n > (1 << 24) ? "n must be in [0, 2^24]" : nullptr);
+  // launches stay below 2^32 threads: 256 a row of more than 2048 values, 512 of more than 8192
+  REFUSE_IF(n < 0 || n > (1 << 24) || n * c->dim > (int64_t)1 << 35 ? "n must be in [0, 2^24], n * dim at most 2^35" : nullptr);
   if (n == 0) return DP_OK;
   REFUSE_IF(!x || (!y && !h) ? "null pointer" : nullptr);
   REFUSE_IF(!y && (x_out || c->post_gain || c->gate) ? "x_out, post_gain and gate go with y" : nullptr);
   REFUSE_IF(!h && (c->gain || c->scale) ? "gain, scale and shift go with h" : nullptr);
   REFUSE_IF(!h && !x_out ? "nothing to write" : nullptr);
+  REFUSE_IF(h == x_out ? "x_out and h must not be the same" : nullptr);
   REFUSE_IF(why_not_2d(x, x_stride, n, c->dim, c->stream_dtype, false));
   if (y) REFUSE_IF(why_not_2d(y, y_stride, n, c->dim, c->dtype, false));
   if (x_out) REFUSE_IF(why_not_2d(x_out, x_out_stride, n, c->dim, c->stream_dtype, true));

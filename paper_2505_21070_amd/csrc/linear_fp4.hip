@@ -580,6 +580,7 @@ extern "C" int dp_linear_fp4(const dp_fp4_matrix* w, const void* x, int64_t x_st
   REFUSE_IF(n > 1 && (x_stride < 0 || x_stride > 1 << 21) ? "x_stride must be in [0, 2^21]" : nullptr);
   REFUSE_IF(((uintptr_t)y | (uintptr_t)w->bias) & (size - 1) ? "y and the bias must be aligned to their type" : nullptr);
   REFUSE_IF(n > 1 && (y_stride < w->out || y_stride > (int64_t)1 << 38) ? "y_stride must be in [out, 2^38]" : nullptr);
+  REFUSE_IF(x == y ? "y must not be x" : nullptr);
   LinearArgs a{};
   a.laid = (const uint8_t*)w->laid; a.bias = w->bias; a.x = x; a.y = y;
   a.x_s = n > 1 ? x_stride : 0; a.y_s = n > 1 ? y_stride : 0; a.n = n; a.in = w->in; a.out = w->out; a.act = act;

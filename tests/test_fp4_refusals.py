@@ -23,7 +23,7 @@ def test_nothing_to_do():
     assert P.write(c=cache4(), n=0) == P.read(c=cache4(), n=0) == P.qkv(c=cache4(), n=0) == P.attend(c=cache4(), n=0) == B.DP_OK
 
 
-def gated(x=P.AT, xs=128, y=P.AT, ys=128, n=3, xo=P.AT, xos=128, h=P.AT, hs=128, **kw):
+def gated(x=P.AT, xs=128, y=2 * P.AT, ys=128, n=3, xo=P.AT, xos=128, h=2 * P.AT, hs=128, **kw):
     d = dict(dim=128, dtype=B.DP_BF16, stream_dtype=B.DP_F32, norm=1, n_groups=2, eps=1e-6, res_scale=1.0, gain=P.AT, post_gain=P.AT, gate=P.AT, scale=P.AT, shift=P.AT, group=P.AT)
     return P.L.dp_gated_norm(bytes(B.GatedNorm(**dict(d, **kw))), x, xs, y, ys, n, xo, xos, h, hs, None)
 
@@ -32,7 +32,8 @@ def gated(x=P.AT, xs=128, y=P.AT, ys=128, n=3, xo=P.AT, xos=128, h=P.AT, hs=128,
                                  dict(eps=-1.0), dict(eps=float("inf")), dict(res_scale=float("inf")), dict(scale=None), dict(shift=None), dict(gain=P.AT + 4), dict(gate=P.AT + 8),
                                  dict(group=P.AT + 1), dict(n=-1), dict(n=(1 << 24) + 1), dict(x=None), dict(y=None), dict(h=None), dict(x=P.AT + 8), dict(y=P.AT + 2), dict(xs=130),
                                  dict(ys=132), dict(hs=-128), dict(xos=0), dict(hs=64), dict(xs=1 << 40), dict(y=None, xo=None, post_gain=None), dict(y=None, xo=None, gate=None),
-                                 dict(h=None, gain=None), dict(h=None, xo=None, gain=None, scale=None, shift=None)], ids=str)
+                                 dict(h=None, gain=None), dict(h=None, xo=None, gain=None, scale=None, shift=None), dict(h=P.AT),
+                                 dict(n=(1 << 24) - 1, dim=2056, xs=2056, ys=2056, xos=2056, hs=2056)], ids=str)
 def test_bad_gated_norms(bad):
     P.refused(gated(**bad), "dp_gated_norm")
 
@@ -46,7 +47,7 @@ def test_the_binding_packs_what_the_struct_holds():
     assert B._PACK_GATED(1, 2, 3, 4, 5, 6.0, 7.0, 8, 9, 10, 11, 12, 13) == bytes(B.GatedNorm(1, 2, 3, 4, 5, 6.0, 7.0, 8, 9, 10, 11, 12, 13))
 
 
-def linear(w=True, x=P.AT, xs=64, n=3, act=0, y=P.AT, ys=40, work=P.AT, nbytes=1 << 40, **kw):
+def linear(w=True, x=P.AT, xs=64, n=3, act=0, y=2 * P.AT, ys=40, work=P.AT, nbytes=1 << 40, **kw):
     d = dict(out=40, in_=64, dtype=B.DP_BF16, laid=P.AT, bias=P.AT)
     return P.L.dp_linear_fp4(bytes(B.Fp4Matrix(**dict(d, **kw))) if w else None, x, xs, n, act, y, ys, work, nbytes, None)
 
@@ -65,7 +66,7 @@ BAD_CODES = [dict(codes=None), dict(scales=None), dict(codes=P.AT + 8)]
 
 @pytest.mark.parametrize("bad", BAD_SIZES + [dict(w=False), dict(dtype=2), dict(n=-1), dict(n=(1 << 24) + 1), dict(n=1 << 12, out=1 << 24), dict(act=3), dict(act=-1), dict(x=None), dict(y=None),
                                              dict(laid=None), dict(laid=P.AT + 32), dict(x=P.AT + 8), dict(xs=68), dict(xs=-64), dict(xs=1 << 22), dict(y=P.AT + 1), dict(bias=P.AT + 1),
-                                             dict(ys=39), dict(ys=1 << 39), dict(dtype=B.DP_F32, y=P.AT + 2), dict(out=512, in_=13824, ys=512, xs=13824, work=P.AT + 128)], ids=str)
+                                             dict(ys=39), dict(ys=1 << 39), dict(y=P.AT), dict(dtype=B.DP_F32, y=P.AT + 2), dict(out=512, in_=13824, ys=512, xs=13824, work=P.AT + 128)], ids=str)
 def test_bad_linears(bad):
     P.refused(linear(**bad), "dp_linear_fp4")
 
