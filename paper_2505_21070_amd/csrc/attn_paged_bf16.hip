@@ -315,8 +315,8 @@ __device__ __forceinline__ void load_queries(const PagedArgs& a, const Block& b,
 // blocks than CUs, bound by a trip's chain of steps, 1.6 us for 256 keys: one token over 517 keys with 12 heads 10.3 us.
 // Codes of 4 bits take so little memory that two blocks on a CU are bound by their own work: keys go from the pages straight into operands (KeyCodes), which frees
 // half of the LDS, and three blocks fit, four with heads of 64: the same 64 sequences, 32 heads on 8, 156 us, 143 with keys straight into operands, 127 with three blocks (4.9 TB/s beside
-// plan and join).
-constexpr int few_per_cu(int head_dim, int nt, int format) { return format == DP_KV_FP4 && nt == 1 ? (head_dim == 64 ? 4 : 3) : 2; }
+// plan and join).  32 rows of heads of 64 leave registers for three: 64 sequences of 16000 keys, 128 heads on 4, 100 -> 91 us; of heads of 128 for two, three spill 400 bytes a lane.
+constexpr int few_per_cu(int head_dim, int nt, int format) { return format != DP_KV_FP4 ? 2 : head_dim == 64 && nt == 1 ? 4 : head_dim == 64 || nt == 1 ? 3 : 2; }
 template <int HD, int NT, int W, int FORMAT, bool PLAN>
 __global__ __launch_bounds__(W * 64, (W == 4 ? few_per_cu(HD, NT, FORMAT) : 2)) void k_paged_few(const PagedArgs a) {
   constexpr int QB = NT * 16, KT = 2, CR = HD / 8, TILE = 32 * CR, JOIN = (W * 16 * (2 + HD + 4) * 4 + 15) / 16;
