@@ -4,8 +4,8 @@
 // v_mfma_f32_16x16x32_bf16: 16 outputs of a row tile against 16 tokens.  fp32 inputs are split into three bf16 parts of 8 bits each, which together are
 // the input exactly (as far as bf16 reaches down: a part below 2^-126 may be lost), so that fp32 takes the same instructions three times instead of ones of 1/16 the rate; all sums are fp32.
 //
-// What bounds it: few tokens, the codes' way from memory (5120 -> 13824, one token 9.4 us, 4.0 TB/s); many, the matrix pipes (6240 tokens 5120 -> 5120 264 us, 1.24
-// PFLOP/s; fp32 1560 tokens 1536 -> 8960 154 us, 280 TFLOP/s, beside the parts' arithmetic).
+// What bounds it: few tokens, the codes' way from memory (5120 -> 13824, one token 9.4 us, 4.0 TB/s); many, the matrix pipes (6240 tokens 5120 -> 5120 262 us, 1.25
+// PFLOP/s; fp32 1560 tokens 1536 -> 8960 130 us, 331 TFLOP/s, beside the parts' arithmetic).
 #include <math.h>
 #include <stdio.h>
 
@@ -37,7 +37,8 @@ struct LinearArgs {
 };
 
 __device__ __forceinline__ float activated(float v, int act) {
-  if (act == DP_ACT_GELU) v = v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.f * 0.7978845608028654f * 1.4426950408889634f * fmaf(0.044715f * v * v, v, v)));
+  constexpr float C = -2.f * 0.7978845608028654f * 1.4426950408889634f;
+  if (act == DP_ACT_GELU) v = v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * fmaf(C * 0.044715f, v * v, C)));
   if (act == DP_ACT_SILU) v = v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * v));
   return v;
 }
@@ -160,17 +161,18 @@ __global__ __launch_bounds__(WR * WT * WK * 64) void k_linear(const LinearArgs a
 #endif
   };
   f32x4 acc[R][NT];
-  // The step whose inputs are at `tile`: four products of 32 inputs, whose tokens' operands are read in pieces of NC tiles, AHEAD pieces before they are used.
-  constexpr int NC = NT * P::N > 4 ? (NT > 4 ? NT / 2 : NT > 1 && P::N > 1 ? NT / 2 : NT) : NT, PIECES = 4 * (NT / NC), AHEAD = NT * P::N <= 4 ? 3 : 1;
-  static_assert(NT % NC == 0, "whole pieces");
+  // The step whose inputs are at `tile`: four products of 32 inputs, whose tokens' operands are read in pieces of NC tiles (which may be of two products), AHEAD pieces before
+  // they are used.  Of 64 tokens and two tiles of rows one piece ahead is enough, and leaves registers for a second block on a CU.
+  constexpr int NC = NT % 2 == 0 && (NT > 4 || P::N > 1) ? NT / 2 : NT > 4 ? 4 : NT, PIECES = 4 * NT / NC, AHEAD = NT * P::N <= (R > 1 && P::N == 1 ? 3 : 4) ? 3 : 1;
+  static_assert(4 * NT % NC == 0, "whole pieces");
   auto multiply = [&](const Step<R>& s, const lds_char* __restrict__ tile, auto careful) __attribute__((always_inline)) {
     const lds_char* const base = tile + (mine + lr) * ROW;
     typename P::Raw raw[AHEAD + 1][NC];
     auto read = [&](int piece) __attribute__((always_inline)) {
-      const int i = piece / (NT / NC), t0 = piece % (NT / NC) * NC;
 #pragma unroll
       for (int t = 0; t < NC; ++t) {
-        const lds_char* const row = base + (t0 + t) * 16 * ROW;
+        const int i = (piece * NC + t) / NT;
+        const lds_char* const row = base + (piece * NC + t) % NT * 16 * ROW;
         auto& to = raw[piece % (AHEAD + 1)][t];
         if constexpr (P::N == 1) to = __builtin_bit_cast(uint4, lds_get(row + ((i * 4 + lg) ^ lr) * 16));
         else { to.a = __builtin_bit_cast(f32x4, lds_get(row + ((i * 8 + lg * 2) ^ lr) * 16)); to.b = __builtin_bit_cast(f32x4, lds_get(row + ((i * 8 + lg * 2 + 1) ^ lr) * 16)); }
@@ -182,23 +184,23 @@ __global__ __launch_bounds__(WR * WT * WK * 64) void k_linear(const LinearArgs a
     bf16x8 w[R];
 #pragma unroll
     for (int piece = 0; piece < PIECES; ++piece) {
-      const int i = piece / (NT / NC), t0 = piece % (NT / NC) * NC;
       if (piece + AHEAD < PIECES) {
         read(piece + AHEAD);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (t0 == 0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) w[r] = weights(s.c[r], s.s[r], i);
-      }
 #pragma unroll
       for (int t = 0; t < NC; ++t) {
+        const int i = (piece * NC + t) / NT, tt = (piece * NC + t) % NT;
+        if (tt == 0) {
+#pragma unroll
+          for (int r = 0; r < R; ++r) w[r] = weights(s.c[r], s.s[r], i);
+        }
         bf16x8 p[P::N];
         P::template split<decltype(careful)::value>(raw[piece % (AHEAD + 1)][t], p);
 #pragma unroll
         for (int j = 0; j < P::N; ++j)
 #pragma unroll
-          for (int r = 0; r < R; ++r) acc[r][t0 + t] = mfma(w[r], p[j], acc[r][t0 + t]);
+          for (int r = 0; r < R; ++r) acc[r][tt] = mfma(w[r], p[j], acc[r][tt]);
       }
     }
   };
@@ -383,8 +385,9 @@ template <typename T, int R, int NT, int WR, int WT, int WK, int NS> void launch
   if (a.parts > 1) k_join<T><<<(unsigned)((a.n * a.out + 255) / 256), 256, 0, st>>>(a);
 }
 // The tiles there are, and what they take: rows and tokens of a block, its groups (WK), how many of them a CU holds, and in units of 10 ns a group's step with 1, 2 .. blocks
-// on a CU in the last round of blocks, in the rounds before it, and what is done around the steps.  Fitted to 1248 launches: 512 .. 13824 outputs, 1504 .. 13824 inputs, 1 .. 6240
-// tokens; the estimate below then takes a tile within 1 % of the best one on average, 8 % at worst.
+// on a CU in the last round of blocks, in the rounds before it, and what is done around the steps.  Fitted to 1962 launches: 512 .. 13824 outputs, 1504 .. 13824 inputs, 1 .. 6240
+// tokens; the estimate below then takes a tile within 0.5 % of the best one on average, 11 % at worst.  Tiles of tokens in steps of 16 or 32 are worth their code where a round of blocks ends
+// just so: 1560 tokens, 8960 -> 1536, 46 us, with 64, 128, 192 and 256 alone 99; 800 tokens, 5120 -> 5120, 45 and 68; 1560 tokens, 1536 -> 8960, 39 and 42.
 struct Tile { int rows, tokens, groups, per_cu, last[3], full, around; };
 #define TILES_BF16(X) \
   X(1, 1, 2, 1, 4, 3, {32, 16, 4, 3, {32, 64, 95}, 88, 152}) \
@@ -394,12 +397,17 @@ struct Tile { int rows, tokens, groups, per_cu, last[3], full, around; };
   X(1, 2, 4, 1, 4, 3, {64, 32, 4, 1, {57}, 62, 251}) \
   X(1, 3, 2, 1, 4, 3, {32, 48, 4, 1, {68}, 82, 207}) \
   X(1, 3, 4, 1, 4, 3, {64, 48, 4, 1, {78}, 94, 301}) \
-  X(1, 4, 4, 1, 2, 4, {64, 64, 2, 1, {60}, 70, 285}) \
-  X(2, 4, 4, 1, 2, 3, {128, 64, 2, 1, {90}, 123, 377}) \
-  X(2, 4, 4, 1, 1, 3, {128, 64, 1, 2, {64, 104}, 108, 356}) \
-  X(4, 4, 4, 2, 1, 2, {256, 128, 1, 1, {150}, 176, 776}) \
-  X(4, 6, 4, 2, 1, 2, {256, 192, 1, 1, {200}, 225, 923}) \
-  X(4, 8, 4, 2, 1, 2, {256, 256, 1, 1, {252}, 291, 1075})
+  X(1, 4, 4, 1, 2, 4, {64, 64, 2, 1, {61}, 67, 213}) \
+  X(2, 3, 4, 1, 2, 2, {128, 48, 2, 2, {82, 144}, 150, 181}) \
+  X(2, 4, 4, 1, 2, 2, {128, 64, 2, 2, {95, 183}, 195, 219}) \
+  X(2, 5, 4, 1, 2, 2, {128, 80, 2, 2, {110, 208}, 221, 260}) \
+  X(2, 4, 4, 1, 1, 2, {128, 64, 1, 3, {63, 106, 153}, 164, 275}) \
+  X(2, 5, 4, 1, 1, 2, {128, 80, 1, 3, {70, 123, 189}, 193, 321}) \
+  X(4, 4, 4, 2, 1, 2, {256, 128, 1, 1, {156}, 188, 632}) \
+  X(4, 5, 4, 2, 1, 2, {256, 160, 1, 1, {179}, 203, 645}) \
+  X(4, 6, 4, 2, 1, 2, {256, 192, 1, 1, {200}, 231, 676}) \
+  X(4, 7, 4, 2, 1, 2, {256, 224, 1, 1, {222}, 261, 803}) \
+  X(4, 8, 4, 2, 1, 2, {256, 256, 1, 1, {251}, 304, 781})
 #define TILES_F32(X) \
   X(1, 1, 1, 1, 8, 2, {16, 16, 8, 1, {117}, 130, 203}) \
   X(1, 1, 2, 1, 4, 3, {32, 16, 4, 1, {108}, 116, 185}) \
