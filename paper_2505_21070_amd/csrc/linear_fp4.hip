@@ -5,7 +5,7 @@
 // the input exactly (as far as bf16 reaches down: a part below 2^-126 may be lost), so that fp32 takes the same instructions three times instead of ones of 1/16 the rate; all sums are fp32.
 //
 // What bounds it: few tokens, the codes' way from memory (5120 -> 13824, one token 9.4 us, 4.0 TB/s); many, the matrix pipes (6240 tokens 5120 -> 5120 262 us, 1.25
-// PFLOP/s; fp32 1560 tokens 1536 -> 8960 130 us, 331 TFLOP/s, beside the parts' arithmetic).
+// PFLOP/s; fp32 1560 tokens 1536 -> 8960 127 us, 338 TFLOP/s, beside the parts' arithmetic).
 #include <math.h>
 #include <stdio.h>
 
@@ -385,9 +385,9 @@ template <typename T, int R, int NT, int WR, int WT, int WK, int NS> void launch
   if (a.parts > 1) k_join<T><<<(unsigned)((a.n * a.out + 255) / 256), 256, 0, st>>>(a);
 }
 // The tiles there are, and what they take: rows and tokens of a block, its groups (WK), how many of them a CU holds, and in units of 10 ns a group's step with 1, 2 .. blocks
-// on a CU in the last round of blocks, in the rounds before it, and what is done around the steps.  Fitted to 1962 launches: 512 .. 13824 outputs, 1504 .. 13824 inputs, 1 .. 6240
+// on a CU in the last round of blocks, in the rounds before it, and what is done around the steps.  Fitted to 2595 launches: 512 .. 13824 outputs, 1504 .. 13824 inputs, 1 .. 6240
 // tokens; the estimate below then takes a tile within 0.5 % of the best one on average, 11 % at worst.  Tiles of tokens in steps of 16 or 32 are worth their code where a round of blocks ends
-// just so: 1560 tokens, 8960 -> 1536, 46 us, with 64, 128, 192 and 256 alone 99; 800 tokens, 5120 -> 5120, 45 and 68; 1560 tokens, 1536 -> 8960, 39 and 42.
+// just so: 1560 tokens, 8960 -> 1536, 46 us, with 64, 128, 192 and 256 alone 99; 800 tokens, 5120 -> 5120, 45 and 68; 1560 tokens, 1536 -> 8960, 39 and 42; fp32, 1560 tokens, 1536 -> 1536, 33 and 41.
 struct Tile { int rows, tokens, groups, per_cu, last[3], full, around; };
 #define TILES_BF16(X) \
   X(1, 1, 2, 1, 4, 3, {32, 16, 4, 3, {32, 64, 95}, 88, 152}) \
@@ -411,13 +411,17 @@ struct Tile { int rows, tokens, groups, per_cu, last[3], full, around; };
 #define TILES_F32(X) \
   X(1, 1, 1, 1, 8, 2, {16, 16, 8, 1, {117}, 130, 203}) \
   X(1, 1, 2, 1, 4, 3, {32, 16, 4, 1, {108}, 116, 185}) \
-  X(1, 1, 4, 1, 4, 2, {64, 16, 4, 1, {179}, 165, 215}) \
-  X(1, 2, 4, 1, 2, 3, {64, 32, 2, 1, {162}, 171, 231}) \
-  X(2, 2, 4, 1, 2, 2, {128, 32, 2, 2, {210, 391}, 319, 273}) \
-  X(2, 2, 4, 1, 1, 3, {128, 32, 1, 3, {121, 210, 306}, 301, 276}) \
-  X(4, 2, 4, 1, 1, 2, {256, 32, 1, 2, {164, 312}, 293, 579}) \
-  X(8, 2, 2, 1, 1, 2, {256, 32, 1, 2, {238, 283}, 262, 1104}) \
-  X(8, 2, 4, 2, 1, 2, {512, 64, 1, 1, {434}, 457, 1347})
+  X(1, 1, 4, 1, 4, 2, {64, 16, 4, 1, {177}, 174, 221}) \
+  X(1, 2, 4, 1, 2, 3, {64, 32, 2, 1, {162}, 169, 232}) \
+  X(2, 2, 4, 1, 2, 2, {128, 32, 2, 2, {209, 395}, 368, 237}) \
+  X(2, 3, 4, 1, 2, 2, {128, 48, 2, 1, {281}, 318, 348}) \
+  X(2, 2, 4, 1, 1, 3, {128, 32, 1, 3, {122, 206, 301}, 289, 272}) \
+  X(2, 3, 4, 1, 1, 2, {128, 48, 1, 3, {167, 279, 419}, 378, 328}) \
+  X(4, 2, 4, 1, 1, 2, {256, 32, 1, 2, {163, 297}, 282, 568}) \
+  X(4, 3, 4, 1, 1, 2, {256, 48, 1, 2, {213, 387}, 368, 595}) \
+  X(8, 2, 2, 1, 1, 2, {256, 32, 1, 2, {251, 278}, 268, 814}) \
+  X(6, 2, 4, 2, 1, 2, {384, 64, 1, 1, {352}, 356, 680}) \
+  X(8, 2, 4, 2, 1, 2, {512, 64, 1, 1, {437}, 461, 1090})
 template <typename T> struct Tiles;
 #define X(R, NT, WR, WT, WK, NS, ...) __VA_ARGS__,
 template <> struct Tiles<bf16_t> { static constexpr Tile all[] = {TILES_BF16(X)}; };

@@ -57,13 +57,14 @@ REACH = {
              (7, 1): (50, 8801, 1504), (8, 1): (33, 20001, 1504), (8, 2): (33, 20001, 13792), (8, 8): (33, 2900, 8992), (9, 1): (49, 20001, 992), (9, 2): (49, 8801, 8992),
              (10, 1): (65, 20001, 992), (10, 4): (65, 6601, 13792), (10, 8): (65, 3333, 13792), (11, 1): (450, 11001, 992), (12, 1): (300, 20001, 992), (13, 1): (333, 20001, 992),
              (14, 1): (400, 20001, 992), (15, 1): (500, 20001, 992), (16, 1): (1000, 11001, 992), (17, 1): (700, 20001, 992)},
-    "f32": {(0, 1): (1, 500, 1504), (0, 8): (1, 500, 8992), (1, 1): (1, 4505, 1504), (1, 8): (1, 500, 4000), (2, 1): (1, 8801, 1504), (2, 4): (1, 2900, 13792), (3, 1): (17, 8801, 1504),
-            (3, 8): (17, 1500, 13792), (4, 1): (17, 20001, 1504), (4, 2): (65, 3333, 2016), (4, 8): (33, 1500, 4000), (5, 2): (33, 20001, 4000), (5, 8): (33, 1500, 5088), (6, 1): (33, 20001, 1504),
-            (7, 1): (130, 20001, 4000), (8, 1): (1550, 3333, 1504)},
+    "f32": {(0, 1): (1, 500, 1504), (0, 8): (1, 500, 8992), (1, 1): (1, 4505, 1504), (1, 8): (1, 500, 4000), (2, 1): (1, 8801, 1504), (2, 4): (1, 2900, 13792), (3, 1): (17, 8801, 992),
+            (3, 8): (17, 1500, 13792), (4, 1): (17, 20001, 1504), (4, 2): (17, 8801, 1504), (4, 8): (33, 1500, 4000), (5, 1): (33, 20001, 992), (5, 4): (65, 3333, 2016), (6, 1): (600, 5003, 992),
+            (6, 2): (49, 20001, 4000), (6, 8): (1, 8801, 8992), (7, 4): (33, 20001, 4000), (7, 8): (33, 2900, 5088), (8, 1): (49, 20001, 1504), (9, 1): (161, 11001, 992),
+            (10, 1): (257, 11001, 2016), (11, 1): (193, 20001, 992), (12, 1): (300, 20001, 992)},
 }
 # rows that end with a whole eight: the tiles that go through LDS on their way out
 EVEN = [("bf16", (11, 1), (450, 11000, 992)), ("bf16", (12, 1), (300, 20000, 992)), ("bf16", (13, 1), (333, 20000, 992)), ("bf16", (14, 1), (400, 20000, 992)),
-        ("bf16", (15, 1), (500, 20000, 992)), ("bf16", (16, 1), (1000, 11000, 992)), ("bf16", (17, 1), (700, 20000, 992)), ("f32", (8, 1), (1550, 3336, 1504))]
+        ("bf16", (15, 1), (500, 20000, 992)), ("bf16", (16, 1), (1000, 11000, 992)), ("bf16", (17, 1), (700, 20000, 992)), ("f32", (12, 1), (300, 20000, 992))]
 
 
 def kind_of(out, in_, dtype, n):
