@@ -421,8 +421,8 @@ int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_
                   void* hip_stream);
 
 /* Products with weights held in 4 bits: y = act(x W^T + bias) for n tokens, one to many.  W [out, in] is held as DP_KV_FP4 holds rows: codes e2m1, two to a byte,
- * the first one in its low half, and a byte for each 32 values of a row.  dp_fp4_pack makes codes and bytes of a matrix; the bytes 27 .. 252 and 255 (NaN) are those it
- * writes, 2 .. 252 are read as 2^(b - 127) (others have no meaning: a code times such a power may not be a normal number).  dp_fp4_lay puts both, once, into the order that the products read them in: out and in are filled up to multiples of 16 and
+ * the first one in its low half, and a byte for each 32 values of a row.  dp_fp4_pack makes codes and bytes of a matrix, with the bytes 27 .. 252 and 255; any other byte may come from
+ * elsewhere: b stands for 2^(b - 127), 255 for NaN, and a group of 253 or 254 that has a weight of 2^128 or more is NaN, all of it.  dp_fp4_lay puts both, once, into the order that the products read them in: out and in are filled up to multiples of 16 and
  * 128, which is all that is known of that order; it takes 0.53 bytes a weight as the codes do, which are not needed any more.
  *   codes  : device [out, in / 2], 16-byte aligned;  scales : device [out, in / 32]
  *   laid   : device, dp_fp4_laid_bytes(out, in) bytes, 64-byte aligned;  bias : device [out] of dtype, or NULL

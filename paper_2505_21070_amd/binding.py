@@ -637,7 +637,7 @@ def pack_fp4(w, stream=None):
 
 class Linear4:
     """y = act(x W^T + bias) with weights in 4 bits.  codes: float4_e2m1fn_x2 [out, in / 2], scales: uint8 [out, in / 32], a byte b for 32 values that stands for
-    the factor 2^(b - 127) (2 .. 252; 255: NaN), as pack_fp4 makes them; bias: [out] of the tokens' type, or None.  dtype ("f32", "bf16") is that of the tokens.  Codes and
+    the factor 2^(b - 127) (255: NaN; so is a group with a weight of 2^128 or more), as pack_fp4 makes them or other programs; bias: [out] of the tokens' type, or None.  dtype ("f32", "bf16") is that of the tokens.  Codes and
     scales are read once, here, into the order that the products want (`laid`, of the same size), and not kept.  Calls on a named stream wait for nobody, as
     KVCache's; the object has to live until such calls, and graphs that hold calls of it, are done."""
 

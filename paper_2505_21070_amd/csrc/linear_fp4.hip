@@ -481,7 +481,10 @@ template <typename T> __global__ __launch_bounds__(256) void k_pack(const T* src
   scales[id] = (uint8_t)byte;
 }
 
-// A chunk of a tile and step a wavefront: each lane its 16 bytes, the first 16 lanes the rows' group bytes.
+// Whether one of eight codes times 2^(byte - 127) is 2^128 or more: 4 and 6 times 2^126, 2 and more times 2^127
+__device__ __forceinline__ bool beyond(uint32_t w, uint32_t byte) { return byte == 253 ? (w & w << 1 & 0x44444444u) != 0 : byte == 254 && (w & 0x44444444u); }
+// A chunk of a tile and step a wavefront: each lane its 16 bytes, the first 16 lanes the rows' group bytes.  A group with a weight that fp32 does not hold is NaN, as one
+// with a value that was not finite: as an infinity it would be NaN with a part of an input that is 0, and only there.
 __global__ __launch_bounds__(256) void k_lay(const uint8_t* codes, const uint8_t* scales, int32_t out, int32_t in, uint8_t* laid) {
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4, steps = (in + 127) / 128, groups = in / FP4_GROUP;
   const int64_t chunk = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), tile = chunk / steps;
@@ -492,12 +495,16 @@ __global__ __launch_bounds__(256) void k_lay(const uint8_t* codes, const uint8_t
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = row < out && step * 4 + i < groups ? *(const uint32_t*)(codes + row * (in / 2) + (step * 4 + i) * 16 + lg * 4) : 0u;
   *(uint4*)(laid + chunk * CHUNK + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-  if (lg == 0) {
-    uint32_t b = 0;
+  uint32_t b = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b |= (row < out && step * 4 + i < groups ? scales[row * groups + step * 4 + i] : 127u) << (8 * i);
-    *(uint32_t*)(laid + chunk * CHUNK + 1024 + lr * 4) = b;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t byte = row < out && step * 4 + i < groups ? scales[row * groups + step * 4 + i] : 127u;
+    int nan = beyond(w[i], byte);
+    nan |= __shfl_xor(nan, 16, 64);
+    nan |= __shfl_xor(nan, 32, 64);
+    b |= (nan ? FP4_NAN : byte) << (8 * i);
   }
+  if (lg == 0) *(uint32_t*)(laid + chunk * CHUNK + 1024 + lr * 4) = b;
 }
 
 int refuse_linear(const char* entry, const char* why) {
