@@ -339,9 +339,10 @@ typedef struct {
  * bit of a floating-point code's precision, and the value it stands for is exact in bfloat16 and float.  Rounding is to nearest,
  * ties to even, but never beyond the largest of these values, 240 * 2^120; a value that is not finite reads back as NaN.
  * DP_KV_FP4: codes of 4 bits, two to a byte, the first one in its low half (OCP e2m1: sign, 0 0.5 1 1.5 2 3 4 6); each group of 32 values of a token's head
- * has one power of two, the least 2^e with -100 <= e <= 125 by which no finite value of the group exceeds 7, held as the byte e + 127 (27 .. 252).  Rounding
- * is to nearest, ties to even, and from 5 on to 6: up to 7 by half of the codes' last step at most, as any other code.  The value that a code stands for is exact in bfloat16 and float.  A
- * group with a value that is not finite has the byte 255 and reads back as NaN, all of it. */
+ * has one power of two, the least 2^e with -100 <= e <= 125 by which no finite value of the group exceeds 7 (125 where none does: values above 7 * 2^125 become
+ * 6 * 2^125), held as the byte e + 127 (27 .. 252; a group of zeros has 27).  Rounding is to nearest, ties to even: 2.5 times the power to 2, 3.5 to 4, 5 to 4, and all above 5 to 6, up to 7 by half of
+ * the codes' last step at most, as any other code.  The value that a code stands for is exact in bfloat16 and float.  A group with a value that is not finite has the byte 255 and reads back as
+ * NaN, all of it. */
 enum { DP_KV_PLAIN = 0, DP_KV_FP8 = 1, DP_KV_FP4 = 4 };
 typedef struct {
   int32_t kv_heads;           /* 1 .. 1024                                                         */
@@ -431,7 +432,7 @@ int dp_attn_paged(const dp_kv_cache* cache, const dp_attn_config* cfg, const dp_
  *   y      : device, token t's out values at y + t * y_stride, of dtype; must not overlap anything that is read
  * Sums are fp32: an input of 32 bits is multiplied in three exact parts of 8 bits (parts below 2^-126 may count as 0, as inputs of 16 bits below it may), a weight is exact, the
  * activation is fp32; one rounding at the end.  A token's result does not depend on the tokens beside it, but for the order of its sum, which goes by the number of tokens; a call
- * repeats its bits.  What is not finite in x reaches that token's outputs as in exact arithmetic (infinity times 0 is NaN), a NaN byte its row's.
+ * repeats its bits.  What is not finite in x reaches that token's outputs as in exact arithmetic (infinity times 0 is NaN; so is either activation of -infinity, as its formula), a NaN byte its row's.
  *   workspace  : device, 256-byte aligned, dp_linear_fp4_workspace_bytes(w, n) bytes (0 for many calls: then it may be NULL), used by one call at a time; nothing has to be
  *                kept in it between calls.
  * n == 0 is a no-op.  Asynchronous on hip_stream; allocates nothing and may be recorded into a HIP graph.
