@@ -496,14 +496,21 @@ __global__ __launch_bounds__(256) void k_lay(const uint8_t* codes, const uint8_t
   for (int i = 0; i < 4; ++i) w[i] = row < out && step * 4 + i < groups ? *(const uint32_t*)(codes + row * (in / 2) + (step * 4 + i) * 16 + lg * 4) : 0u;
   *(uint4*)(laid + chunk * CHUNK + lane * 16) = make_uint4(w[0], w[1], w[2], w[3]);
   uint32_t b = 0;
+  if (lg == 0)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t byte = row < out && step * 4 + i < groups ? scales[row * groups + step * 4 + i] : 127u;
-    int nan = beyond(w[i], byte);
-    nan |= __shfl_xor(nan, 16, 64);
-    nan |= __shfl_xor(nan, 32, 64);
-    b |= (nan ? FP4_NAN : byte) << (8 * i);
-  }
+    for (int i = 0; i < 4; ++i) b |= (row < out && step * 4 + i < groups ? scales[row * groups + step * 4 + i] : 127u) << (8 * i);
+  b = (uint32_t)__shfl((int)b, lr, 64);    // a row's bytes, to the lanes that have its codes
+  uint32_t high = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) high |= (b >> (8 * i) & 255u) - 253u < 2u;
+  if (__any(high))
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int nan = beyond(w[i], b >> (8 * i) & 255u);
+      nan |= __shfl_xor(nan, 16, 64);
+      nan |= __shfl_xor(nan, 32, 64);
+      b |= nan ? FP4_NAN << (8 * i) : 0u;
+    }
   if (lg == 0) *(uint32_t*)(laid + chunk * CHUNK + 1024 + lr * 4) = b;
 }
 
