@@ -787,7 +787,7 @@ Route route(const PagedArgs& a, int head_dim, int format) {
         r.parts = (int)((keys + r.part_keys - 1) / r.part_keys);
       }
     } else if (blocks < 8192 && blocks * units < INT_MAX) {
-      // Equal runs of all sequences' keys, two blocks a CU, where there is so much work that lengths below the bound count for more than a plan: 64 sequences of 100 to
+      // Equal runs of all sequences' keys, as many blocks as a CU holds (few_per_cu), where there is so much work that lengths below the bound count for more than a plan: 64 sequences of 100 to
       // 16000 keys 215 us.  Equal lengths lose little: 8 of 16000 keys with 8 heads 51 us, in ranges 47; 4 of 6000 23 and 17.  Not for sequences up to 2048
       // keys (64 of 2000 52 and 44), nor for very many; units are counted in 32 bits.
       const int64_t most = 256 * few_per_cu(head_dim, rows <= 16 ? 1 : 2, format);

@@ -4,8 +4,10 @@
 // v_mfma_f32_16x16x32_bf16: 16 outputs of a row tile against 16 tokens.  fp32 inputs are split into three bf16 parts of 8 bits each, which together are
 // the input exactly (as far as bf16 reaches down: a part below 2^-126 may be lost), so that fp32 takes the same instructions three times instead of ones of 1/16 the rate; all sums are fp32.
 //
-// What bounds it: few tokens, the codes' way from memory (5120 -> 13824, one token 9.4 us, 4.0 TB/s); many, the matrix pipes (6240 tokens 5120 -> 5120 262 us, 1.25
-// PFLOP/s; fp32 1560 tokens 1536 -> 8960 127 us, 338 TFLOP/s, beside the parts' arithmetic).
+// What bounds it: a few tokens, the codes' way and the steps' latency around it: one token, 5120 -> 13824, 10.7 us with matrices out of memory, 9.2 with one out of the last-level cache,
+// where a kernel that reads as many bytes and no more takes 7.0 and 4.2 (16 tokens 11.6 and 9.2).  Some 20 to 500 tokens, conversions and reads of LDS, which each tile of tokens repeats: 48 tokens, 13824 -> 5120, 16 us out of the
+// cache (memory 7, products 5), 256 tokens, 5120 -> 5120, 20 (products 10).  Many, the matrix pipes: 6240 tokens, 5120 -> 5120, 256 us, 1.28 PFLOP/s.  fp32 pays three instructions and the splitting, which
+// each wavefront repeats: one token, 13824 -> 5120, 29 us (bf16 11 to 13), 48 tokens 47, 1560 tokens, 1536 -> 8960, 127, 338 TFLOP/s.
 #include <math.h>
 #include <stdio.h>
 
@@ -385,8 +387,10 @@ template <typename T, int R, int NT, int WR, int WT, int WK, int NS> void launch
   if (a.parts > 1) k_join<T><<<(unsigned)((a.n * a.out + 255) / 256), 256, 0, st>>>(a);
 }
 // The tiles there are, and what they take: rows and tokens of a block, its groups (WK), how many of them a CU holds, and in units of 10 ns a group's step with 1, 2 .. blocks
-// on a CU in the last round of blocks, in the rounds before it, and what is done around the steps.  Fitted to 2595 launches: 512 .. 13824 outputs, 1504 .. 13824 inputs, 1 .. 6240
-// tokens; the estimate below then takes a tile within 0.5 % of the best one on average, 11 % at worst.  Tiles of tokens in steps of 16 or 32 are worth their code where a round of blocks ends
+// on a CU in the last round of blocks, in the rounds before it, and what is done around the steps.  Fitted to some 2600 launches: 512 .. 13824 outputs, 1504 .. 13824 inputs, 1 .. 6240
+// tokens.  Against the best tile measured, what the estimate below takes with these constants is 1.0 % slower on average over 95 shapes in bf16 and 0.6 % over 79 in fp32; at worst 23 % (1200 tokens, 5120 ->
+// 5120: tiles of 128 x 64 83 us, of 128 x 48 68), 18 % (48 tokens, 1536 -> 8960), 10 %.  A remainder of blocks behind a full round is charged as one block a CU, while places come free in pairs.
+// Tiles of tokens in steps of 16 or 32 are worth their code where a round of blocks ends
 // just so: 1560 tokens, 8960 -> 1536, 46 us, with 64, 128, 192 and 256 alone 99; 800 tokens, 5120 -> 5120, 45 and 68; 1560 tokens, 1536 -> 8960, 39 and 42; fp32, 1560 tokens, 1536 -> 1536, 33 and 41.
 struct Tile { int rows, tokens, groups, per_cu, last[3], full, around; };
 #define TILES_BF16(X) \
